@@ -432,6 +432,89 @@ kvtc_status kvtc_offsets_append(const kvtc_batch* batch, const kvtc_job* jobs_de
                                 const uint64_t* region_dev, const int64_t* n_coded_dev,
                                 uint64_t* offsets_dev, kvtc_stream stream);
 
+/*
+ * ---- The live cache: pages, quantised as they are written ----------------------------------
+ * (paper, Section "Method": the coder compresses caches that an attention kernel has written and will read
+ * again; Section "Sliding Windows and Sink Tokens": what has not been coded stays in 16 bits or in FP8.)
+ * A cache of one layer lives in a pool of n_pages pages of page_tokens tokens each, for keys and for values:
+ * the row of (page, head, token in the page) is d_head values at
+ *     k_dev + page * page_stride + head * head_stride + token * token_stride          (bytes; v_dev likewise)
+ * in one of three formats:
+ *   KVTC_CACHE_BF16   d_head bf16 values (to nearest even)
+ *   KVTC_CACHE_FP8    d_head bytes of OCP E4M3 and an fp32 scale per row: scale = a / 448 for the row's largest
+ *                     finite magnitude a (0 where that is below 2^-126; all codes are then 0 or NaN), code =
+ *                     E4M3(x * (1 / scale)), to nearest even; infinities give +-448 and NaN stays NaN.  Value = code * scale.
+ *   KVTC_CACHE_INT4   4-bit codes, and for every 32 features the coder's own header: fp16 shift (low half), fp16
+ *                     scale (high half), both and the codes decided as in a record's group of 4 bits (see above; NaN gives an
+ *                     unspecified code).  Feature f's code is in byte (f % 32) / 2 * (d_head / 32) + f / 32 of the
+ *                     row, the low four bits for even f.  Value = shift + code * scale.
+ * Scales and headers are arrays of their own, [n_pages][n_heads][page_tokens] entries of kvtc_cache_scale_bytes.
+ * The strides may nest in any order (pages of [heads][tokens][d_head] or [tokens][heads][d_head], one slab
+ * per head cut into pages, ...) but rows must not overlap (KVTC_E_ARG).
+ *   d_head        64, 128 or 256 (KVTC_E_UNSUPPORTED otherwise)
+ *   page_tokens   at least 1, of any size; (page_tokens - 1) * token_stride + a row below 2^31
+ *   n_heads       1 .. 1024; n_pages 1 .. 2^31 - 1
+ *   bases and strides 16-byte aligned; the scale arrays are not read in KVTC_CACHE_BF16 (may be null)
+ */
+typedef enum { KVTC_CACHE_BF16 = 0, KVTC_CACHE_FP8 = 1, KVTC_CACHE_INT4 = 2 } kvtc_cache_format;
+typedef struct {
+    int32_t format, n_heads, d_head, page_tokens;
+    int64_t n_pages, page_stride, head_stride, token_stride;     /* strides in bytes */
+    void *k_dev, *v_dev, *k_scales_dev, *v_scales_dev;
+} kvtc_cache;
+size_t kvtc_cache_row_bytes(kvtc_cache_format format, int d_head);      /* of a head's row of one token; 0 for what is not supported */
+size_t kvtc_cache_scale_bytes(kvtc_cache_format format, int d_head);    /* of that row's scale or headers (0 in bf16)                */
+
+/*
+ * Tokens into the cache and out of it.  Feature f of head h of token i sits at
+ * x[i * token_stride + h * head_stride + f] (elements of `dtype`; base and strides 16-byte aligned, heads and tokens not
+ * overlapping, as kvtc_rope), for keys and values alike; the token's place is slots_dev[i] (device, 8-byte aligned) =
+ * page * page_tokens + token in the page.  A negative slot is no place (padding of a batch): nothing is written, and read gives
+ * zeros.  A slot beyond the pool is treated so as well, and *status_dev (device, may be null; the caller zeroes it) becomes
+ * 1 + the index of the lowest such token.  Two tokens with the same slot in one write leave either's rows, not
+ * necessarily the same one's for all heads.  Quantisation looks at one token at a time: a write of many tokens leaves what
+ * writes of single tokens leave.  fp32 features are not rounded before they are quantised.
+ * kvtc_cache_read rounds once to dtype (nearest even).  Both are ordered on `stream`, allocate nothing and do not
+ * synchronise; n_tokens == 0 is a no-op.
+ */
+kvtc_status kvtc_cache_write(const kvtc_cache* cache, const void* k_dev, const void* v_dev, kvtc_dtype dtype, int64_t n_tokens,
+                             int64_t token_stride, int64_t head_stride, const int64_t* slots_dev, uint32_t* status_dev,
+                             kvtc_stream stream);
+kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, int64_t n_tokens, void* k_out_dev, void* v_out_dev,
+                            kvtc_dtype dtype, int64_t token_stride, int64_t head_stride, uint32_t* status_dev, kvtc_stream stream);
+
+/*
+ * Attention of one new token of every sequence over its pages (a decode step; the new token's own keys and values are
+ * in the cache already).  For sequence b and query head h, which reads KV head h / (n_q_heads / n_heads):
+ *     s_t = scale * q . k_t,   out = sum_t e^(s_t) v_t / sum_t e^(s_t),   lse = log sum_t e^(s_t)
+ * over the tokens t < lengths_dev[b] that are seen: all of them if window == 0, else t < sinks or t >= length - window
+ * (the sinks and the window of a streaming cache).  A row that sees no token (or only scores of minus infinity) gives out = 0 and lse = minus infinity; lse lets
+ * a caller join this with attention over other tokens.  What lies in pages beyond a sequence's tokens, or in tokens
+ * that are not seen, is never part of a result, whatever it holds.
+ *   q_dev         [n_seqs][n_q_heads][d_head] of `dtype` with strides in elements (base and strides 16-byte aligned);
+ *                 n_q_heads a multiple of the cache's n_heads, at most 1024; n_seqs at most 65536
+ *   pages_dev     page number of token t of sequence b: pages_dev[b * pages_stride + t / page_tokens] (device, int32);
+ *                 entries beyond a sequence's last token, or of pages without a seen token, are not looked at
+ *   lengths_dev   tokens per sequence (device, int32), at most max_tokens, the host's bound for sizing the launch;
+ *                 pages_stride >= ceil(max_tokens / page_tokens)
+ *   out_dev       [n_seqs][n_q_heads][d_head] of `dtype`, contiguous, 16-byte aligned; lse_dev [n_seqs][n_q_heads] fp32, or null
+ *   work_dev      kvtc_attend_work_bytes(...) bytes of device memory, 256-byte aligned (work_bytes less: KVTC_E_SMALL), all zero
+ *                 before its first use (a call leaves zero what the next one needs so): calls on one stream may share
+ *                 it, of any sizes that it is large enough for; calls that may overlap need one each
+ *   status_dev    as above: 1 + the lowest sequence whose length is negative or above max_tokens (its rows become 0 and minus infinity) or
+ *                 one of whose pages with seen tokens is not in the pool (those tokens are not seen)
+ * Sums and softmax statistics are fp32, products of bf16 values and codes are exact in them; probabilities enter their
+ * product with the values as two bf16 parts (16 bits), for fp32 queries and outputs as three (24 bits), queries as one or three.
+ * The result is rounded once to dtype.  A fixed split and order of summation: results are reproducible.
+ * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 is a no-op.
+ */
+size_t kvtc_attend_work_bytes(const kvtc_cache* cache, int n_seqs, int n_q_heads, int64_t max_tokens);     /* 0 for what kvtc_attend refuses */
+kvtc_status kvtc_attend(const kvtc_cache* cache, const void* q_dev, kvtc_dtype dtype, int n_seqs, int n_q_heads,
+                        int64_t q_seq_stride, int64_t q_head_stride, const int32_t* pages_dev, int64_t pages_stride,
+                        const int32_t* lengths_dev, int64_t max_tokens, float scale, int64_t sinks, int64_t window,
+                        void* out_dev, float* lse_dev, void* work_dev, size_t work_bytes, uint32_t* status_dev,
+                        kvtc_stream stream);
+
 /* Thread-local text for the last non-OK status returned on this thread (static storage). */
 const char* kvtc_last_error(void);
 

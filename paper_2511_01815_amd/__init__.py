@@ -18,6 +18,8 @@ from .binding import (  # noqa: F401
     EntropyTables, kvtc_entropy_create, kvtc_entropy_destroy, kvtc_entropy_bound, kvtc_entropy_encode, kvtc_entropy_decode,
     kvtc_entropy_encode_batch, kvtc_entropy_decode_batch, make_entropy_jobs, ENTROPY_JOB_DTYPE,
     kvtc_calib_block_errors, kvtc_calib_moments,
+    KVTC_CACHE_BF16, KVTC_CACHE_FP8, KVTC_CACHE_INT4, KvtcCache, cache, kvtc_cache_row_bytes, kvtc_cache_scale_bytes,
+    kvtc_cache_write, kvtc_cache_read, kvtc_attend_work_bytes, kvtc_attend,
     KvtcLayout, layout, kvtc_encode_blocked, kvtc_decode_blocked, kvtc_encode_batch_blocked, kvtc_decode_batch_blocked,
 )
 from . import bundles  # noqa: F401

@@ -8,6 +8,7 @@ from typing import Optional, Sequence, Tuple
 import numpy as np
 
 KVTC_BF16, KVTC_F32 = 0, 1
+KVTC_CACHE_BF16, KVTC_CACHE_FP8, KVTC_CACHE_INT4 = 0, 1, 2
 _STATUS = {0: "KVTC_OK", 1: "KVTC_E_ARG", 2: "KVTC_E_UNSUPPORTED", 3: "KVTC_E_SMALL", 4: "KVTC_E_HIP", 5: "KVTC_E_NOMEM"}
 
 # layout of kvtc_job: { int32 plan; int32 n_tokens; int64 x_row0; }
@@ -30,6 +31,12 @@ class KvtcSplit(C.Structure):
 
 class KvtcLayout(C.Structure):
     _fields_ = [("token_stride", C.c_int64), ("block_features", C.c_int32), ("reserved", C.c_int32), ("block_stride", C.c_int64)]
+
+
+class KvtcCache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("n_heads", C.c_int32), ("d_head", C.c_int32), ("page_tokens", C.c_int32),
+                ("n_pages", C.c_int64), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_scales_dev", C.c_void_p), ("v_scales_dev", C.c_void_p)]
 
 
 def lib_path() -> str:
@@ -117,6 +124,18 @@ def lib() -> C.CDLL:
         L.kvtc_calib_moments.restype = C.c_int
         L.kvtc_rope.argtypes = [vp, C.c_int, i64, C.c_int, C.c_int, i64, i64, vp, i64, C.c_double, C.c_int, C.c_int, vp]
         L.kvtc_rope.restype = C.c_int
+        cp = C.POINTER(KvtcCache)
+        L.kvtc_cache_row_bytes.argtypes = [C.c_int, C.c_int]
+        L.kvtc_cache_row_bytes.restype = sz
+        L.kvtc_cache_scale_bytes.argtypes = [C.c_int, C.c_int]
+        L.kvtc_cache_scale_bytes.restype = sz
+        L.kvtc_cache_write.argtypes = [cp, vp, vp, C.c_int, i64, i64, i64, vp, vp, vp]
+        L.kvtc_cache_read.argtypes = [cp, vp, i64, vp, vp, C.c_int, i64, i64, vp, vp]
+        L.kvtc_attend_work_bytes.argtypes = [cp, C.c_int, C.c_int, i64]
+        L.kvtc_attend_work_bytes.restype = sz
+        L.kvtc_attend.argtypes = [cp, vp, C.c_int, C.c_int, C.c_int, i64, i64, vp, i64, vp, i64, C.c_float, i64, i64, vp, vp, vp, sz, vp, vp]
+        for f in (L.kvtc_cache_write, L.kvtc_cache_read, L.kvtc_attend):
+            f.restype = C.c_int
         L.kvtc_last_error.argtypes = []
         L.kvtc_last_error.restype = C.c_char_p
         L.kvtc_host_f16_round_down.argtypes = [C.c_float]
@@ -326,6 +345,45 @@ def kvtc_rope(x_dev, dtype: int, n_tokens: int, n_heads: int, d_head: int, token
     _check(lib().kvtc_rope(_ptr(x_dev), dtype, n_tokens, n_heads, d_head, token_stride, head_stride,
                            _ptr(positions_dev) if positions_dev is not None else None, position0, float(base), pairing,
                            1 if inverse else 0, _stream(stream)))
+
+
+def cache(format: int, n_pages: int, page_tokens: int, n_heads: int, d_head: int, k_dev, v_dev, page_stride: int, head_stride: int,
+          token_stride: int, k_scales_dev=None, v_scales_dev=None) -> "KvtcCache":
+    """A kvtc_cache over the caller's buffers (which must outlive it); strides in bytes."""
+    return KvtcCache(format, n_heads, d_head, page_tokens, n_pages, page_stride, head_stride, token_stride,
+                     _ptr(k_dev), _ptr(v_dev), _ptr(k_scales_dev), _ptr(v_scales_dev))
+
+
+def kvtc_cache_row_bytes(format: int, d_head: int) -> int:
+    return lib().kvtc_cache_row_bytes(format, d_head)
+
+
+def kvtc_cache_scale_bytes(format: int, d_head: int) -> int:
+    return lib().kvtc_cache_scale_bytes(format, d_head)
+
+
+def kvtc_cache_write(cache, k_dev, v_dev, dtype: int, n_tokens: int, token_stride: int, head_stride: int, slots_dev,
+                     status_dev=None, stream=None) -> None:
+    _check(lib().kvtc_cache_write(C.byref(cache), _ptr(k_dev), _ptr(v_dev), dtype, n_tokens, token_stride, head_stride,
+                                  _ptr(slots_dev), _ptr(status_dev), _stream(stream)))
+
+
+def kvtc_cache_read(cache, slots_dev, n_tokens: int, k_out_dev, v_out_dev, dtype: int, token_stride: int, head_stride: int,
+                    status_dev=None, stream=None) -> None:
+    _check(lib().kvtc_cache_read(C.byref(cache), _ptr(slots_dev), n_tokens, _ptr(k_out_dev), _ptr(v_out_dev), dtype,
+                                 token_stride, head_stride, _ptr(status_dev), _stream(stream)))
+
+
+def kvtc_attend_work_bytes(cache, n_seqs: int, n_q_heads: int, max_tokens: int) -> int:
+    return lib().kvtc_attend_work_bytes(C.byref(cache), n_seqs, n_q_heads, max_tokens)
+
+
+def kvtc_attend(cache, q_dev, dtype: int, n_seqs: int, n_q_heads: int, q_seq_stride: int, q_head_stride: int, pages_dev, pages_stride: int,
+                lengths_dev, max_tokens: int, scale: float, sinks: int, window: int, out_dev, lse_dev, work_dev, work_bytes: int,
+                status_dev=None, stream=None) -> None:
+    _check(lib().kvtc_attend(C.byref(cache), _ptr(q_dev), dtype, n_seqs, n_q_heads, q_seq_stride, q_head_stride, _ptr(pages_dev),
+                             pages_stride, _ptr(lengths_dev), max_tokens, scale, sinks, window, _ptr(out_dev), _ptr(lse_dev),
+                             _ptr(work_dev), work_bytes, _ptr(status_dev), _stream(stream)))
 
 
 def kvtc_probe_stream(mode: int, src_dev, dst_dev, nbytes: int, stream=None) -> None:

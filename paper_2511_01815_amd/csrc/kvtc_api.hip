@@ -11,6 +11,7 @@
 #include <new>
 #include <vector>
 
+#include "kvtc_cache.h"
 #include "kvtc_dev.h"
 #include "kvtc_numeric.h"
 #include "../../include/kvtc_test_hooks.h"
@@ -1383,6 +1384,132 @@ kvtc_status kvtc_calib_moments(const void* x_dev, kvtc_dtype dtype, int64_t n_to
     const hipError_t e = launch_calib_moments(x_dev, dtype, n_tokens, p, xl.ld, xl.blk_log2, xl.blk_jump, sum_dev, gram_dev,
                                               static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(KVTC_E_HIP, "kvtc_calib_moments: launch failed: %s", hipGetErrorString(e));
+    return KVTC_OK;
+}
+
+// ---- the live cache ----------------------------------------------------------------------------------
+
+size_t kvtc_cache_row_bytes(kvtc_cache_format format, int d_head) {
+    const bool ok = (unsigned)format <= KVTC_CACHE_INT4 && (d_head == 64 || d_head == 128 || d_head == 256);
+    return ok ? (size_t)cache_row_bytes((int)format, d_head) : 0;
+}
+
+size_t kvtc_cache_scale_bytes(kvtc_cache_format format, int d_head) {
+    return kvtc_cache_row_bytes(format, d_head) ? (size_t)cache_scale_bytes((int)format, d_head) : 0;
+}
+
+static kvtc_status check_cache(const char* who, const kvtc_cache* c) {
+    if (!c) return fail(KVTC_E_ARG, "%s: null cache", who);
+    if ((unsigned)c->format > KVTC_CACHE_INT4) return fail(KVTC_E_ARG, "%s: unknown cache format %d", who, c->format);
+    if (c->d_head != 64 && c->d_head != 128 && c->d_head != 256) return fail(KVTC_E_UNSUPPORTED, "%s: d_head=%d (64, 128 and 256 are served)", who, c->d_head);
+    if (c->n_heads < 1 || c->n_heads > kCacheMaxHeads) return fail(KVTC_E_ARG, "%s: n_heads=%d outside 1..%d", who, c->n_heads, kCacheMaxHeads);
+    if (c->page_tokens < 1 || c->n_pages < 1 || c->n_pages > 0x7fffffffLL)
+        return fail(KVTC_E_ARG, "%s: need page_tokens >= 1 and 1 <= n_pages < 2^31 (page_tokens=%d n_pages=%lld)", who, c->page_tokens, (long long)c->n_pages);
+    if (!c->k_dev || !c->v_dev) return fail(KVTC_E_ARG, "%s: null pool", who);
+    const int64_t row = cache_row_bytes(c->format, c->d_head);
+    if (((reinterpret_cast<uintptr_t>(c->k_dev) | reinterpret_cast<uintptr_t>(c->v_dev)) & 15u) || ((c->page_stride | c->head_stride | c->token_stride) & 15))
+        return fail(KVTC_E_ARG, "%s: pools and strides must be 16-byte aligned", who);
+    // rows must not overlap: the dimensions of more than one, by stride, each beyond the extent of those before it
+    struct { int64_t stride, count; } dim[3] = {{c->page_stride, c->n_pages}, {c->head_stride, c->n_heads}, {c->token_stride, c->page_tokens}};
+    std::sort(dim, dim + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    __int128 extent = row;
+    for (const auto& d : dim) {
+        if (d.count == 1) continue;
+        if ((__int128)d.stride < extent)
+            return fail(KVTC_E_ARG, "%s: strides (page %lld, head %lld, token %lld) let rows overlap", who, (long long)c->page_stride, (long long)c->head_stride, (long long)c->token_stride);
+        extent += (__int128)d.stride * (d.count - 1);
+    }
+    if (extent > (__int128)0x7fffffffffffffffLL) return fail(KVTC_E_ARG, "%s: the pool's extent passes 63 bits", who);
+    if ((__int128)c->token_stride * (c->page_tokens - 1) + row > (__int128)0x7fffffff)
+        return fail(KVTC_E_ARG, "%s: the tokens of a page extend over 2^31 bytes or more", who);
+    if (c->format != KVTC_CACHE_BF16) {
+        if (!c->k_scales_dev || !c->v_scales_dev) return fail(KVTC_E_ARG, "%s: null scales", who);
+        if ((reinterpret_cast<uintptr_t>(c->k_scales_dev) | reinterpret_cast<uintptr_t>(c->v_scales_dev)) & 15u) return fail(KVTC_E_ARG, "%s: scales must be 16-byte aligned", who);
+    }
+    return KVTC_OK;
+}
+
+// Features of n_tokens tokens, all heads, and where they go in the cache.
+static kvtc_status check_tokens(const char* who, const kvtc_cache* c, const void* k, const void* v, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride,
+                                int64_t head_stride, const int64_t* slots, const uint32_t* status) {
+    const kvtc_status st = check_cache(who, c);
+    if (st != KVTC_OK) return st;
+    if (!dtype_ok(dtype)) return fail(KVTC_E_ARG, "%s: unknown dtype %d", who, (int)dtype);
+    if (n_tokens < 0 || n_tokens > 0x7fffffffLL) return fail(KVTC_E_ARG, "%s: n_tokens=%lld", who, (long long)n_tokens);
+    if (n_tokens == 0) return KVTC_OK;
+    if (!k || !v || !slots) return fail(KVTC_E_ARG, "%s: null buffer", who);
+    const int64_t e = (int64_t)elem_size(dtype), d = c->d_head, far = (int64_t)1 << 40;
+    if (((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) || (token_stride * e) % 16 != 0 || (head_stride * e) % 16 != 0)
+        return fail(KVTC_E_ARG, "%s: features and their strides must be 16-byte aligned", who);
+    if ((reinterpret_cast<uintptr_t>(slots) & 7u) || (reinterpret_cast<uintptr_t>(status) & 3u)) return fail(KVTC_E_ARG, "%s: slots must be 8-byte aligned, status 4", who);
+    const bool in_range = token_stride >= 0 && token_stride <= far && head_stride >= 0 && head_stride <= far;
+    const bool tokens_major = in_range && (c->n_heads == 1 || head_stride >= d) && (n_tokens == 1 || token_stride >= (c->n_heads - 1) * head_stride + d);
+    const bool heads_major = in_range && (n_tokens == 1 || token_stride >= d) && (c->n_heads == 1 || (__int128)head_stride >= (__int128)(n_tokens - 1) * token_stride + d);
+    if (!tokens_major && !heads_major)
+        return fail(KVTC_E_ARG, "%s: strides (token %lld, head %lld) let elements overlap", who, (long long)token_stride, (long long)head_stride);
+    return KVTC_OK;
+}
+
+kvtc_status kvtc_cache_write(const kvtc_cache* cache, const void* k_dev, const void* v_dev, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride,
+                             int64_t head_stride, const int64_t* slots_dev, uint32_t* status_dev, kvtc_stream stream) {
+    const kvtc_status st = check_tokens("kvtc_cache_write", cache, k_dev, v_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev);
+    if (st != KVTC_OK || n_tokens == 0) return st;
+    const CacheTokenArgs a{*cache, const_cast<void*>(k_dev), const_cast<void*>(v_dev), token_stride, head_stride, slots_dev, n_tokens, status_dev};
+    const hipError_t e = launch_cache_write(a, dtype, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(KVTC_E_HIP, "kvtc_cache_write: launch failed: %s", hipGetErrorString(e));
+    return KVTC_OK;
+}
+
+kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, int64_t n_tokens, void* k_out_dev, void* v_out_dev, kvtc_dtype dtype,
+                            int64_t token_stride, int64_t head_stride, uint32_t* status_dev, kvtc_stream stream) {
+    const kvtc_status st = check_tokens("kvtc_cache_read", cache, k_out_dev, v_out_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev);
+    if (st != KVTC_OK || n_tokens == 0) return st;
+    const CacheTokenArgs a{*cache, k_out_dev, v_out_dev, token_stride, head_stride, slots_dev, n_tokens, status_dev};
+    const hipError_t e = launch_cache_read(a, dtype, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(KVTC_E_HIP, "kvtc_cache_read: launch failed: %s", hipGetErrorString(e));
+    return KVTC_OK;
+}
+
+static kvtc_status check_attend(const char* who, const kvtc_cache* c, int n_seqs, int n_q_heads, int64_t max_tokens) {
+    const kvtc_status st = check_cache(who, c);
+    if (st != KVTC_OK) return st;
+    if (n_seqs < 0 || n_seqs > kAttendMaxSeqs) return fail(KVTC_E_ARG, "%s: n_seqs=%d outside 0..%d", who, n_seqs, kAttendMaxSeqs);
+    if (n_q_heads < 1 || n_q_heads > kCacheMaxHeads || n_q_heads % c->n_heads != 0)
+        return fail(KVTC_E_ARG, "%s: n_q_heads=%d must be a multiple of the cache's %d heads, at most %d", who, n_q_heads, c->n_heads, kCacheMaxHeads);
+    if (max_tokens < 1 || max_tokens > 0x7fffffffLL) return fail(KVTC_E_ARG, "%s: max_tokens=%lld outside 1..2^31-1", who, (long long)max_tokens);
+    return KVTC_OK;
+}
+
+size_t kvtc_attend_work_bytes(const kvtc_cache* cache, int n_seqs, int n_q_heads, int64_t max_tokens) {
+    return check_attend("kvtc_attend_work_bytes", cache, n_seqs, n_q_heads, max_tokens) == KVTC_OK ? attend_work_bytes(*cache, n_seqs, n_q_heads, max_tokens) : 0;
+}
+
+kvtc_status kvtc_attend(const kvtc_cache* cache, const void* q_dev, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t q_seq_stride, int64_t q_head_stride,
+                        const int32_t* pages_dev, int64_t pages_stride, const int32_t* lengths_dev, int64_t max_tokens, float scale, int64_t sinks,
+                        int64_t window, void* out_dev, float* lse_dev, void* work_dev, size_t work_bytes, uint32_t* status_dev, kvtc_stream stream) {
+    const kvtc_status st = check_attend("kvtc_attend", cache, n_seqs, n_q_heads, max_tokens);
+    if (st != KVTC_OK) return st;
+    if (!dtype_ok(dtype)) return fail(KVTC_E_ARG, "kvtc_attend: unknown dtype %d", (int)dtype);
+    if (!std::isfinite(scale)) return fail(KVTC_E_ARG, "kvtc_attend: scale must be finite");
+    if (sinks < 0 || window < 0) return fail(KVTC_E_ARG, "kvtc_attend: sinks=%lld window=%lld", (long long)sinks, (long long)window);
+    if (n_seqs == 0) return KVTC_OK;
+    if (!q_dev || !pages_dev || !lengths_dev || !out_dev || !work_dev) return fail(KVTC_E_ARG, "kvtc_attend: null buffer");
+    const int64_t e = (int64_t)elem_size(dtype), far = (int64_t)1 << 40;
+    if (q_seq_stride < 0 || q_seq_stride > far || q_head_stride < 0 || q_head_stride > far)
+        return fail(KVTC_E_ARG, "kvtc_attend: query strides (sequence %lld, head %lld)", (long long)q_seq_stride, (long long)q_head_stride);
+    if (((reinterpret_cast<uintptr_t>(q_dev) | reinterpret_cast<uintptr_t>(out_dev)) & 15u) || (q_seq_stride * e) % 16 != 0 || (q_head_stride * e) % 16 != 0)
+        return fail(KVTC_E_ARG, "kvtc_attend: queries, their strides and the output must be 16-byte aligned");
+    if (((reinterpret_cast<uintptr_t>(pages_dev) | reinterpret_cast<uintptr_t>(lengths_dev) | reinterpret_cast<uintptr_t>(lse_dev) | reinterpret_cast<uintptr_t>(status_dev)) & 3u) ||
+        (reinterpret_cast<uintptr_t>(work_dev) & 255u))
+        return fail(KVTC_E_ARG, "kvtc_attend: misaligned table, lengths, lse, status (4 bytes) or workspace (256)");
+    if (pages_stride < (max_tokens + cache->page_tokens - 1) / cache->page_tokens)
+        return fail(KVTC_E_ARG, "kvtc_attend: pages_stride=%lld holds less than max_tokens=%lld", (long long)pages_stride, (long long)max_tokens);
+    const size_t need = attend_work_bytes(*cache, n_seqs, n_q_heads, max_tokens);
+    if (work_bytes < need) return fail(KVTC_E_SMALL, "kvtc_attend: work_bytes=%zu < %zu", work_bytes, need);
+    const AttendArgs a{*cache, q_dev, q_seq_stride, q_head_stride, pages_dev, pages_stride, lengths_dev, max_tokens, sinks, window, scale, n_seqs, n_q_heads,
+                       out_dev, lse_dev, work_dev, status_dev};
+    const hipError_t err = launch_attend(a, dtype, static_cast<hipStream_t>(stream));
+    if (err != hipSuccess) return fail(KVTC_E_HIP, "kvtc_attend: launch failed: %s", hipGetErrorString(err));
     return KVTC_OK;
 }
 
