@@ -441,12 +441,13 @@ kvtc_status kvtc_offsets_append(const kvtc_batch* batch, const kvtc_job* jobs_de
  *     k_dev + page * page_stride + head * head_stride + token * token_stride          (bytes; v_dev likewise)
  * in one of three formats:
  *   KVTC_CACHE_BF16   d_head bf16 values (to nearest even)
- *   KVTC_CACHE_FP8    d_head bytes of OCP E4M3 and an fp32 scale per row: scale = a / 448 for the row's largest
+ *   KVTC_CACHE_FP8    d_head bytes of OCP E4M3 and an fp32 scale per row: scale = a * (1 / 448) for the row's largest
  *                     finite magnitude a (0 where that is below 2^-126; all codes are then 0 or NaN), code =
  *                     E4M3(x * (1 / scale)), to nearest even; infinities give +-448 and NaN stays NaN.  Value = code * scale.
  *   KVTC_CACHE_INT4   4-bit codes, and for every 32 features the coder's own header: fp16 shift (low half), fp16
- *                     scale (high half), both and the codes decided as in a record's group of 4 bits (see above; NaN gives an
- *                     unspecified code).  Feature f's code is in byte (f % 32) / 2 * (d_head / 32) + f / 32 of the
+ *                     scale (high half), both and the codes decided as in a record's group of 4 bits (see above), but
+ *                     the range is multiplied by fp32 1 / 15 where that divides it by 15; NaN gives an unspecified
+ *                     code.  Feature f's code is in byte (f % 32) / 2 * (d_head / 32) + f / 32 of the
  *                     row, the low four bits for even f.  Value = shift + code * scale.
  * Scales and headers are arrays of their own, [n_pages][n_heads][page_tokens] entries of kvtc_cache_scale_bytes.
  * The strides may nest in any order (pages of [heads][tokens][d_head] or [tokens][heads][d_head], one slab

@@ -7,9 +7,10 @@ the coder's own group quantiser, values and attention in float64, one sequence a
 library and imports nothing from it.
 
 Readings (the paper fixes none of these):
-  * 8 bits: E4M3 codes of x * (1 / scale), scale = (largest finite magnitude of the row) / 448, each a single float32 operation;
-    scales below 2^-126 count as 0 (all codes 0); NaN keeps its code, infinities give +-448;
-  * 4 bits: the coder's min-max quantiser (kvtc_oracle.quantise_group) over every 32 features, value = shift + code * scale;
+  * 8 bits: E4M3 codes of x * (1 / scale), scale = (largest finite magnitude of the row) * (1 / 448), each a single float32
+    operation; scales below 2^-126 count as 0 (all codes 0); NaN keeps its code, infinities give +-448;
+  * 4 bits: the coder's min-max quantiser (kvtc_oracle.quantise_group at 4 bits) over every 32 features, but for the range,
+    which is multiplied by float32 1 / 15 instead of divided by 15; value = shift + code * scale;
     byte pair * (d / 32) + group of a row holds features 2 * pair (low four bits) and 2 * pair + 1 of the group;
   * a softmax over no tokens, or over scores of minus infinity alone, gives zeros and a log-sum of minus infinity.
 
@@ -50,6 +51,18 @@ def e4m3_codes(x: np.ndarray) -> np.ndarray:
     return np.where(np.isnan(x), 0x7F, k).astype(np.uint8)
 
 
+def quantise_group(d32: np.ndarray):
+    """d32 [T, n] float32: shift [T] and scale [T] fp16, codes [T, n] of 4 bits."""
+    shift = ko.fp16_floor(d32.min(axis=1))
+    low = shift.astype(np.float32)
+    with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
+        scale = ko.fp16_ceil((d32.max(axis=1) - low) * (np.float32(1) / np.float32(15)))
+        s = scale.astype(np.float32)
+        inv = np.where(s > 0, np.float32(1) / s, np.float32(0)).astype(np.float32)
+        q = (d32 - low[:, None]) * inv[:, None]
+    return shift, scale, np.nan_to_num(np.clip(np.rint(q), 0, 15), nan=0.0).astype(np.uint8)
+
+
 def quantise(x: np.ndarray, fmt: str):
     """Rows x [..., d] (float32): (what the cache's rows hold as bytes [..., row_bytes], their scales as bytes or None)."""
     x = np.ascontiguousarray(x, dtype=np.float32)
@@ -58,16 +71,16 @@ def quantise(x: np.ndarray, fmt: str):
         return bf16_bits(x).view(np.uint8).reshape(*lead, 2 * d), None
     if fmt == "fp8":
         finite = np.where(np.isfinite(x), np.abs(x), np.float32(0))
-        scale = (finite.max(-1) / np.float32(448)).astype(np.float32)
+        scale = (finite.max(-1) * (np.float32(1) / np.float32(448))).astype(np.float32)
         scale = np.where(scale < np.float32(2.0 ** -126), np.float32(0), scale)
         with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
             inv = np.where(scale > 0, np.float32(1) / scale, np.float32(0)).astype(np.float32)
             y = np.where(np.isnan(x), x, np.where(inv[..., None] > 0, x * inv[..., None], np.float32(0)))
         return e4m3_codes(y), scale[..., None].view(np.uint8)
     g = x.reshape(-1, GROUP)
-    shift, scale, codes = ko.quantise_group(g, 4)
+    shift, scale, codes = quantise_group(g)
     header = np.stack([shift, scale], -1).reshape(*lead, -1)
-    pairs = codes.astype(np.uint8).reshape(*lead, d // GROUP, GROUP // 2, 2)
+    pairs = codes.reshape(*lead, d // GROUP, GROUP // 2, 2)
     packed = pairs[..., 0] | (pairs[..., 1] << 4)                # [..., group, pair]
     return np.ascontiguousarray(np.swapaxes(packed, -1, -2)).reshape(*lead, d // 2), np.ascontiguousarray(header).view(np.uint8)
 

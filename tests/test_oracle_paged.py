@@ -38,6 +38,19 @@ def test_values_are_near_what_was_quantised(d, fmt, most):
         assert (np.abs(got - x) <= most * np.abs(x) + 2.0 ** -9 * top / 448 * 1.01).all()
 
 
+def test_groups_of_four_bits_are_the_coders_but_for_a_last_place_of_the_scale():
+    """A range times 1 / 15 in float32 is within one place of the range divided by 15, so a scale is the coder's or its neighbour, and rarely that."""
+    rng = np.random.default_rng(6)
+    g = (rng.standard_normal((20000, 32)) * np.exp(rng.normal(0, 3, (20000, 1)))).astype(np.float32)
+    shift, scale, codes = kp.quantise_group(g)
+    want = ko.quantise_group(g, 4)
+    np.testing.assert_array_equal(shift.view(np.uint16), want[0].view(np.uint16))
+    apart = np.abs(scale.view(np.uint16).astype(int) - want[1].view(np.uint16).astype(int))
+    assert apart.max() <= 1 and apart.mean() < 0.01
+    same = apart == 0
+    np.testing.assert_array_equal(codes[same], want[2][same])
+
+
 def test_a_row_of_four_bits_packed_by_hand():
     """64 features: 0 .. 15 four times over in the first group's order, the second group reversed: shift 0, scale 1, code = value."""
     x = np.concatenate([np.arange(32) % 16, 15 - np.arange(32) % 16]).astype(np.float32)[None]
@@ -56,9 +69,10 @@ def test_rows_that_are_zero_tiny_or_not_finite():
     x[2, 0], x[2, 1], x[2, 2], x[2, 3] = np.inf, -np.inf, np.nan, 7.0
     x[3] = -3.0
     rows, scales = kp.quantise(x, "fp8")
-    got = kp.values(rows, scales, "fp8", 64).astype(np.float32)      # (the scale is itself rounded to float32)
-    assert (got[:2] == 0).all() and (got[3] == -3.0).all()
-    assert got[2, 0] == 7.0 and got[2, 1] == -7.0 and np.isnan(got[2, 2]) and got[2, 3] == 7.0 and (got[2, 4:] == 0).all()
+    got = kp.values(rows, scales, "fp8", 64)
+    near = lambda v, want: np.abs(v - want) <= 2.0 ** -22 * abs(want)          # (1 / 448 and the scale are each rounded to float32)
+    assert (got[:2] == 0).all() and near(got[3], -3.0).all()
+    assert near(got[2, 0], 7.0) and near(got[2, 1], -7.0) and np.isnan(got[2, 2]) and near(got[2, 3], 7.0) and (got[2, 4:] == 0).all()
 
 
 def test_attention_in_closed_form():
