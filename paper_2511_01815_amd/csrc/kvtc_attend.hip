@@ -1,107 +1,759 @@
 // Attention of one new token of every sequence over the pages of a live cache, for gfx950.
 //
-// One pass over keys and values with the running maximum m and sum l of a softmax: for a score s,
-//     m' = max(m, s),  l' = l e^(m - m') + e^(s - m'),  o' = o e^(m - m') + e^(s - m') v.
-// A workgroup has a (sequence, query head), its waves every fourth token each, joined in the LDS at the end; a lane has D / 64
-// features of the token in hand.
+// One pass over keys and values with the running maximum m and sum l of a softmax: for the scores s of some more tokens,
+//     m' = max(m, s),  l' = l e^(m - m') + sum e^(s - m'),  o' = o e^(m - m') + sum e^(s - m') v.
+// Bytes bound it: every key and value is used for the few query heads of its group only.
+//
+// Work.  An item is (sequence, KV head, up to 16 of its query heads); its tokens come in tiles of 128, 32 to a wave.  The tiles of all
+// items, one after another, are cut into as many equal shares as there are workgroups: whatever the lengths, all workgroups have
+// the same amount to read, and a share begins and ends inside an item where it happens to.  Parts of an item are left in the
+// workspace as (m, l, o); the last of its workgroups to arrive joins them, in their order.
+//
+// Products.  Matrix instructions of 16 x 16 x 32, tokens in the rows and query heads in the columns: S^T = K Q^T, O^T = V^T P^T.  Both sum over an
+// index whose order is free, so long as both operands have the same one, and so
+//   keys    a lane has 16 bytes of one token (lane % 16): the operand as it lies in memory; the queries are laid out to match
+//   scores  a lane has those of one query head (lane % 16) and four tokens, 4 (lane / 16) + 0..3, of each of two products: the
+//           8 tokens that its part of the next operand needs -- probabilities never leave their registers
+//   values  a lane has d / 16 neighbouring features of those 8 tokens (a row over 16 lanes), and turns 8 tokens x d / 16 features into d / 16
+//           operands by byte permutations: a matrix product for every d / 16-th feature
+// Nothing goes through the LDS before the four waves' results are joined.
+//
+// 8 bits: E4M3 codes are bf16 values; scores and probabilities take the token's scale.  4 bits: byte pair * G + group of a row
+// (G = d / 32 groups) holds two neighbouring features, so that a lane's bytes are of one pair or four and of every group; a nibble over the bf16
+// pattern of 128 is 128 + code.  Scores: per group a product of its own, starting from -128 times the sum of the group's query,
+// times the token's scale, plus the sum times its shift.  Values: per group the probabilities times the tokens' scales; shifts and the 128s by
+// sums apart.
+// Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Parts are cut towards zero so that they have
+// one sign, and in 16 bits are at least 2^-120, so that an infinite value stays one.
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
+#include "kvtc_dev.h"
 #include "kvtc_numeric.h"
 
 namespace kvtc {
 
-__device__ __forceinline__ float query(const uint16_t* x) { return bf16_f32(*x); }
-__device__ __forceinline__ float query(const float* x) { return *x; }
-__device__ __forceinline__ void put_out(uint16_t* x, float v) { *x = f32_bf16(v); }
-__device__ __forceinline__ void put_out(float* x, float v) { *x = v; }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAttendTile = 128;                           // tokens of a workgroup's step, 32 to each of four waves
+constexpr int kAttendCols = 16;                            // query heads of an item, at most
+constexpr int kAttendMaxGroups = 1024;                     // workgroups of a launch, at most: a counter each in the workspace
+constexpr float kNoScore = -__builtin_huge_valf();
+
+struct AttendPlan {                                        // what the host works out
+    AttendArgs a;
+    int32_t group, parts, cols;                            // query heads of a KV head; items that share them; of each, at most
+    int32_t in_page;                                       // a wave's 32 tokens lie in one page
+    int32_t seqs_each;                                     // sequences whose lengths a thread adds up
+    uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// the high halves of two words (bf16 by cutting), first one low
+__device__ __forceinline__ uint32_t high_halves(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x07060302u); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x05040100u); }
+__device__ __forceinline__ float cut(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t round_pair(float first, float second) {
+    bf16x2 v;
+    v[0] = (__bf16)first;
+    v[1] = (__bf16)second;
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float half_of(uint32_t w, int high) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(high ? w >> 16 : w)); }
+
+// Eight values as a sum of PARTS operands.
+template <int PARTS, bool KEEP_SIGN>
+__device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS]) {
+    float rest[8];
+    uint32_t w[4];
+    auto least = [](float r, float of) { return KEEP_SIGN ? __builtin_copysignf(fmaxf(__builtin_fabsf(r), 0x1p-120f), of) : r; };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = PARTS > 1 ? high_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1])) : round_pair(v[2 * i], v[2 * i + 1]);
+    out[0] = operand(w[0], w[1], w[2], w[3]);
+    if constexpr (PARTS > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] = least(v[i] - cut(v[i]), v[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = PARTS > 2 ? high_halves(__float_as_uint(rest[2 * i]), __float_as_uint(rest[2 * i + 1])) : round_pair(rest[2 * i], rest[2 * i + 1]);
+        out[1] = operand(w[0], w[1], w[2], w[3]);
+    }
+    if constexpr (PARTS > 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = round_pair(least(rest[2 * i] - cut(rest[2 * i]), v[2 * i]), least(rest[2 * i + 1] - cut(rest[2 * i + 1]), v[2 * i + 1]));
+        out[2] = operand(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// ---- the tokens in hand --------------------------------------------------------------------------------------------------------
+
+// N dwords (or half of one) from a row, by an address of the lane's own or by an offset from what the wave has in common.
+template <int BYTES>
+__device__ __forceinline__ void from_pointer(const uint8_t* p, uint32_t* w) {
+    if constexpr (BYTES == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+    else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    else if constexpr (BYTES == 8) { const u32x2 v = *reinterpret_cast<const u32x2*>(p); w[0] = v[0]; w[1] = v[1]; }
+    else {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+        }
+    }
+}
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+template <int BYTES>
+__device__ __forceinline__ void from_buffer(Rsrc r, uint32_t lane_off, uint32_t off, uint32_t* w) {
+    if constexpr (BYTES == 2) w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane_off, off, 0);
+    else if constexpr (BYTES == 4) w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane_off, off, 0);
+    else if constexpr (BYTES == 8) { const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_off, off, 0); w[0] = v[0]; w[1] = v[1]; }
+    else {
+#pragma unroll
+        for (int i = 0; i < BYTES / 16; ++i) {
+            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_off + 16 * i, off, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+        }
+    }
+}
+
+__device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
+    const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+}
+
+// Where a wave's 32 tokens are, and which of them are seen.
+template <bool IN_PAGE>
+struct Where {
+    uint32_t seen;             // a bit each, the same in all lanes; none: nothing is loaded
+    int64_t row, scale;        // IN_PAGE: of the first token (bytes; entries), the same in all lanes; else of token lane % 32
+};
+
+template <int F, int D, bool IN_PAGE>
+__device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, const int32_t* table, int b, int h, int64_t t, int64_t length, int64_t from) {
+    const AttendArgs& a = p.a;
+    auto below = [](int64_t n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+    Where<IN_PAGE> w;
+    w.seen = below(length - t) & (below(a.sinks - t) | ~below(from - t));
+    w.row = w.scale = 0;
+    if constexpr (IN_PAGE) {
+        if (w.seen == 0u) return w;
+        const uint32_t index = (uint32_t)(((uint64_t)(uint32_t)t * p.page_mul) >> p.page_shift), in = (uint32_t)t - index * (uint32_t)a.c.page_tokens;
+        const int32_t page = __builtin_amdgcn_readfirstlane(table[index]);
+        if ((uint32_t)page >= (uint32_t)a.c.n_pages) {
+            if ((threadIdx.x & 63) == 0) report_lowest(a.status, (uint32_t)b);
+            w.seen = 0u;
+            return w;
+        }
+        w.row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
+        w.scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
+    } else {
+        const int mine = (int)(threadIdx.x & 31);
+        bool is = w.seen >> mine & 1u;
+        if (is) {
+            const uint32_t token = (uint32_t)t + mine, index = (uint32_t)(((uint64_t)token * p.page_mul) >> p.page_shift), in = token - index * (uint32_t)a.c.page_tokens;
+            const int32_t page = table[index];
+            is = (uint32_t)page < (uint32_t)a.c.n_pages;
+            if (is) {
+                w.row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
+                w.scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
+            } else {
+                report_lowest(a.status, (uint32_t)b);
+            }
+        }
+        w.seen = (uint32_t)__ballot(is);
+    }
+    return w;
+}
 
 template <int F, int D>
-__device__ __forceinline__ float cache_value(const uint8_t* row, const uint8_t* scales, int64_t scale_at, int f) {
-    if (F == KVTC_CACHE_BF16) return bf16_f32(reinterpret_cast<const uint16_t*>(row)[f]);
-    if (F == KVTC_CACHE_FP8) return __builtin_amdgcn_cvt_f32_fp8((int)row[f], 0) * reinterpret_cast<const float*>(scales)[scale_at];
-    const uint32_t header = reinterpret_cast<const uint32_t*>(scales)[scale_at * (D / kCacheGroup) + f / kCacheGroup];
-    const uint32_t code = row[(f % kCacheGroup) / 2 * (D / kCacheGroup) + f / kCacheGroup] >> (4 * (f & 1)) & 15u;
-    return __builtin_fmaf((float)code, f16_bits_to_f32((uint16_t)(header >> 16)), f16_bits_to_f32((uint16_t)header));
+struct Shape {
+    static constexpr int NK = D / 32;                                          // products over a row of keys; groups of the 4-bit format
+    static constexpr int KW = F == KVTC_CACHE_BF16 ? 4 * NK : F == KVTC_CACHE_FP8 ? 2 * NK : NK;      // dwords of a lane's part of a row of keys
+    static constexpr int VB = F == KVTC_CACHE_BF16 ? 4 * NK : F == KVTC_CACHE_FP8 ? 2 * NK : NK;      // bytes of a lane's part of a row of values
+    static constexpr int VW = (VB + 3) / 4;
+    static constexpr int SW = F == KVTC_CACHE_BF16 ? 0 : F == KVTC_CACHE_FP8 ? 1 : NK;                // dwords of a row's scales
+    static constexpr int NO = D / 16;                                          // products for the features
+};
+
+// A lane's part of the keys of tokens lane % 16 and 16 + lane % 16, and the scales of its 8 tokens' scores.
+template <int F, int D>
+struct Keys {
+    using S = Shape<F, D>;
+    uint32_t w[2][S::KW], scale[8][S::SW > 0 ? S::SW : 1];
+};
+template <int F, int D>
+struct Values {
+    using S = Shape<F, D>;
+    uint32_t w[8][S::VW], scale[8][S::SW > 0 ? S::SW : 1];
+};
+
+// the k-th of the lane's 8 tokens, among the wave's 32
+__device__ __forceinline__ int token_of(int k, int quarter) { return (k < 4 ? k : 12 + k) + 4 * quarter; }
+
+template <int F, int D, bool IN_PAGE>
+__device__ __forceinline__ void load_scales(const void* scales, const Where<IN_PAGE>& at, int quarter, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
+    constexpr int SW = Shape<F, D>::SW;
+    if constexpr (SW > 0) {
+        const uint8_t* base = static_cast<const uint8_t*>(scales);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int64_t entry = IN_PAGE ? at.scale + token_of(k, quarter) : shfl64(at.scale, token_of(k, quarter));
+            from_pointer<4 * SW>(base + entry * (4 * SW), out[k]);
+        }
+    }
+}
+
+// (tokens that are not seen: IN_PAGE, rows of the same page, which exist; else the pool's first row)
+template <int F, int D, bool IN_PAGE>
+__device__ __forceinline__ void load_keys(const kvtc_cache& c, const Where<IN_PAGE>& at, Keys<F, D>& k) {
+    using S = Shape<F, D>;
+    if (at.seen == 0u) return;
+    const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
+    constexpr int kPiece = F == KVTC_CACHE_INT4 ? 4 * S::KW : 16, kPieces = 4 * S::KW / kPiece, kStep = F == KVTC_CACHE_INT4 ? 0 : 64;
+    const uint32_t mine = quarter * kPiece;
+    if constexpr (IN_PAGE) {
+        const uint8_t* base = static_cast<const uint8_t*>(c.k_dev) + at.row;
+        const uint32_t ts = (uint32_t)c.token_stride;
+        const Rsrc r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(31u * ts + (uint32_t)cache_row_bytes(F, D)), 0x00027000);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) from_buffer<kPiece>(r, (uint32_t)row * ts + mine + i * kStep, 16u * n * ts, &k.w[n][i * kPiece / 4]);
+    } else {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const uint8_t* p = static_cast<const uint8_t*>(c.k_dev) + shfl64(at.row, 16 * n + row) + mine;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) from_pointer<kPiece>(p + i * kStep, &k.w[n][i * kPiece / 4]);
+        }
+    }
+    load_scales<F, D, IN_PAGE>(c.k_scales_dev, at, quarter, k.scale);
+}
+
+template <int F, int D, bool IN_PAGE>
+__device__ __forceinline__ void load_values(const kvtc_cache& c, const Where<IN_PAGE>& at, Values<F, D>& v) {
+    using S = Shape<F, D>;
+    if (at.seen == 0u) return;
+    const int lane = threadIdx.x & 63, mine = (lane & 15) * S::VB, quarter = lane >> 4;
+    if constexpr (IN_PAGE) {
+        const uint8_t* base = static_cast<const uint8_t*>(c.v_dev) + at.row;
+        const uint32_t ts = (uint32_t)c.token_stride;
+        const Rsrc r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(31u * ts + (uint32_t)cache_row_bytes(F, D)), 0x00027000);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from_buffer<S::VB>(r, (uint32_t)(4 * quarter) * ts + mine, (uint32_t)token_of(k, 0) * ts, v.w[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) from_pointer<S::VB>(static_cast<const uint8_t*>(c.v_dev) + shfl64(at.row, token_of(k, quarter)) + mine, v.w[k]);
+    }
+    load_scales<F, D, IN_PAGE>(c.v_scales_dev, at, quarter, v.scale);
+    if (at.seen != 0xffffffffu) {                          // what is not seen counts for nothing, whatever it holds
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool is = at.seen >> token_of(k, quarter) & 1u;
+#pragma unroll
+            for (int i = 0; i < S::VW; ++i) v.w[k][i] = is ? v.w[k][i] : 0u;
+#pragma unroll
+            for (int i = 0; i < S::SW; ++i) v.scale[k][i] = is ? v.scale[k][i] : 0u;
+        }
+    }
+}
+
+// ---- queries and scores --------------------------------------------------------------------------------------------------------
+
+template <typename XT> struct Parts;
+template <> struct Parts<uint16_t> { static constexpr int q = 1, p = 2; };
+template <> struct Parts<float> { static constexpr int q = 3, p = 3; };
+
+template <typename XT, int F, int D>
+struct Query {
+    static constexpr int NK = D / 32;
+    bf16x8 w[NK][Parts<XT>::q];
+    float sum[F == KVTC_CACHE_INT4 ? NK : 1];              // 4 bits: of the query over a group
+};
+
+// Of one query head (or none: zeros) the features that go with the lane's part of the keys.
+template <typename XT, int F, int D>
+__device__ __forceinline__ void load_query(const XT* q, bool is, Query<XT, F, D>& out) {
+    constexpr int NK = D / 32;
+    const int quarter = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+        // (8 bits: 16 bytes of keys are two products' worth)
+        const int first = F == KVTC_CACHE_FP8 ? s / 2 * 64 + quarter * 16 + s % 2 * 8 : s * 32 + quarter * 8;
+        float v[8];
+        if (is) {
+            if constexpr (sizeof(XT) == 2) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(q + first);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_f32(w[i] & 0xffffu); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x4 w = reinterpret_cast<const f32x4*>(q + first)[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[4 * i + j] = w[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
+        if constexpr (F == KVTC_CACHE_INT4) {
+            float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            out.sum[s] = sum;
+            const float o[8] = {v[0], v[2], v[1], v[3], v[4], v[6], v[5], v[7]};          // the order in which codes come out of their bytes
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = o[i];
+        }
+        split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v, out.w[s]);
+    }
+}
+
+// bf16 patterns of 128 + code: of the low (even features) and the high four bits of byte `at` of one and of another run of dwords
+__device__ __forceinline__ void nibbles(uint32_t first, uint32_t second, int at_first, int at_second, uint32_t& even, uint32_t& odd) {
+    const uint32_t u = __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
+    even = (u & 0x000f000fu) | 0x43004300u;
+    odd = (u >> 4 & 0x000f000fu) | 0x43004300u;
+}
+// bf16 patterns of the codes themselves
+__device__ __forceinline__ void nibbles_exact(uint32_t first, uint32_t second, int at_first, int at_second, uint32_t& even, uint32_t& odd) {
+    const uint32_t u = __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
+    const float a = (float)(u & 15u), b = (float)(u >> 16 & 15u), c = (float)(u >> 4 & 15u), d = (float)(u >> 20 & 15u);
+    even = high_halves(__float_as_uint(a), __float_as_uint(b));
+    odd = high_halves(__float_as_uint(c), __float_as_uint(d));
+}
+// two E4M3 codes (the low or the high ones of a dword) as bf16
+template <bool HIGH>
+__device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH)); }
+
+// Scores (without the common factor) of the lane's query head and 8 tokens.
+template <typename XT, int F, int D>
+__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D>& k, float (&s)[8]) {
+    constexpr int NK = D / 32, QP = Parts<XT>::q;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (F == KVTC_CACHE_INT4) {
+#pragma unroll
+            for (int g = 0; g < NK; ++g) {
+                uint32_t w[4];
+                auto at = [&](int pair) { return pair * NK + g; };                        // byte of the lane's run
+                nibbles(k.w[n][at(0) / 4], k.w[n][at(1) / 4], at(0) % 4, at(1) % 4, w[0], w[1]);
+                nibbles(k.w[n][at(2) / 4], k.w[n][at(3) / 4], at(2) % 4, at(3) % 4, w[2], w[3]);
+                const float start = -128.0f * q.sum[g];
+                f32x4 c = {start, start, start, start};
+#pragma unroll
+                for (int j = QP - 1; j >= 0; --j) c = mfma(operand(w[0], w[1], w[2], w[3]), q.w[g][j], c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t header = k.scale[4 * n + i][g];
+                    sum[i] = __builtin_fmaf(half_of(header, 1), c[i], __builtin_fmaf(half_of(header, 0), q.sum[g], sum[i]));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < NK; ++t) {
+                bf16x8 a;
+                if constexpr (F == KVTC_CACHE_BF16) a = operand(k.w[n][4 * t], k.w[n][4 * t + 1], k.w[n][4 * t + 2], k.w[n][4 * t + 3]);
+                else a = operand(e4m3_to_bf16<false>(k.w[n][2 * t]), e4m3_to_bf16<true>(k.w[n][2 * t]), e4m3_to_bf16<false>(k.w[n][2 * t + 1]), e4m3_to_bf16<true>(k.w[n][2 * t + 1]));
+#pragma unroll
+                for (int j = QP - 1; j >= 0; --j) sum = mfma(a, q.w[t][j], sum);
+            }
+            if constexpr (F == KVTC_CACHE_FP8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] *= __uint_as_float(k.scale[4 * n + i][0]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * n + i] = sum[i];
+    }
+}
+
+// ---- running sums --------------------------------------------------------------------------------------------------------------
+
+// Of the lane's query head: the maximum (of all lanes of the head), and this lane's parts of the sums.
+template <typename XT, int F, int D>
+struct Running {
+    static constexpr int NO = D / 16, G = D / 32;
+    f32x4 o[NO];
+    float m, l;
+    float low[F == KVTC_CACHE_INT4 ? G : 1];               // 4 bits: of p * shift (and the 128s), per group
+};
+
+// the feature of o[i][r]
+template <int F, int D>
+__device__ __forceinline__ int feature_of(int i, int r, int quarter) {
+    const int c = 4 * quarter + r;
+    return F == KVTC_CACHE_INT4 ? i / 2 * 32 + 2 * c + i % 2 : c * (D / 16) + i;
 }
 
 template <typename XT, int F, int D>
-__global__ void __launch_bounds__(256) attend_kernel(const AttendArgs a) {
-    constexpr int N = D / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int b = (int)(blockIdx.x / (uint32_t)a.n_q_heads), hq = (int)(blockIdx.x - (uint32_t)b * (uint32_t)a.n_q_heads), h = hq / (a.n_q_heads / a.c.n_heads);
-    int64_t length = a.lengths[b];
-    if (length < 0 || length > a.max_tokens) {
-        if (threadIdx.x == 0) report_lowest(a.status, (uint32_t)b);
-        length = 0;
-    }
-    const int64_t from = a.window ? length - a.window : 0;
-    const XT* q = static_cast<const XT*>(a.q) + b * a.q_seq_stride + hq * a.q_head_stride + lane * N;
-    float qv[N], o[N], m = -__builtin_huge_valf(), l = 0.0f;
+__device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<F, D>& v, float (&s)[8], uint32_t seen, float factor) {
+    constexpr int NO = D / 16, G = D / 32, P = Parts<XT>::p;
+    constexpr bool kExact = sizeof(XT) == 4;               // fp32 results: codes without the 128 that bf16 results can bear in their sums
+    const int quarter = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int i = 0; i < N; ++i) { qv[i] = query(q + i) * a.scale; o[i] = 0.0f; }
-    for (int64_t t = wave; t < length; t += 4) {
-        if (t >= a.sinks && t < from) continue;
-        const int64_t index = t / a.c.page_tokens, in = t - index * a.c.page_tokens, page = a.pages[b * a.pages_stride + index];
-        if (page < 0 || page >= a.c.n_pages) {
-            if (lane == 0) report_lowest(a.status, (uint32_t)b);
+    for (int i = 0; i < 8; ++i) s[i] *= factor;
+    if (seen != 0xffffffffu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = seen >> token_of(i, quarter) & 1u ? s[i] : kNoScore;
+    }
+    float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    if (__any(top > run.m)) {
+        const float now = fmaxf(top, run.m), keep = exp2_fast(run.m - (now == kNoScore ? 0.0f : now));
+        run.l *= keep;
+        run.m = now;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) run.o[i] *= keep;
+        if constexpr (F == KVTC_CACHE_INT4) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) run.low[g] *= keep;
+        }
+    }
+    const float base = run.m == kNoScore ? 0.0f : run.m;
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = exp2_fast(s[i] - base);
+    run.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    if constexpr (F == KVTC_CACHE_INT4) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float ps[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t header = v.scale[i][g];
+                ps[i] = p[i] * half_of(header, 1);
+                run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
+            }
+            if constexpr (!kExact) run.low[g] = __builtin_fmaf(-128.0f, ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7])), run.low[g]);
+            bf16x8 b[P];
+            split<P, false>(ps, b);
+            uint32_t even[4], odd[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (kExact) nibbles_exact(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, even[i], odd[i]);
+                else nibbles(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, even[i], odd[i]);
+            }
+#pragma unroll
+            for (int j = P - 1; j >= 0; --j) {
+                run.o[2 * g] = mfma(operand(even[0], even[1], even[2], even[3]), b[j], run.o[2 * g]);
+                run.o[2 * g + 1] = mfma(operand(odd[0], odd[1], odd[2], odd[3]), b[j], run.o[2 * g + 1]);
+            }
+        }
+    } else {
+        if constexpr (F == KVTC_CACHE_FP8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] *= __uint_as_float(v.scale[i][0]);
+        }
+        bf16x8 b[P];
+        split<P, F == KVTC_CACHE_BF16>(p, b);
+        if constexpr (F == KVTC_CACHE_BF16) {
+#pragma unroll
+            for (int i = 0; i < NO; ++i) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = i % 2 ? high_halves(v.w[2 * j][i / 2], v.w[2 * j + 1][i / 2]) : low_halves(v.w[2 * j][i / 2], v.w[2 * j + 1][i / 2]);
+#pragma unroll
+                for (int j = P - 1; j >= 0; --j) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[j], run.o[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NO; i += 2) {
+                uint32_t w[4], x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {                                 // features i and i + 1 of two tokens: [i, i, i + 1, i + 1]
+                    const uint32_t at = (uint32_t)(i % 4), u = __builtin_amdgcn_perm(v.w[2 * j + 1][i / 4], v.w[2 * j][i / 4], at | (at + 4) << 8 | (at + 1) << 16 | (at + 5) << 24);
+                    w[j] = e4m3_to_bf16<false>(u);
+                    x[j] = e4m3_to_bf16<true>(u);
+                }
+#pragma unroll
+                for (int j = P - 1; j >= 0; --j) {
+                    run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[j], run.o[i]);
+                    run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[j], run.o[i + 1]);
+                }
+            }
+        }
+    }
+}
+
+// ---- the shares ----------------------------------------------------------------------------------------------------------------
+
+// Tiles of a sequence that hold a seen token: those of the sinks, then those of the window.  (At least one: every row has a result.)
+struct Tiles { uint32_t n, sinks, window0; int64_t length, from; };
+__device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int64_t length) {
+    if (length < 0 || length > a.max_tokens) length = 0;
+    Tiles t;
+    t.length = length;
+    t.from = a.window ? max((int64_t)0, length - a.window) : 0;
+    const uint32_t all = (uint32_t)((length + kAttendTile - 1) / kAttendTile);
+    t.sinks = a.window ? min((uint32_t)((min(a.sinks, length) + kAttendTile - 1) / kAttendTile), all) : 0u;
+    t.window0 = max(t.sinks, (uint32_t)(t.from / kAttendTile));
+    t.n = max(1u, t.sinks + (all > t.window0 ? all - t.window0 : 0u));
+    return t;
+}
+
+template <typename XT> __device__ __forceinline__ void put_out(XT* x, float v);
+template <> __device__ __forceinline__ void put_out<uint16_t>(uint16_t* x, float v) { *x = f32_bf16(v); }
+template <> __device__ __forceinline__ void put_out<float>(float* x, float v) { *x = v; }
+
+// floats of a part of an item in the workspace
+__host__ __device__ constexpr int part_floats(int cols, int d) { return (cols * (d + 2) + 3) / 4 * 4; }
+
+template <typename XT, int F, int D, bool IN_PAGE>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
+    const AttendArgs& a = p.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
+    __shared__ float s_o[4][kAttendCols][D + 4];
+    __shared__ float s_m[4][kAttendCols], s_l[4][kAttendCols];
+    __shared__ uint64_t s_scan[4], s_start;
+    __shared__ int s_seq;
+    __shared__ uint32_t s_last;
+
+    // where the workgroup's share begins: a prefix sum over the sequences' tiles
+    const uint64_t heads = (uint64_t)a.c.n_heads * (uint32_t)p.parts, me = blockIdx.x;
+    uint64_t mine = 0;
+    const int first = tid * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
+    for (int b = first; b < last; ++b) {
+        const int64_t length = a.lengths[b];
+        if (me == 0 && (length < 0 || length > a.max_tokens)) report_lowest(a.status, (uint32_t)b);
+        mine += tiles_of(a, length).n;
+    }
+    uint64_t before = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t v = __shfl_up(before, d, 64);
+        if (lane >= d) before += v;
+    }
+    if (lane == 63) s_scan[wave] = before;
+    __syncthreads();
+    uint64_t all = 0;
+    before -= mine;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += s_scan[w];
+        all += s_scan[w];
+    }
+    all *= heads;
+    const uint64_t groups = min((uint64_t)gridDim.x, all); // (no share is empty: each of an item's workgroups is waited for)
+    if (me >= groups) return;
+    const uint64_t share0 = me * all / groups, share1 = (me + 1) * all / groups;
+    if (before * heads <= share0 && share0 < (before + mine) * heads) {
+        int b = first;
+        for (; b + 1 < last; ++b) {
+            const uint64_t n = tiles_of(a, a.lengths[b]).n;
+            if (share0 < (before + n) * heads) break;
+            before += n;
+        }
+        s_seq = b;
+        s_start = before * heads;
+    }
+    __syncthreads();
+    int b = s_seq;
+    uint64_t seq0 = s_start;                               // the sequence's first tile, counted over all items
+    auto owner = [&](uint64_t tile) { return (uint32_t)(((tile + 1) * groups - 1) / all); };
+    const float factor = a.scale * 1.44269504088896340736f;
+
+    uint64_t at = share0;
+    while (at < share1) {
+        const Tiles t = tiles_of(a, a.lengths[b]);
+        if (at >= seq0 + t.n * heads) {
+            seq0 += t.n * heads;
+            ++b;
             continue;
         }
-        const int64_t at = page * a.c.page_stride + h * a.c.head_stride + in * a.c.token_stride, scale_at = (page * a.c.n_heads + h) * a.c.page_tokens + in;
-        float s = 0.0f;
+        const uint32_t item = (uint32_t)((at - seq0) / t.n), tile0 = (uint32_t)((at - seq0) - (uint64_t)item * t.n);
+        const uint32_t tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at));
+        const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
+        const int col0 = h * p.group + part * p.cols, cols = min(p.cols, p.group - part * p.cols);
+
+        Query<XT, F, D> q;
+        load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (col < cols ? col : 0)) * a.q_head_stride, col < cols, q);
+        const int32_t* table = a.pages + (int64_t)b * a.pages_stride;
+        auto look = [&](uint32_t i) {
+            const uint32_t tile = i < t.sinks ? i : t.window0 + (i - t.sinks);
+            return where<F, D, IN_PAGE>(p, table, b, h, (int64_t)tile * kAttendTile + wave * 32, t.length, t.from);
+        };
+        Running<XT, F, D> run;
 #pragma unroll
-        for (int i = 0; i < N; ++i) s += qv[i] * cache_value<F, D>(static_cast<const uint8_t*>(a.c.k_dev) + at, static_cast<const uint8_t*>(a.c.k_scales_dev), scale_at, lane * N + i);
+        for (int i = 0; i < D / 16; ++i) run.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        run.m = kNoScore;
+        run.l = 0.0f;
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, 64);
-        const float top = fmaxf(m, s), base = top == -__builtin_huge_valf() ? 0.0f : top, keep = expf(m - base), p = expf(s - base);
-        l = l * keep + p;
+        for (int g = 0; g < (F == KVTC_CACHE_INT4 ? D / 32 : 1); ++g) run.low[g] = 0.0f;
+
+        Keys<F, D> keys;
+        Values<F, D> values;
+        Where<IN_PAGE> now = look(tile0);
+        load_keys<F, D, IN_PAGE>(a.c, now, keys);
+        load_values<F, D, IN_PAGE>(a.c, now, values);
+        for (uint32_t i = tile0; i < tile1; ++i) {
+            Where<IN_PAGE> next = now;
+            next.seen = 0u;
+            if (i + 1 < tile1) next = look(i + 1);
+            float s[8];
+            if (now.seen != 0u) scores<XT, F, D>(q, keys, s);
+            load_keys<F, D, IN_PAGE>(a.c, next, keys);
+            if (now.seen != 0u) add_tokens<XT, F, D>(run, values, s, now.seen, factor);
+            load_values<F, D, IN_PAGE>(a.c, next, values);
+            now = next;
+        }
+
+        // the four waves' results, joined
+        run.l += __shfl_xor(run.l, 16, 64);
+        run.l += __shfl_xor(run.l, 32, 64);
+        if constexpr (F == KVTC_CACHE_INT4) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            o[i] = o[i] * keep + p * cache_value<F, D>(static_cast<const uint8_t*>(a.c.v_dev) + at, static_cast<const uint8_t*>(a.c.v_scales_dev), scale_at, lane * N + i);
-        m = top;
+            for (int g = 0; g < D / 32; ++g) {
+                run.low[g] += __shfl_xor(run.low[g], 16, 64);
+                run.low[g] += __shfl_xor(run.low[g], 32, 64);
+            }
+        }
+        if (col < cols) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
+            if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
+        }
+        __syncthreads();
+        const uint64_t item0 = seq0 + (uint64_t)item * t.n;
+        const uint32_t g0 = owner(item0), g1 = owner(item0 + t.n - 1);
+        const bool whole = g0 == g1;
+        const int64_t row0 = (int64_t)b * a.n_q_heads + col0;
+        uint32_t* counters = static_cast<uint32_t*>(a.work);
+        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxGroups * 4);
+        const int slot_floats = part_floats(p.cols, D);
+        float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
+        for (int j = tid; j < cols * D; j += 256) {
+            const int c = j / D, f = j % D;
+            float top = s_m[0][c];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][c]);
+            const float base = top == kNoScore ? 0.0f : top;
+            float l = 0.0f, o = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float keep = exp2_fast(s_m[w][c] - base);
+                l = __builtin_fmaf(s_l[w][c], keep, l);
+                o = __builtin_fmaf(s_o[w][c][f], keep, o);
+            }
+            if (whole) {
+                put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f, l == 0.0f ? 0.0f : o / l);
+                if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            } else {
+                slot[c * D + f] = o;
+                if (f == 0) { slot[p.cols * D + c] = top; slot[p.cols * D + p.cols + c] = l; }
+            }
+        }
+        if (!whole) {
+            // the last of the item's workgroups to come here joins them
+            __syncthreads();
+            if (tid == 0) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+                const uint32_t came = __hip_atomic_fetch_add(&counters[g0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+                s_last = came == g1 - g0;
+                if (came == g1 - g0) __hip_atomic_store(&counters[g0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (s_last) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+                auto part_at = [&](uint32_t g) { return slots + (int64_t)(2 * g + (g == g0 ? 1 : 0)) * slot_floats; };
+                for (int j = tid; j < cols * D; j += 256) {
+                    const int c = j / D, f = j % D;
+                    float top = kNoScore;
+                    for (uint32_t g = g0; g <= g1; ++g) top = fmaxf(top, part_at(g)[p.cols * D + c]);
+                    const float base = top == kNoScore ? 0.0f : top;
+                    float l = 0.0f, o = 0.0f;
+                    for (uint32_t g = g0; g <= g1; ++g) {
+                        const float* s = part_at(g);
+                        const float keep = exp2_fast(s[p.cols * D + c] - base);
+                        l = __builtin_fmaf(s[p.cols * D + p.cols + c], keep, l);
+                        o = __builtin_fmaf(s[c * D + f], keep, o);
+                    }
+                    put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f, l == 0.0f ? 0.0f : o / l);
+                    if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                }
+            }
+        }
+        __syncthreads();
+        at += tile1 - tile0;
     }
-    __shared__ float part[4][D + 2];
-#pragma unroll
-    for (int i = 0; i < N; ++i) part[wave][lane * N + i] = o[i];
-    if (lane == 0) { part[wave][D] = m; part[wave][D + 1] = l; }
-    __syncthreads();
-    if (wave != 0) return;
-    float top = part[0][D];
-    for (int w = 1; w < 4; ++w) top = fmaxf(top, part[w][D]);
-    const float base = top == -__builtin_huge_valf() ? 0.0f : top;
-    float total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = 0.0f;
-    for (int w = 0; w < 4; ++w) {
-        const float keep = expf(part[w][D] - base);
-        total += part[w][D + 1] * keep;
-#pragma unroll
-        for (int i = 0; i < N; ++i) o[i] += part[w][lane * N + i] * keep;
-    }
-    const int64_t row = (int64_t)b * a.n_q_heads + hq;
-    XT* out = static_cast<XT*>(a.out) + row * D + lane * N;
-#pragma unroll
-    for (int i = 0; i < N; ++i) put_out(out + i, total == 0.0f ? 0.0f : o[i] / total);
-    if (a.lse && lane == 0) a.lse[row] = base + logf(total);
 }
 
-size_t attend_work_bytes(const kvtc_cache&, int, int, int64_t) { return 256; }
+// ---- launches ------------------------------------------------------------------------------------------------------------------
 
+// Items that share a KV head's query heads, and how many of these each has.
+static void shares_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) {
+    const int group = n_q_heads / c.n_heads;
+    parts = (group + kAttendCols - 1) / kAttendCols;
+    cols = (group + parts - 1) / parts;
+}
+
+// Workgroups: two to a compute unit (one of wide heads), no more than there can be tiles.
+static int groups_of(const kvtc_cache& c, int n_seqs, int parts, int64_t max_tokens, int64_t sinks, int64_t window) {
+    int64_t tiles = (max_tokens + kAttendTile - 1) / kAttendTile;
+    if (window) {
+        const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / kAttendTile + (window < max_tokens ? window : max_tokens) / kAttendTile + 3;
+        tiles = some < tiles ? some : tiles;
+    }
+    const int64_t most = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), cap = most < kAttendMaxGroups ? most : kAttendMaxGroups;
+    const __int128 all = (__int128)tiles * n_seqs * c.n_heads * parts;
+    return (int)(all < cap ? (int64_t)all : cap);
+}
+
+size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {
+    int parts, cols;
+    shares_of(c, n_q_heads, parts, cols);
+    return (size_t)kAttendMaxGroups * 4 + (size_t)groups_of(c, n_seqs < 1 ? 1 : n_seqs, parts, max_tokens, 0, 0) * 2 * part_floats(cols, c.d_head) * sizeof(float);
+}
+
+template <typename XT, int F, int D>
+static void launch_pages(const AttendPlan& p, int groups, hipStream_t stream) {
+    if (p.in_page) hipLaunchKernelGGL((attend_kernel<XT, F, D, true>), dim3(groups), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attend_kernel<XT, F, D, false>), dim3(groups), dim3(256), 0, stream, p);
+}
 template <typename XT, int F>
-hipError_t launch_d(const AttendArgs& a, hipStream_t stream) {
-    const dim3 grid((uint32_t)a.n_seqs * (uint32_t)a.n_q_heads), block(256);
-    if (a.c.d_head == 64) hipLaunchKernelGGL((attend_kernel<XT, F, 64>), grid, block, 0, stream, a);
-    else if (a.c.d_head == 128) hipLaunchKernelGGL((attend_kernel<XT, F, 128>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attend_kernel<XT, F, 256>), grid, block, 0, stream, a);
-    return hipGetLastError();
+static void launch_width(const AttendPlan& p, int groups, hipStream_t stream) {
+    if (p.a.c.d_head == 64) launch_pages<XT, F, 64>(p, groups, stream);
+    else if (p.a.c.d_head == 128) launch_pages<XT, F, 128>(p, groups, stream);
+    else launch_pages<XT, F, 256>(p, groups, stream);
 }
 template <typename XT>
-hipError_t launch_format(const AttendArgs& a, hipStream_t stream) {
-    if (a.c.format == KVTC_CACHE_BF16) return launch_d<XT, KVTC_CACHE_BF16>(a, stream);
-    if (a.c.format == KVTC_CACHE_FP8) return launch_d<XT, KVTC_CACHE_FP8>(a, stream);
-    return launch_d<XT, KVTC_CACHE_INT4>(a, stream);
+static void launch_format(const AttendPlan& p, int groups, hipStream_t stream) {
+    if (p.a.c.format == KVTC_CACHE_BF16) launch_width<XT, KVTC_CACHE_BF16>(p, groups, stream);
+    else if (p.a.c.format == KVTC_CACHE_FP8) launch_width<XT, KVTC_CACHE_FP8>(p, groups, stream);
+    else launch_width<XT, KVTC_CACHE_INT4>(p, groups, stream);
 }
+
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream) {
-    return dtype == KVTC_BF16 ? launch_format<uint16_t>(a, stream) : launch_format<float>(a, stream);
+    AttendPlan p;
+    p.a = a;
+    int parts, cols;
+    shares_of(a.c, a.n_q_heads, parts, cols);
+    p.group = a.n_q_heads / a.c.n_heads;
+    p.parts = parts;
+    p.cols = cols;
+    p.in_page = a.c.page_tokens % 32 == 0;
+    p.seqs_each = (a.n_seqs + 255) / 256;
+    uint32_t s = 0;                                        // (n < 2^31: m = ceil(2^(31 + s) / d) is near enough)
+    while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
+    p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);
+    p.page_shift = 31 + s;
+    const int groups = groups_of(a.c, a.n_seqs, parts, a.max_tokens, a.sinks, a.window);
+    if (dtype == KVTC_BF16) launch_format<uint16_t>(p, groups, stream);
+    else launch_format<float>(p, groups, stream);
+    return hipGetLastError();
 }
 
 }  // namespace kvtc
