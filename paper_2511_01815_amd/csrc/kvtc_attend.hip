@@ -509,6 +509,66 @@ template <> __device__ __forceinline__ void put_out<float>(float* x, float v) { 
 // floats of a part of an item in the workspace
 __host__ __device__ constexpr int part_floats(int cols, int d) { return (cols * (d + 2) + 3) / 4 * 4; }
 
+// The parts g0 .. g1 of an item, joined by a workgroup in their order.  Four outputs to a thread; where a row has less than 256 such, several threads share
+// the parts of one.  The loads of many parts are on their way together: the last workgroup of an item of a long context joins 64 parts of 2 KB.
+// lds: 4 x 16 x (D + 4) floats; stats: 64.
+constexpr int kJoinStep = 128;                             // parts whose weights are in the LDS at a time
+template <typename XT, int D>
+__device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* lds, float* stats) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float* weight = lds;                                   // [col][kJoinStep]
+    float* sum = lds + kAttendCols * kJoinStep;            // [256][4]
+    static_assert(4 * kAttendCols * (D + 4) >= kAttendCols * kJoinStep + 1024, "");
+    auto part_at = [&](uint32_t g) { return slots + (int64_t)(2 * g + (g == g0 ? 1 : 0)) * slot_floats; };
+    for (int c = wave; c < cols; c += 4) {                 // maximum and sum of each row
+        float top = kNoScore, l = 0.0f;
+        for (uint32_t g = g0 + lane; g <= g1; g += 64) top = fmaxf(top, part_at(g)[cols_all * D + c]);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+        const float base = top == kNoScore ? 0.0f : top;
+        for (uint32_t g = g0 + lane; g <= g1; g += 64) l = __builtin_fmaf(part_at(g)[cols_all * D + cols_all + c], exp2_fast(part_at(g)[cols_all * D + c] - base), l);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
+        if (lane == 0) { stats[c] = base; stats[16 + c] = l; }
+    }
+    __syncthreads();
+    const int quads = cols * D / 4, teams = quads < 256 ? 256 / quads : 1;
+    for (int j0 = 0; j0 < quads; j0 += 256) {
+        const int team = quads < 256 ? tid / quads : 0, j = quads < 256 ? tid - team * quads : j0 + tid, c = min(4 * j / D, cols - 1);
+        const bool is = team < teams && j < quads;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t from = g0; from <= g1; from += kJoinStep) {
+            const int n = (int)min((uint32_t)kJoinStep, g1 + 1 - from);
+            __syncthreads();
+            for (int k = tid; k < cols * kJoinStep; k += 256) {
+                const int cc = k / kJoinStep, g = k % kJoinStep;
+                if (g < n) weight[k] = exp2_fast(part_at(from + g)[cols_all * D + cc] - stats[cc]);
+            }
+            __syncthreads();
+            if (is) {
+#pragma unroll 8
+                for (int g = team; g < n; g += teams) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(part_at(from + g) + 4 * j);
+                    o += v * weight[c * kJoinStep + g];
+                }
+            }
+        }
+        if (teams > 1) {
+            *reinterpret_cast<f32x4*>(sum + 4 * tid) = o;
+            __syncthreads();
+            for (int k = 1; k < teams; ++k)
+                if (is && team == 0) o += *reinterpret_cast<const f32x4*>(sum + 4 * (k * quads + j));
+        }
+        if (is && team == 0) {
+            const int f = 4 * j - c * D;
+            const float l = stats[16 + c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f + i, l == 0.0f ? 0.0f : o[i] / l);
+            if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+        }
+    }
+}
+
 template <typename XT, int F, int D, bool IN_PAGE>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
     const AttendArgs& a = p.a;
@@ -668,22 +728,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
             __syncthreads();
             if (s_last) {
                 __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-                auto part_at = [&](uint32_t g) { return slots + (int64_t)(2 * g + (g == g0 ? 1 : 0)) * slot_floats; };
-                for (int j = tid; j < cols * D; j += 256) {
-                    const int c = j / D, f = j % D;
-                    float top = kNoScore;
-                    for (uint32_t g = g0; g <= g1; ++g) top = fmaxf(top, part_at(g)[p.cols * D + c]);
-                    const float base = top == kNoScore ? 0.0f : top;
-                    float l = 0.0f, o = 0.0f;
-                    for (uint32_t g = g0; g <= g1; ++g) {
-                        const float* s = part_at(g);
-                        const float keep = exp2_fast(s[p.cols * D + c] - base);
-                        l = __builtin_fmaf(s[p.cols * D + p.cols + c], keep, l);
-                        o = __builtin_fmaf(s[c * D + f], keep, o);
-                    }
-                    put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f, l == 0.0f ? 0.0f : o / l);
-                    if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
-                }
+                join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_m[0][0]);
             }
         }
         __syncthreads();
