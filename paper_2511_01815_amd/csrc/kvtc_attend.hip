@@ -46,7 +46,7 @@ constexpr float kNoScore = -__builtin_huge_valf();
 struct AttendPlan {                                        // what the host works out
     AttendArgs a;
     int32_t group, parts, cols;                            // query heads of a KV head; items that share them; of each, at most
-    int32_t in_page;                                       // a wave's 32 tokens lie in one page
+    int32_t in_page;                                       // 16 tokens from a multiple of 16 on lie in one page
     int32_t seqs_each;                                     // sequences whose lengths a thread adds up
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
 };
@@ -122,6 +122,9 @@ __device__ __forceinline__ void from_buffer(Rsrc r, uint32_t lane_off, uint32_t 
     }
 }
 
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+}
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
@@ -131,41 +134,71 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
 template <bool IN_PAGE>
 struct Where {
     uint32_t seen;             // a bit each, the same in all lanes; none: nothing is loaded
-    int64_t row, scale;        // IN_PAGE: of the first token (bytes; entries), the same in all lanes; else of token lane % 32
+    int64_t row[IN_PAGE ? 2 : 1], scale[IN_PAGE ? 2 : 1];      // IN_PAGE: of the first token of each half (bytes; entries), the same in all lanes; else of token lane % 32
 };
 
-template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, const int32_t* table, int b, int h, int64_t t, int64_t length, int64_t from) {
-    const AttendArgs& a = p.a;
+// The same before the pages are known: their numbers are on their way, and are not waited for until the places are worked out, a step later.  (The vector
+// unit's loads come back in order: a look that is waited for at once waits for the keys and values before it.)  IN_PAGE: 16 tokens lie in one
+// page, and the numbers come through the scalar cache.
+template <bool IN_PAGE>
+struct Look {
+    uint32_t seen, token;
+    int32_t page[IN_PAGE ? 2 : 1];
+};
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+__device__ __forceinline__ int32_t scalar_at(const int32_t* p, int64_t i) { return reinterpret_cast<ScalarInts>(reinterpret_cast<uintptr_t>(p))[i]; }
+
+__device__ __forceinline__ uint32_t page_index(const AttendPlan& p, uint32_t token) { return (uint32_t)(((uint64_t)token * p.page_mul) >> p.page_shift); }
+
+template <bool IN_PAGE>
+__device__ __forceinline__ Look<IN_PAGE> look_at(const AttendPlan& p, const int32_t* table, int64_t t, int64_t length, int64_t from) {
     auto below = [](int64_t n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
-    Where<IN_PAGE> w;
-    w.seen = below(length - t) & (below(a.sinks - t) | ~below(from - t));
-    w.row = w.scale = 0;
+    Look<IN_PAGE> w;
+    w.seen = below(length - t) & (below(p.a.sinks - t) | ~below(from - t));
     if constexpr (IN_PAGE) {
-        if (w.seen == 0u) return w;
-        const uint32_t index = (uint32_t)(((uint64_t)(uint32_t)t * p.page_mul) >> p.page_shift), in = (uint32_t)t - index * (uint32_t)a.c.page_tokens;
-        const int32_t page = __builtin_amdgcn_readfirstlane(table[index]);
-        if ((uint32_t)page >= (uint32_t)a.c.n_pages) {
-            if ((threadIdx.x & 63) == 0) report_lowest(a.status, (uint32_t)b);
-            w.seen = 0u;
-            return w;
+        w.token = (uint32_t)t;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            w.page[n] = 0;
+            if (w.seen >> (16 * n) & 0xffffu) w.page[n] = scalar_at(table, page_index(p, w.token + 16 * n));
         }
-        w.row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
-        w.scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
     } else {
         const int mine = (int)(threadIdx.x & 31);
-        bool is = w.seen >> mine & 1u;
-        if (is) {
-            const uint32_t token = (uint32_t)t + mine, index = (uint32_t)(((uint64_t)token * p.page_mul) >> p.page_shift), in = token - index * (uint32_t)a.c.page_tokens;
-            const int32_t page = table[index];
-            is = (uint32_t)page < (uint32_t)a.c.n_pages;
-            if (is) {
-                w.row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
-                w.scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
+        w.token = (uint32_t)t + mine;
+        w.page[0] = 0;
+        if (w.seen >> mine & 1u) w.page[0] = table[page_index(p, w.token)];
+    }
+    return w;
+}
+
+template <bool IN_PAGE>
+__device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, int b, int h, const Look<IN_PAGE>& l) {
+    const AttendArgs& a = p.a;
+    Where<IN_PAGE> w;
+    w.seen = l.seen;
+    auto place = [&](uint32_t token, int32_t page, int64_t& row, int64_t& scale) {
+        const uint32_t in = token - page_index(p, token) * (uint32_t)a.c.page_tokens;
+        row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
+        scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
+    };
+    if constexpr (IN_PAGE) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const uint32_t mine = 0xffffu << (16 * n);
+            w.row[n] = w.scale[n] = 0;
+            if ((l.seen & mine) == 0u) continue;
+            if ((uint32_t)l.page[n] < (uint32_t)a.c.n_pages) {
+                place(l.token + 16 * n, l.page[n], w.row[n], w.scale[n]);
             } else {
-                report_lowest(a.status, (uint32_t)b);
+                if ((threadIdx.x & 63) == 0) report_lowest(a.status, (uint32_t)b);
+                w.seen &= ~mine;
             }
         }
+    } else {
+        w.row[0] = w.scale[0] = 0;
+        const bool mine = l.seen >> (threadIdx.x & 31) & 1u, is = mine && (uint32_t)l.page[0] < (uint32_t)a.c.n_pages;
+        if (is) place(l.token, l.page[0], w.row[0], w.scale[0]);
+        else if (mine) report_lowest(a.status, (uint32_t)b);
         w.seen = (uint32_t)__ballot(is);
     }
     return w;
@@ -196,20 +229,34 @@ struct Values {
 // the k-th of the lane's 8 tokens, among the wave's 32
 __device__ __forceinline__ int token_of(int k, int quarter) { return (k < 4 ? k : 12 + k) + 4 * quarter; }
 
+// What a half's 16 tokens have in common: `bytes` from the first one's on; a half without a seen token has none, and its loads give zeros.
+template <bool IN_PAGE>
+__device__ __forceinline__ Rsrc half_at(const void* pool, int64_t offset, uint32_t bytes, uint32_t seen, int n) {
+    return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(const_cast<void*>(pool)) + offset, 0, (seen >> (16 * n) & 0xffffu) != 0u ? (int)bytes : 0, 0x00027000);
+}
+
 template <int F, int D, bool IN_PAGE>
 __device__ __forceinline__ void load_scales(const void* scales, const Where<IN_PAGE>& at, int quarter, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
     constexpr int SW = Shape<F, D>::SW;
     if constexpr (SW > 0) {
-        const uint8_t* base = static_cast<const uint8_t*>(scales);
+        if constexpr (IN_PAGE) {                           // the four tokens' scales lie side by side
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t entry = IN_PAGE ? at.scale + token_of(k, quarter) : shfl64(at.scale, token_of(k, quarter));
-            from_pointer<4 * SW>(base + entry * (4 * SW), out[k]);
+            for (int n = 0; n < 2; ++n) {
+                const Rsrc r = half_at<IN_PAGE>(scales, at.scale[n] * (4 * SW), 16 * 4 * SW, at.seen, n);
+                uint32_t w[4 * SW];
+                from_buffer<16 * SW>(r, (uint32_t)(quarter * 16 * SW), 0, w);
+#pragma unroll
+                for (int i = 0; i < 4 * SW; ++i) out[4 * n + i / SW][i % SW] = w[i];
+            }
+        } else {
+            const uint8_t* base = static_cast<const uint8_t*>(scales);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) from_pointer<4 * SW>(base + shfl64(at.scale[0], token_of(k, quarter)) * (4 * SW), out[k]);
         }
     }
 }
 
-// (tokens that are not seen: IN_PAGE, rows of the same page, which exist; else the pool's first row)
+// (single tokens that are not seen: IN_PAGE, rows of the same page, which exist; else the pool's first row)
 template <int F, int D, bool IN_PAGE>
 __device__ __forceinline__ void load_keys(const kvtc_cache& c, const Where<IN_PAGE>& at, Keys<F, D>& k) {
     using S = Shape<F, D>;
@@ -217,18 +264,15 @@ __device__ __forceinline__ void load_keys(const kvtc_cache& c, const Where<IN_PA
     const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
     constexpr int kPiece = F == KVTC_CACHE_INT4 ? 4 * S::KW : 16, kPieces = 4 * S::KW / kPiece, kStep = F == KVTC_CACHE_INT4 ? 0 : 64;
     const uint32_t mine = quarter * kPiece;
-    if constexpr (IN_PAGE) {
-        const uint8_t* base = static_cast<const uint8_t*>(c.k_dev) + at.row;
-        const uint32_t ts = (uint32_t)c.token_stride;
-        const Rsrc r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(31u * ts + (uint32_t)cache_row_bytes(F, D)), 0x00027000);
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n) {
+        if constexpr (IN_PAGE) {
+            const uint32_t ts = (uint32_t)c.token_stride;
+            const Rsrc r = half_at<IN_PAGE>(c.k_dev, at.row[n], 15u * ts + (uint32_t)cache_row_bytes(F, D), at.seen, n);
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) from_buffer<kPiece>(r, (uint32_t)row * ts + mine + i * kStep, 16u * n * ts, &k.w[n][i * kPiece / 4]);
-    } else {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const uint8_t* p = static_cast<const uint8_t*>(c.k_dev) + shfl64(at.row, 16 * n + row) + mine;
+            for (int i = 0; i < kPieces; ++i) from_buffer<kPiece>(r, (uint32_t)row * ts + mine + i * kStep, 0, &k.w[n][i * kPiece / 4]);
+        } else {
+            const uint8_t* p = static_cast<const uint8_t*>(c.k_dev) + shfl64(at.row[0], 16 * n + row) + mine;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) from_pointer<kPiece>(p + i * kStep, &k.w[n][i * kPiece / 4]);
         }
@@ -242,14 +286,16 @@ __device__ __forceinline__ void load_values(const kvtc_cache& c, const Where<IN_
     if (at.seen == 0u) return;
     const int lane = threadIdx.x & 63, mine = (lane & 15) * S::VB, quarter = lane >> 4;
     if constexpr (IN_PAGE) {
-        const uint8_t* base = static_cast<const uint8_t*>(c.v_dev) + at.row;
         const uint32_t ts = (uint32_t)c.token_stride;
-        const Rsrc r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(31u * ts + (uint32_t)cache_row_bytes(F, D)), 0x00027000);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) from_buffer<S::VB>(r, (uint32_t)(4 * quarter) * ts + mine, (uint32_t)token_of(k, 0) * ts, v.w[k]);
+        for (int n = 0; n < 2; ++n) {
+            const Rsrc r = half_at<IN_PAGE>(c.v_dev, at.row[n], 15u * ts + (uint32_t)cache_row_bytes(F, D), at.seen, n);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) from_buffer<S::VB>(r, (uint32_t)(4 * quarter) * ts + mine, (uint32_t)k * ts, v.w[4 * n + k]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) from_pointer<S::VB>(static_cast<const uint8_t*>(c.v_dev) + shfl64(at.row, token_of(k, quarter)) + mine, v.w[k]);
+        for (int k = 0; k < 8; ++k) from_pointer<S::VB>(static_cast<const uint8_t*>(c.v_dev) + shfl64(at.row[0], token_of(k, quarter)) + mine, v.w[k]);
     }
     load_scales<F, D, IN_PAGE>(c.v_scales_dev, at, quarter, v.scale);
     if (at.seen != 0xffffffffu) {                          // what is not seen counts for nothing, whatever it holds
@@ -572,7 +618,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slo
 template <typename XT, int F, int D, bool IN_PAGE>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
     const AttendArgs& a = p.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
     __shared__ float s_o[4][kAttendCols][D + 4];
     __shared__ float s_m[4][kAttendCols], s_l[4][kAttendCols];
     __shared__ uint64_t s_scan[4], s_start;
@@ -606,6 +652,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     all *= heads;
     const uint64_t groups = min((uint64_t)gridDim.x, all); // (no share is empty: each of an item's workgroups is waited for)
     if (me >= groups) return;
+    all = uniform64(all);
     const uint64_t share0 = me * all / groups, share1 = (me + 1) * all / groups;
     if (before * heads <= share0 && share0 < (before + mine) * heads) {
         int b = first;
@@ -618,14 +665,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         s_start = before * heads;
     }
     __syncthreads();
-    int b = s_seq;
-    uint64_t seq0 = s_start;                               // the sequence's first tile, counted over all items
+    int b = __builtin_amdgcn_readfirstlane(s_seq);
+    uint64_t seq0 = uniform64(s_start);                               // the sequence's first tile, counted over all items
     auto owner = [&](uint64_t tile) { return (uint32_t)(((tile + 1) * groups - 1) / all); };
     const float factor = a.scale * 1.44269504088896340736f;
 
     uint64_t at = share0;
     while (at < share1) {
-        const Tiles t = tiles_of(a, a.lengths[b]);
+        const Tiles t = tiles_of(a, scalar_at(a.lengths, b));
         if (at >= seq0 + t.n * heads) {
             seq0 += t.n * heads;
             ++b;
@@ -641,7 +688,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         const int32_t* table = a.pages + (int64_t)b * a.pages_stride;
         auto look = [&](uint32_t i) {
             const uint32_t tile = i < t.sinks ? i : t.window0 + (i - t.sinks);
-            return where<F, D, IN_PAGE>(p, table, b, h, (int64_t)tile * kAttendTile + wave * 32, t.length, t.from);
+            return look_at<IN_PAGE>(p, table, i < tile1 ? (int64_t)tile * kAttendTile + wave * 32 : t.length, t.length, t.from);
         };
         Running<XT, F, D> run;
 #pragma unroll
@@ -653,13 +700,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
 
         Keys<F, D> keys;
         Values<F, D> values;
-        Where<IN_PAGE> now = look(tile0);
+        Look<IN_PAGE> ahead = look(tile0);
+        Where<IN_PAGE> now = where<IN_PAGE>(p, b, h, ahead);
+        ahead = look(tile0 + 1);
         load_keys<F, D, IN_PAGE>(a.c, now, keys);
         load_values<F, D, IN_PAGE>(a.c, now, values);
         for (uint32_t i = tile0; i < tile1; ++i) {
-            Where<IN_PAGE> next = now;
-            next.seen = 0u;
-            if (i + 1 < tile1) next = look(i + 1);
+            const Where<IN_PAGE> next = where<IN_PAGE>(p, b, h, ahead);
+            ahead = look(i + 2);
             float s[8];
             if (now.seen != 0u) scores<XT, F, D>(q, keys, s);
             load_keys<F, D, IN_PAGE>(a.c, next, keys);
@@ -789,7 +837,7 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     p.group = a.n_q_heads / a.c.n_heads;
     p.parts = parts;
     p.cols = cols;
-    p.in_page = a.c.page_tokens % 32 == 0;
+    p.in_page = a.c.page_tokens % 16 == 0;
     p.seqs_each = (a.n_seqs + 255) / 256;
     uint32_t s = 0;                                        // (n < 2^31: m = ceil(2^(31 + s) / d) is near enough)
     while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
