@@ -497,7 +497,7 @@ kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, i
  *   pages_dev     page number of token t of sequence b: pages_dev[b * pages_stride + t / page_tokens] (device, int32);
  *                 entries beyond a sequence's last token, or of pages without a seen token, are not looked at
  *   lengths_dev   tokens per sequence (device, int32), at most max_tokens, the host's bound for sizing the launch;
- *                 pages_stride >= ceil(max_tokens / page_tokens)
+ *                 pages_stride >= ceil(max_tokens / page_tokens), n_seqs * ceil(max_tokens / 128) below 2^31 (KVTC_E_UNSUPPORTED beyond)
  *   out_dev       [n_seqs][n_q_heads][d_head] of `dtype`, contiguous, 16-byte aligned; lse_dev [n_seqs][n_q_heads] fp32, or null
  *   work_dev      kvtc_attend_work_bytes(...) bytes of device memory, 256-byte aligned (work_bytes less: KVTC_E_SMALL), all zero
  *                 before its first use (a call leaves zero what the next one needs so): calls on one stream may share

@@ -1477,6 +1477,7 @@ static kvtc_status check_attend(const char* who, const kvtc_cache* c, int n_seqs
     if (n_q_heads < 1 || n_q_heads > kCacheMaxHeads || n_q_heads % c->n_heads != 0)
         return fail(KVTC_E_ARG, "%s: n_q_heads=%d must be a multiple of the cache's %d heads, at most %d", who, n_q_heads, c->n_heads, kCacheMaxHeads);
     if (max_tokens < 1 || max_tokens > 0x7fffffffLL) return fail(KVTC_E_ARG, "%s: max_tokens=%lld outside 1..2^31-1", who, (long long)max_tokens);
+    if ((max_tokens + 127) / 128 * n_seqs > 0x7fffffffLL) return fail(KVTC_E_UNSUPPORTED, "%s: %d sequences of up to %lld tokens", who, n_seqs, (long long)max_tokens);
     return KVTC_OK;
 }
 

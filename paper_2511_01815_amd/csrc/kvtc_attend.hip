@@ -47,7 +47,7 @@ struct AttendPlan {                                        // what the host work
     AttendArgs a;
     int32_t group, parts, cols;                            // query heads of a KV head; items that share them; of each, at most
     int32_t in_page;                                       // 16 tokens from a multiple of 16 on lie in one page
-    int32_t seqs_each;                                     // sequences whose lengths a thread adds up
+    int32_t seqs_each;                                     // sequences whose lengths a lane adds up
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
 };
 
@@ -122,9 +122,8 @@ __device__ __forceinline__ void from_buffer(Rsrc r, uint32_t lane_off, uint32_t 
     }
 }
 
-__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
-}
+// (a division of 64 bits costs several times one of 32)
+__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) { return (n | d) >> 32 ? n / d : (uint32_t)n / (uint32_t)d; }
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
@@ -534,17 +533,19 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 
 // ---- the shares ----------------------------------------------------------------------------------------------------------------
 
-// Tiles of a sequence that hold a seen token: those of the sinks, then those of the window.  (At least one: every row has a result.)
-struct Tiles { uint32_t n, sinks, window0; int64_t length, from; };
+// The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles of four pieces.  (At least one: every
+// row has a result.)
+struct Tiles { uint32_t n, pieces, sinks, window0; int64_t length, from; };
 __device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int64_t length) {
     if (length < 0 || length > a.max_tokens) length = 0;
     Tiles t;
     t.length = length;
-    t.from = a.window ? max((int64_t)0, length - a.window) : 0;
-    const uint32_t all = (uint32_t)((length + kAttendTile - 1) / kAttendTile);
-    t.sinks = a.window ? min((uint32_t)((min(a.sinks, length) + kAttendTile - 1) / kAttendTile), all) : 0u;
-    t.window0 = max(t.sinks, (uint32_t)(t.from / kAttendTile));
-    t.n = max(1u, t.sinks + (all > t.window0 ? all - t.window0 : 0u));
+    t.from = a.window && length > a.window ? length - a.window : 0;
+    const uint32_t all = (uint32_t)((length + 31) / 32);
+    t.sinks = a.window ? (uint32_t)((a.sinks < length ? a.sinks : length) + 31) / 32 : 0u;
+    t.window0 = max(t.sinks, (uint32_t)(t.from / 32));
+    t.pieces = t.sinks + (all > t.window0 ? all - t.window0 : 0u);
+    t.n = max(1u, (t.pieces + 3) / 4);
     return t;
 }
 
@@ -555,61 +556,115 @@ template <> __device__ __forceinline__ void put_out<float>(float* x, float v) { 
 // floats of a part of an item in the workspace
 __host__ __device__ constexpr int part_floats(int cols, int d) { return (cols * (d + 2) + 3) / 4 * 4; }
 
-// The parts g0 .. g1 of an item, joined by a workgroup in their order.  Four outputs to a thread; where a row has less than 256 such, several threads share
-// the parts of one.  The loads of many parts are on their way together: the last workgroup of an item of a long context joins 64 parts of 2 KB.
-// lds: 4 x 16 x (D + 4) floats; stats: 64.
-constexpr int kJoinStep = 128;                             // parts whose weights are in the LDS at a time
+// Parts go from one workgroup to another whose L2 is another one.  They are stored and loaded at agent scope, past the L2: no cache needs to be written back or
+// emptied for them, which, at the end of every workgroup, cost more than all else there.  A workgroup is counted as come when its stores have been acknowledged.
+union Pair { uint64_t u; float f[2]; };
+__device__ __forceinline__ void put_pair(float* p, float first, float second) {
+    Pair v;
+    v.f[0] = first;
+    v.f[1] = second;
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Pair get_pair(const float* p) {
+    Pair v;
+    v.u = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return v;
+}
+
+// The parts g0 .. g1 of an item, joined by a workgroup in their order: (m, l) of every row, then the outputs, two to a thread; where the rows have fewer than
+// 512 outputs, several threads share the parts of one.  The first kAhead parts of each are under way while the maxima are found.
+// weight: [16][kJoinStep]; sum: [512]; stats: [32].
+constexpr int kJoinStep = 64, kAhead = 16;
 template <typename XT, int D>
-__device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* lds, float* stats) {
+__device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* weight, float* sum,
+                                           float* stats) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    float* weight = lds;                                   // [col][kJoinStep]
-    float* sum = lds + kAttendCols * kJoinStep;            // [256][4]
-    static_assert(4 * kAttendCols * (D + 4) >= kAttendCols * kJoinStep + 1024, "");
-    auto part_at = [&](uint32_t g) { return slots + (int64_t)(2 * g + (g == g0 ? 1 : 0)) * slot_floats; };
-    for (int c = wave; c < cols; c += 4) {                 // maximum and sum of each row
-        float top = kNoScore, l = 0.0f;
-        for (uint32_t g = g0 + lane; g <= g1; g += 64) top = fmaxf(top, part_at(g)[cols_all * D + c]);
+    const uint32_t n = g1 - g0 + 1;
+    auto part_at = [&](uint32_t k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
+    const int pairs = cols * D / 2, teams = pairs < 256 ? 256 / pairs : 1;
+    for (int j0 = 0; j0 < pairs; j0 += 256) {
+        const int team = pairs < 256 ? tid / pairs : 0, j = pairs < 256 ? tid - team * pairs : j0 + tid, c = min(2 * j / D, cols - 1);
+        const bool is = team < teams && j < pairs;
+        const int mine = is && team < (int)n ? ((int)n - team + teams - 1) / teams : 0;      // parts of this thread: team, team + teams, ...
+        auto mine_at = [&](int i) { return part_at((uint32_t)(team + i * teams)) + 2 * cols_all + 2 * j; };
+        Pair first[kAhead];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-        const float base = top == kNoScore ? 0.0f : top;
-        for (uint32_t g = g0 + lane; g <= g1; g += 64) l = __builtin_fmaf(part_at(g)[cols_all * D + cols_all + c], exp2_fast(part_at(g)[cols_all * D + c] - base), l);
+        for (int i = 0; i < kAhead; ++i) {
+            first[i].u = 0;
+            if (i < mine) first[i] = get_pair(mine_at(i));
+        }
+        if (j0 == 0) {
+            for (int cc = wave; cc < cols; cc += 4) {      // maximum and sum of a row, and the weights of its first parts
+                float m = kNoScore, l = 0.0f, m0 = kNoScore;
+                for (uint32_t k = lane; k < n; k += 64) {
+                    const Pair v = get_pair(part_at(k) + 2 * cc);
+                    const float top = fmaxf(m, v.f[0]), base = top == kNoScore ? 0.0f : top;
+                    l = l * exp2_fast(m - base) + v.f[1] * exp2_fast(v.f[0] - base);
+                    m = top;
+                    if (k < 64) m0 = v.f[0];
+                }
+                float top = m;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
-        if (lane == 0) { stats[c] = base; stats[16 + c] = l; }
-    }
-    __syncthreads();
-    const int quads = cols * D / 4, teams = quads < 256 ? 256 / quads : 1;
-    for (int j0 = 0; j0 < quads; j0 += 256) {
-        const int team = quads < 256 ? tid / quads : 0, j = quads < 256 ? tid - team * quads : j0 + tid, c = min(4 * j / D, cols - 1);
-        const bool is = team < teams && j < quads;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t from = g0; from <= g1; from += kJoinStep) {
-            const int n = (int)min((uint32_t)kJoinStep, g1 + 1 - from);
-            __syncthreads();
-            for (int k = tid; k < cols * kJoinStep; k += 256) {
-                const int cc = k / kJoinStep, g = k % kJoinStep;
-                if (g < n) weight[k] = exp2_fast(part_at(from + g)[cols_all * D + cc] - stats[cc]);
+                for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+                const float base = top == kNoScore ? 0.0f : top;
+                l *= exp2_fast(m - base);
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
+                if (lane == 0) { stats[cc] = base; stats[16 + cc] = l; }
+                weight[cc * kJoinStep + lane] = exp2_fast(m0 - base);
             }
             __syncthreads();
-            if (is) {
-#pragma unroll 8
-                for (int g = team; g < n; g += teams) {
-                    const f32x4 v = *reinterpret_cast<const f32x4*>(part_at(from + g) + 4 * j);
-                    o += v * weight[c * kJoinStep + g];
+        }
+        float o0 = 0.0f, o1 = 0.0f;
+        for (uint32_t from = 0; from < n; from += kJoinStep) {
+            if (from > 0 || j0 > 0) {                      // the weights of other parts than the first
+                if (n > kJoinStep) {
+                    __syncthreads();
+                    for (int k = tid; k < cols * kJoinStep; k += 256) {
+                        const int cc = k / kJoinStep;
+                        const uint32_t g = from + k % kJoinStep;
+                        if (g < n) weight[k] = exp2_fast(get_pair(part_at(g) + 2 * cc).f[0] - stats[cc]);
+                    }
+                    __syncthreads();
                 }
+            }
+            // this thread's parts among from .. from + kJoinStep
+            const int i0 = from == 0 ? 0 : ((int)from - team + teams - 1) / teams, i1 = min(mine, ((int)from + kJoinStep - team + teams - 1) / teams);
+            int i = i0;
+            if (from == 0) {
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                    if (k < i1) {
+                        const float w = weight[c * kJoinStep + team + k * teams];
+                        o0 = __builtin_fmaf(first[k].f[0], w, o0);
+                        o1 = __builtin_fmaf(first[k].f[1], w, o1);
+                    }
+                i = min(kAhead, i1);
+            }
+#pragma unroll 16
+            for (; i < i1; ++i) {
+                const Pair v = get_pair(mine_at(i));
+                const float w = weight[c * kJoinStep + team + i * teams - (int)from];
+                o0 = __builtin_fmaf(v.f[0], w, o0);
+                o1 = __builtin_fmaf(v.f[1], w, o1);
             }
         }
         if (teams > 1) {
-            *reinterpret_cast<f32x4*>(sum + 4 * tid) = o;
+            sum[2 * tid] = o0;
+            sum[2 * tid + 1] = o1;
             __syncthreads();
-            for (int k = 1; k < teams; ++k)
-                if (is && team == 0) o += *reinterpret_cast<const f32x4*>(sum + 4 * (k * quads + j));
+            if (is && team == 0)
+                for (int k = 1; k < teams; ++k) {
+                    o0 += sum[2 * (k * pairs + j)];
+                    o1 += sum[2 * (k * pairs + j) + 1];
+                }
         }
         if (is && team == 0) {
-            const int f = 4 * j - c * D;
+            const int f = 2 * j - c * D;
             const float l = stats[16 + c];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f + i, l == 0.0f ? 0.0f : o[i] / l);
+            XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+            put_out(out, l == 0.0f ? 0.0f : o0 / l);
+            put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
             if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
         }
     }
@@ -621,64 +676,43 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
     __shared__ float s_o[4][kAttendCols][D + 4];
     __shared__ float s_m[4][kAttendCols], s_l[4][kAttendCols];
-    __shared__ uint64_t s_scan[4], s_start;
-    __shared__ int s_seq;
     __shared__ uint32_t s_last;
 
-    // where the workgroup's share begins: a prefix sum over the sequences' tiles
-    const uint64_t heads = (uint64_t)a.c.n_heads * (uint32_t)p.parts, me = blockIdx.x;
-    uint64_t mine = 0;
-    const int first = tid * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
+    // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
+    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = blockIdx.x;
+    uint32_t mine = 0;
+    const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
     for (int b = first; b < last; ++b) {
         const int64_t length = a.lengths[b];
         if (me == 0 && (length < 0 || length > a.max_tokens)) report_lowest(a.status, (uint32_t)b);
         mine += tiles_of(a, length).n;
     }
-    uint64_t before = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t v = __shfl_up(before, d, 64);
-        if (lane >= d) before += v;
-    }
-    if (lane == 63) s_scan[wave] = before;
-    __syncthreads();
-    uint64_t all = 0;
-    before -= mine;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (w < wave) before += s_scan[w];
-        all += s_scan[w];
-    }
-    all *= heads;
-    const uint64_t groups = min((uint64_t)gridDim.x, all); // (no share is empty: each of an item's workgroups is waited for)
+    const uint32_t upto = wave_inclusive_scan(mine);
+    const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
+    const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
     if (me >= groups) return;
-    all = uniform64(all);
-    const uint64_t share0 = me * all / groups, share1 = (me + 1) * all / groups;
-    if (before * heads <= share0 && share0 < (before + mine) * heads) {
-        int b = first;
-        for (; b + 1 < last; ++b) {
-            const uint64_t n = tiles_of(a, a.lengths[b]).n;
-            if (share0 < (before + n) * heads) break;
-            before += n;
-        }
-        s_seq = b;
-        s_start = before * heads;
+    // me * all / groups, by the quotient and the remainder of all / groups
+    const uint64_t each = quotient(all, groups);
+    const uint32_t odd = (uint32_t)(all - each * groups);
+    const uint64_t share0 = me * each + me * odd / groups, share1 = (me + 1) * each + (me + 1) * odd / groups;
+    // the lane whose sequences it falls among, and the sequence
+    const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
+    int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
+    uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
+    Tiles t = tiles_of(a, scalar_at(a.lengths, b));
+    while (share0 >= seq0 + (uint64_t)t.n * heads) {
+        seq0 += (uint64_t)t.n * heads;
+        t = tiles_of(a, scalar_at(a.lengths, ++b));
     }
-    __syncthreads();
-    int b = __builtin_amdgcn_readfirstlane(s_seq);
-    uint64_t seq0 = uniform64(s_start);                               // the sequence's first tile, counted over all items
-    auto owner = [&](uint64_t tile) { return (uint32_t)(((tile + 1) * groups - 1) / all); };
+    uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
     const float factor = a.scale * 1.44269504088896340736f;
 
-    uint64_t at = share0;
-    while (at < share1) {
-        const Tiles t = tiles_of(a, scalar_at(a.lengths, b));
-        if (at >= seq0 + t.n * heads) {
-            seq0 += t.n * heads;
-            ++b;
-            continue;
+    for (uint64_t at = share0; at < share1;) {
+        if (item == heads) {
+            item = 0;
+            seq0 += (uint64_t)t.n * heads;
+            t = tiles_of(a, scalar_at(a.lengths, ++b));
         }
-        const uint32_t item = (uint32_t)((at - seq0) / t.n), tile0 = (uint32_t)((at - seq0) - (uint64_t)item * t.n);
         const uint32_t tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at));
         const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
         const int col0 = h * p.group + part * p.cols, cols = min(p.cols, p.group - part * p.cols);
@@ -687,8 +721,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (col < cols ? col : 0)) * a.q_head_stride, col < cols, q);
         const int32_t* table = a.pages + (int64_t)b * a.pages_stride;
         auto look = [&](uint32_t i) {
-            const uint32_t tile = i < t.sinks ? i : t.window0 + (i - t.sinks);
-            return look_at<IN_PAGE>(p, table, i < tile1 ? (int64_t)tile * kAttendTile + wave * 32 : t.length, t.length, t.from);
+            const uint32_t k = 4 * i + wave, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
+            return look_at<IN_PAGE>(p, table, i < tile1 && k < t.pieces ? (int64_t)piece * 32 : t.length, t.length, t.from);
         };
         Running<XT, F, D> run;
 #pragma unroll
@@ -734,53 +768,55 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
             if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
         }
         __syncthreads();
-        const uint64_t item0 = seq0 + (uint64_t)item * t.n;
-        const uint32_t g0 = owner(item0), g1 = owner(item0 + t.n - 1);
-        const bool whole = g0 == g1;
+        const bool whole = tile0 == 0 && tile1 == t.n;
         const int64_t row0 = (int64_t)b * a.n_q_heads + col0;
-        uint32_t* counters = static_cast<uint32_t*>(a.work);
         float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxGroups * 4);
         const int slot_floats = part_floats(p.cols, D);
         float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
-        for (int j = tid; j < cols * D; j += 256) {
-            const int c = j / D, f = j % D;
+        for (int j = tid; j < cols * D / 2; j += 256) {
+            const int c = 2 * j / D, f = 2 * j % D;
             float top = s_m[0][c];
 #pragma unroll
             for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][c]);
             const float base = top == kNoScore ? 0.0f : top;
-            float l = 0.0f, o = 0.0f;
+            float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float keep = exp2_fast(s_m[w][c] - base);
                 l = __builtin_fmaf(s_l[w][c], keep, l);
-                o = __builtin_fmaf(s_o[w][c][f], keep, o);
+                o0 = __builtin_fmaf(s_o[w][c][f], keep, o0);
+                o1 = __builtin_fmaf(s_o[w][c][f + 1], keep, o1);
             }
             if (whole) {
-                put_out(static_cast<XT*>(a.out) + (row0 + c) * D + f, l == 0.0f ? 0.0f : o / l);
+                XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+                put_out(out, l == 0.0f ? 0.0f : o0 / l);
+                put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
                 if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
             } else {
-                slot[c * D + f] = o;
-                if (f == 0) { slot[p.cols * D + c] = top; slot[p.cols * D + p.cols + c] = l; }
+                put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
+                if (f == 0) put_pair(slot + 2 * c, top, l);
             }
         }
         if (!whole) {
-            // the last of the item's workgroups to come here joins them
+            // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
+            const uint64_t item0 = seq0 + (uint64_t)item * t.n;
+            const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
+            const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (tid == 0) {
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-                const uint32_t came = __hip_atomic_fetch_add(&counters[g0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+                uint32_t* counter = static_cast<uint32_t*>(a.work) + g0;
+                const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 s_last = came == g1 - g0;
-                if (came == g1 - g0) __hip_atomic_store(&counters[g0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            if (s_last) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-                join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_m[0][0]);
-            }
+            if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
         }
         __syncthreads();
         at += tile1 - tile0;
+        tile0 = 0;
+        ++item;
     }
 }
 
@@ -797,7 +833,7 @@ static void shares_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols)
 static int groups_of(const kvtc_cache& c, int n_seqs, int parts, int64_t max_tokens, int64_t sinks, int64_t window) {
     int64_t tiles = (max_tokens + kAttendTile - 1) / kAttendTile;
     if (window) {
-        const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / kAttendTile + (window < max_tokens ? window : max_tokens) / kAttendTile + 3;
+        const int64_t some = ((sinks < max_tokens ? sinks : max_tokens) + (window < max_tokens ? window : max_tokens) + 3 * 32 + kAttendTile) / kAttendTile;
         tiles = some < tiles ? some : tiles;
     }
     const int64_t most = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), cap = most < kAttendMaxGroups ? most : kAttendMaxGroups;
@@ -838,7 +874,7 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     p.parts = parts;
     p.cols = cols;
     p.in_page = a.c.page_tokens % 16 == 0;
-    p.seqs_each = (a.n_seqs + 255) / 256;
+    p.seqs_each = (a.n_seqs + 63) / 64;
     uint32_t s = 0;                                        // (n < 2^31: m = ceil(2^(31 + s) / d) is near enough)
     while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
     p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);

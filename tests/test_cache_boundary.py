@@ -92,6 +92,7 @@ def test_bad_attention_is_refused():
     assert _attend(c, n=-1) == ARG and _attend(c, n=65537) == ARG
     assert _attend(c, hq=0) == ARG and _attend(c, hq=6) == ARG and _attend(c, hq=1028) == ARG
     assert _attend(c, most=0) == ARG and _attend(c, most=1 << 31) == ARG
+    assert _attend(c, n=65536, most=1 << 23, ps=1 << 30) == UNSUPPORTED        # more tiles than 31 bits count
     assert _attend(c, dtype=2) == ARG
     for name in ("q", "pages", "lengths", "out", "work"):
         assert _attend(c, **{name: None}) == ARG and "null" in kv.kvtc_last_error()
