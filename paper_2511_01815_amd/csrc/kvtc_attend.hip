@@ -26,6 +26,7 @@
 // Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Parts are cut towards zero so that they have
 // one sign, and in 16 bits are at least 2^-120, so that an infinite value stays one.
 #include <hip/hip_runtime.h>
+#include <cstdlib>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
 #include "kvtc_numeric.h"
@@ -38,9 +39,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kAttendTile = 128;                           // tokens of a workgroup's step, 32 to each of four waves
 constexpr int kAttendCols = 16;                            // query heads of an item, at most
-constexpr int kAttendMaxGroups = 1024;                     // workgroups of a launch, at most: a counter each in the workspace
+constexpr int kAttendMaxShares = 4096;                     // shares of a launch, at most: a counter each in the workspace
+constexpr int kShortPieces = 16;                          // rows of so many pieces at most are a wave's each
 constexpr float kNoScore = -__builtin_huge_valf();
 
 struct AttendPlan {                                        // what the host works out
@@ -533,9 +534,10 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 
 // ---- the shares ----------------------------------------------------------------------------------------------------------------
 
-// The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles of four pieces.  (At least one: every
+// The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles, a piece to each of WAVES waves.  (At least one: every
 // row has a result.)
 struct Tiles { uint32_t n, pieces, sinks, window0; int64_t length, from; };
+template <int WAVES>
 __device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int64_t length) {
     if (length < 0 || length > a.max_tokens) length = 0;
     Tiles t;
@@ -545,7 +547,7 @@ __device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int64_t length) {
     t.sinks = a.window ? (uint32_t)((a.sinks < length ? a.sinks : length) + 31) / 32 : 0u;
     t.window0 = max(t.sinks, (uint32_t)(t.from / 32));
     t.pieces = t.sinks + (all > t.window0 ? all - t.window0 : 0u);
-    t.n = max(1u, (t.pieces + 3) / 4);
+    t.n = max(1u, (t.pieces + WAVES - 1) / WAVES);
     return t;
 }
 
@@ -583,7 +585,7 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slo
     auto part_at = [&](uint32_t k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
     const int pairs = cols * D / 2, teams = pairs < 256 ? 256 / pairs : 1;
     for (int j0 = 0; j0 < pairs; j0 += 256) {
-        const int team = pairs < 256 ? tid / pairs : 0, j = pairs < 256 ? tid - team * pairs : j0 + tid, c = min(2 * j / D, cols - 1);
+        const int team = teams > 1 ? tid / pairs : 0, j = teams > 1 ? tid - team * pairs : j0 + tid, c = min(2 * j / D, cols - 1);
         const bool is = team < teams && j < pairs;
         const int mine = is && team < (int)n ? ((int)n - team + teams - 1) / teams : 0;      // parts of this thread: team, team + teams, ...
         auto mine_at = [&](int i) { return part_at((uint32_t)(team + i * teams)) + 2 * cols_all + 2 * j; };
@@ -670,26 +672,59 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slo
     }
 }
 
-template <typename XT, int F, int D, bool IN_PAGE>
+// A lane's results in runs of neighbouring features: put(first feature, values).
+template <typename XT, int F, int D, typename PUT>
+__device__ __forceinline__ void in_runs(const Running<XT, F, D>& run, int quarter, PUT put) {
+    if constexpr (F == KVTC_CACHE_INT4) {
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = run.o[2 * g + i % 2][i / 2] + run.low[g];
+            put(g * 32 + 8 * quarter, v);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v[D / 16];
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) v[i] = run.o[i][r];
+            put((4 * quarter + r) * (D / 16), v);
+        }
+    }
+}
+template <int N>
+__device__ __forceinline__ void put_run(uint16_t* x, const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<u32x2*>(x + i) = u32x2{round_pair(v[i], v[i + 1]), round_pair(v[i + 2], v[i + 3])};
+}
+template <int N>
+__device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(x + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+}
+
+// WAVES = 4: the waves of a workgroup take a piece each of the same tile, and their results are joined in the LDS.  WAVES = 1, for many short rows: every wave has a
+// share of its own, of whole items (those whose first piece falls into it), and nothing is joined.
+template <typename XT, int F, int D, bool IN_PAGE, int WAVES>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
     const AttendArgs& a = p.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
-    __shared__ float s_o[4][kAttendCols][D + 4];
-    __shared__ float s_m[4][kAttendCols], s_l[4][kAttendCols];
+    __shared__ float s_o[WAVES][WAVES > 1 ? kAttendCols : 1][WAVES > 1 ? D + 4 : 1], s_m[WAVES][kAttendCols], s_l[WAVES][kAttendCols];
     __shared__ uint32_t s_last;
 
     // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
-    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = blockIdx.x;
+    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave, most = WAVES > 1 ? gridDim.x : gridDim.x * 4;
     uint32_t mine = 0;
     const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
     for (int b = first; b < last; ++b) {
         const int64_t length = a.lengths[b];
         if (me == 0 && (length < 0 || length > a.max_tokens)) report_lowest(a.status, (uint32_t)b);
-        mine += tiles_of(a, length).n;
+        mine += tiles_of<WAVES>(a, length).n;
     }
     const uint32_t upto = wave_inclusive_scan(mine);
     const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
-    const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
+    const uint32_t groups = all < most ? (uint32_t)all : most;       // (no share is empty: each of an item's workgroups is waited for)
     if (me >= groups) return;
     // me * all / groups, by the quotient and the remainder of all / groups
     const uint64_t each = quotient(all, groups);
@@ -699,21 +734,27 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
     int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
     uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
-    Tiles t = tiles_of(a, scalar_at(a.lengths, b));
+    Tiles t = tiles_of<WAVES>(a, scalar_at(a.lengths, b));
     while (share0 >= seq0 + (uint64_t)t.n * heads) {
         seq0 += (uint64_t)t.n * heads;
-        t = tiles_of(a, scalar_at(a.lengths, ++b));
+        t = tiles_of<WAVES>(a, scalar_at(a.lengths, ++b));
     }
     uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
     const float factor = a.scale * 1.44269504088896340736f;
 
-    for (uint64_t at = share0; at < share1;) {
+    uint64_t at = share0;
+    if (WAVES == 1 && tile0 > 0) {
+        at += t.n - tile0;
+        tile0 = 0;
+        ++item;
+    }
+    while (at < share1) {
         if (item == heads) {
             item = 0;
             seq0 += (uint64_t)t.n * heads;
-            t = tiles_of(a, scalar_at(a.lengths, ++b));
+            t = tiles_of<WAVES>(a, scalar_at(a.lengths, ++b));
         }
-        const uint32_t tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at));
+        const uint32_t tile1 = WAVES > 1 ? (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at)) : t.n;
         const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
         const int col0 = h * p.group + part * p.cols, cols = min(p.cols, p.group - part * p.cols);
 
@@ -721,7 +762,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (col < cols ? col : 0)) * a.q_head_stride, col < cols, q);
         const int32_t* table = a.pages + (int64_t)b * a.pages_stride;
         auto look = [&](uint32_t i) {
-            const uint32_t k = 4 * i + wave, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
+            const uint32_t k = WAVES > 1 ? WAVES * i + wave : i, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
             return look_at<IN_PAGE>(p, table, i < tile1 && k < t.pieces ? (int64_t)piece * 32 : t.length, t.length, t.from);
         };
         Running<XT, F, D> run;
@@ -750,7 +791,6 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
             now = next;
         }
 
-        // the four waves' results, joined
         run.l += __shfl_xor(run.l, 16, 64);
         run.l += __shfl_xor(run.l, 32, 64);
         if constexpr (F == KVTC_CACHE_INT4) {
@@ -760,60 +800,74 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
                 run.low[g] += __shfl_xor(run.low[g], 32, 64);
             }
         }
-        if (col < cols) {
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
-            if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
-        }
-        __syncthreads();
-        const bool whole = tile0 == 0 && tile1 == t.n;
         const int64_t row0 = (int64_t)b * a.n_q_heads + col0;
-        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxGroups * 4);
-        const int slot_floats = part_floats(p.cols, D);
-        float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
-        for (int j = tid; j < cols * D / 2; j += 256) {
-            const int c = 2 * j / D, f = 2 * j % D;
-            float top = s_m[0][c];
+        if constexpr (WAVES == 1) {
+            if (col < cols) {
+                const float l = run.l;
+                XT* out = static_cast<XT*>(a.out) + (row0 + col) * D;
+                in_runs<XT, F, D>(run, quarter, [&](int f, auto& v) {
 #pragma unroll
-            for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][c]);
-            const float base = top == kNoScore ? 0.0f : top;
-            float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+                    for (float& x : v) x = l == 0.0f ? 0.0f : x / l;
+                    put_run(out + f, v);
+                });
+                if (a.lse && quarter == 0) a.lse[row0 + col] = l == 0.0f ? kNoScore : (run.m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            }
+        } else {
+            const bool whole = tile0 == 0 && tile1 == t.n;
+            float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxShares * 4);
+            const int slot_floats = part_floats(p.cols, D);
+            float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
+            // the waves' results, joined
+            if (col < cols) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float keep = exp2_fast(s_m[w][c] - base);
-                l = __builtin_fmaf(s_l[w][c], keep, l);
-                o0 = __builtin_fmaf(s_o[w][c][f], keep, o0);
-                o1 = __builtin_fmaf(s_o[w][c][f + 1], keep, o1);
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
+                if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
             }
-            if (whole) {
-                XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
-                put_out(out, l == 0.0f ? 0.0f : o0 / l);
-                put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-                if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
-            } else {
-                put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
-                if (f == 0) put_pair(slot + 2 * c, top, l);
-            }
-        }
-        if (!whole) {
-            // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
-            const uint64_t item0 = seq0 + (uint64_t)item * t.n;
-            const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
-            const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            if (tid == 0) {
+            for (int j = tid; j < cols * D / 2; j += 256) {
+                const int c = 2 * j / D, f = 2 * j % D;
+                float top = s_m[0][c];
+#pragma unroll
+                for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][c]);
+                const float base = top == kNoScore ? 0.0f : top;
+                float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float keep = exp2_fast(s_m[w][c] - base);
+                    l = __builtin_fmaf(s_l[w][c], keep, l);
+                    o0 = __builtin_fmaf(s_o[w][c][f], keep, o0);
+                    o1 = __builtin_fmaf(s_o[w][c][f + 1], keep, o1);
+                }
+                if (whole) {
+                    XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+                    put_out(out, l == 0.0f ? 0.0f : o0 / l);
+                    put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
+                    if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                } else {
+                    put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
+                    if (f == 0) put_pair(slot + 2 * c, top, l);
+                }
+            }
+            if (!whole) {
+                // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
+                const uint64_t item0 = seq0 + (uint64_t)item * t.n;
+                const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
+                const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
                 uint32_t* counter = static_cast<uint32_t*>(a.work) + g0;
-                const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = came == g1 - g0;
-                if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (tid == 0) {
+                    const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    s_last = came == g1 - g0;
+                    if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();
+                if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
             }
             __syncthreads();
-            if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
         }
-        __syncthreads();
         at += tile1 - tile0;
         tile0 = 0;
         ++item;
@@ -822,54 +876,80 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 
+// What runs: shares, a wave's or a workgroup's each.
+struct Shares { int waves, n; };
+
+template <typename XT, int F, int D, bool IN_PAGE>
+static void launch_shares(const AttendPlan& p, const Shares& s, hipStream_t stream) {
+    if (s.waves == 1) hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1>), dim3((s.n + 3) / 4), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4>), dim3(s.n), dim3(256), 0, stream, p);
+}
+template <typename XT, int F, int D>
+static void launch_pages(const AttendPlan& p, const Shares& s, hipStream_t stream) {
+    if (p.in_page) launch_shares<XT, F, D, true>(p, s, stream);
+    else launch_shares<XT, F, D, false>(p, s, stream);
+}
+template <typename XT, int F>
+static void launch_width(const AttendPlan& p, const Shares& s, hipStream_t stream) {
+    if (p.a.c.d_head == 64) launch_pages<XT, F, 64>(p, s, stream);
+    else if (p.a.c.d_head == 128) launch_pages<XT, F, 128>(p, s, stream);
+    else launch_pages<XT, F, 256>(p, s, stream);
+}
+// The kernels of one type and format (the file is compiled once for each, side by side), and with the first of them the host's part.
+#if KVTC_ATTEND_PART < 3
+typedef uint16_t PartType;
+#else
+typedef float PartType;
+#endif
+#define KVTC_ATTEND_NAME_(k) launch_attend_##k
+#define KVTC_ATTEND_NAME(k) KVTC_ATTEND_NAME_(k)
+void KVTC_ATTEND_NAME(KVTC_ATTEND_PART)(const AttendPlan& p, const Shares& s, hipStream_t stream) { launch_width<PartType, KVTC_ATTEND_PART % 3>(p, s, stream); }
+
+#if KVTC_ATTEND_PART == 0
+void launch_attend_1(const AttendPlan&, const Shares&, hipStream_t);
+void launch_attend_2(const AttendPlan&, const Shares&, hipStream_t);
+void launch_attend_3(const AttendPlan&, const Shares&, hipStream_t);
+void launch_attend_4(const AttendPlan&, const Shares&, hipStream_t);
+void launch_attend_5(const AttendPlan&, const Shares&, hipStream_t);
+
 // Items that share a KV head's query heads, and how many of these each has.
-static void shares_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) {
+static void heads_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) {
     const int group = n_q_heads / c.n_heads;
     parts = (group + kAttendCols - 1) / kAttendCols;
     cols = (group + parts - 1) / parts;
 }
 
-// Workgroups: two to a compute unit (one of wide heads), no more than there can be tiles.
-static int groups_of(const kvtc_cache& c, int n_seqs, int parts, int64_t max_tokens, int64_t sinks, int64_t window) {
-    int64_t tiles = (max_tokens + kAttendTile - 1) / kAttendTile;
+// Shares, a wave's or a workgroup's each: as many as run at once (two workgroups to a compute unit, one of wide heads), no more than there can be tiles.
+static Shares shares_at_once(const kvtc_cache& c, int n_seqs, int parts, int64_t max_tokens, int64_t sinks, int64_t window) {
+    int64_t pieces = (max_tokens + 31) / 32;
     if (window) {
-        const int64_t some = ((sinks < max_tokens ? sinks : max_tokens) + (window < max_tokens ? window : max_tokens) + 3 * 32 + kAttendTile) / kAttendTile;
-        tiles = some < tiles ? some : tiles;
+        const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / 32 + (window < max_tokens ? window : max_tokens) / 32 + 3;
+        pieces = some < pieces ? some : pieces;
     }
-    const int64_t most = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), cap = most < kAttendMaxGroups ? most : kAttendMaxGroups;
+    Shares s;
+    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2);
+    s.waves = pieces <= kShortPieces && (int64_t)n_seqs * c.n_heads * parts >= 4 * places ? 1 : 4;
+    if (const char* e = std::getenv("KVTC_W")) s.waves = std::atoi(e);
+    const int64_t tiles = (pieces + s.waves - 1) / s.waves, at_once = places * (4 / s.waves), most = at_once < kAttendMaxShares ? at_once : kAttendMaxShares;
     const __int128 all = (__int128)tiles * n_seqs * c.n_heads * parts;
-    return (int)(all < cap ? (int64_t)all : cap);
+    s.n = (int)(all < most ? (int64_t)all : most);
+    return s;
 }
 
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {
     int parts, cols;
-    shares_of(c, n_q_heads, parts, cols);
-    return (size_t)kAttendMaxGroups * 4 + (size_t)groups_of(c, n_seqs < 1 ? 1 : n_seqs, parts, max_tokens, 0, 0) * 2 * part_floats(cols, c.d_head) * sizeof(float);
-}
-
-template <typename XT, int F, int D>
-static void launch_pages(const AttendPlan& p, int groups, hipStream_t stream) {
-    if (p.in_page) hipLaunchKernelGGL((attend_kernel<XT, F, D, true>), dim3(groups), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attend_kernel<XT, F, D, false>), dim3(groups), dim3(256), 0, stream, p);
-}
-template <typename XT, int F>
-static void launch_width(const AttendPlan& p, int groups, hipStream_t stream) {
-    if (p.a.c.d_head == 64) launch_pages<XT, F, 64>(p, groups, stream);
-    else if (p.a.c.d_head == 128) launch_pages<XT, F, 128>(p, groups, stream);
-    else launch_pages<XT, F, 256>(p, groups, stream);
-}
-template <typename XT>
-static void launch_format(const AttendPlan& p, int groups, hipStream_t stream) {
-    if (p.a.c.format == KVTC_CACHE_BF16) launch_width<XT, KVTC_CACHE_BF16>(p, groups, stream);
-    else if (p.a.c.format == KVTC_CACHE_FP8) launch_width<XT, KVTC_CACHE_FP8>(p, groups, stream);
-    else launch_width<XT, KVTC_CACHE_INT4>(p, groups, stream);
+    heads_of(c, n_q_heads, parts, cols);
+    // (a window may make for smaller tiles, and never for more shares of them than there are waves at once)
+    const int n = n_seqs < 1 ? 1 : n_seqs;
+    const Shares s = shares_at_once(c, n, parts, max_tokens, 0, 0), small = shares_at_once(c, n, parts, max_tokens < 32 * kShortPieces ? max_tokens : 32 * kShortPieces, 0, 0);
+    return (size_t)kAttendMaxShares * 4 + (size_t)(s.n > small.n ? s.n : small.n) * 2 * part_floats(cols, c.d_head) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream) {
     AttendPlan p;
     p.a = a;
     int parts, cols;
-    shares_of(a.c, a.n_q_heads, parts, cols);
+    heads_of(a.c, a.n_q_heads, parts, cols);
     p.group = a.n_q_heads / a.c.n_heads;
     p.parts = parts;
     p.cols = cols;
@@ -879,10 +959,12 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
     p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);
     p.page_shift = 31 + s;
-    const int groups = groups_of(a.c, a.n_seqs, parts, a.max_tokens, a.sinks, a.window);
-    if (dtype == KVTC_BF16) launch_format<uint16_t>(p, groups, stream);
-    else launch_format<float>(p, groups, stream);
+    const Shares shares = shares_at_once(a.c, a.n_seqs, parts, a.max_tokens, a.sinks, a.window);
+    static void (*const launch[6])(const AttendPlan&, const Shares&, hipStream_t) = {launch_attend_0, launch_attend_1, launch_attend_2, launch_attend_3, launch_attend_4, launch_attend_5};
+    launch[(dtype == KVTC_BF16 ? 0 : 3) + a.c.format](p, shares, stream);
     return hipGetLastError();
 }
+
+#endif
 
 }  // namespace kvtc
