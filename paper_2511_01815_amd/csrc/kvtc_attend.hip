@@ -26,7 +26,6 @@
 // Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Parts are cut towards zero so that they have
 // one sign, and in 16 bits are at least 2^-120, so that an infinite value stays one.
 #include <hip/hip_runtime.h>
-#include <cstdlib>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
 #include "kvtc_numeric.h"
@@ -574,81 +573,71 @@ __device__ __forceinline__ Pair get_pair(const float* p) {
 }
 
 // The parts g0 .. g1 of an item, joined by a workgroup in their order: (m, l) of every row, then the outputs, two to a thread; where the rows have fewer than
-// 512 outputs, several threads share the parts of one.  The first kAhead parts of each are under way while the maxima are found.
-// weight: [16][kJoinStep]; sum: [512]; stats: [32].
+// 512 outputs, several threads share the parts of one.  kAhead parts are on their way together, the first of them while the maxima are found (one after another
+// 64 parts took 17 us).  weight: [16][kJoinStep]; sum: [512]; stats: [32].
 constexpr int kJoinStep = 64, kAhead = 16;
 template <typename XT, int D>
 __device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* weight, float* sum,
                                            float* stats) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const uint32_t n = g1 - g0 + 1;
-    auto part_at = [&](uint32_t k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
+    const int n = (int)(g1 - g0) + 1;
+    auto part_at = [&](int k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
     const int pairs = cols * D / 2, teams = pairs < 256 ? 256 / pairs : 1;
     for (int j0 = 0; j0 < pairs; j0 += 256) {
-        const int team = teams > 1 ? tid / pairs : 0, j = teams > 1 ? tid - team * pairs : j0 + tid, c = min(2 * j / D, cols - 1);
-        const bool is = team < teams && j < pairs;
-        const int mine = is && team < (int)n ? ((int)n - team + teams - 1) / teams : 0;      // parts of this thread: team, team + teams, ...
-        auto mine_at = [&](int i) { return part_at((uint32_t)(team + i * teams)) + 2 * cols_all + 2 * j; };
-        Pair first[kAhead];
+        const int team = teams > 1 ? tid / pairs : 0, j = min(teams > 1 ? tid - team * pairs : j0 + tid, pairs - 1), c = 2 * j / D;
+        const bool is = team < teams && (teams > 1 || j0 + tid < pairs);
+        // parts team, team + teams, ...; those past the last are the last again, and count for nothing
+        auto get = [&](int k) { return get_pair(part_at(min(k, n - 1)) + 2 * cols_all + 2 * j); };
+        float o0 = 0.0f, o1 = 0.0f;
+        for (int from = 0; from < n; from += kJoinStep) {
+            Pair v[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            first[i].u = 0;
-            if (i < mine) first[i] = get_pair(mine_at(i));
-        }
-        if (j0 == 0) {
-            for (int cc = wave; cc < cols; cc += 4) {      // maximum and sum of a row, and the weights of its first parts
-                float m = kNoScore, l = 0.0f, m0 = kNoScore;
-                for (uint32_t k = lane; k < n; k += 64) {
-                    const Pair v = get_pair(part_at(k) + 2 * cc);
-                    const float top = fmaxf(m, v.f[0]), base = top == kNoScore ? 0.0f : top;
-                    l = l * exp2_fast(m - base) + v.f[1] * exp2_fast(v.f[0] - base);
-                    m = top;
-                    if (k < 64) m0 = v.f[0];
+            for (int i = 0; i < kAhead; ++i) {
+                v[i].u = 0;
+                if (from + i * teams < n) v[i] = get(from + team + i * teams);      // (the same in all threads)
+            }
+            if (from > 0 || j0 > 0) __syncthreads();       // (the weights before these have been used)
+            if (j0 == 0 && from == 0) {
+                for (int cc = wave; cc < cols; cc += 4) {  // maximum and sum of a row, and the weights of its first parts
+                    float m = kNoScore, l = 0.0f, m0 = kNoScore;
+                    for (int k = lane; k < n; k += 64) {
+                        const Pair w = get_pair(part_at(k) + 2 * cc);
+                        const float top = fmaxf(m, w.f[0]), base = top == kNoScore ? 0.0f : top;
+                        l = l * exp2_fast(m - base) + w.f[1] * exp2_fast(w.f[0] - base);
+                        m = top;
+                        if (k < 64) m0 = w.f[0];
+                    }
+                    float top = m;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+                    const float base = top == kNoScore ? 0.0f : top;
+                    l *= exp2_fast(m - base);
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
+                    if (lane == 0) { stats[cc] = base; stats[16 + cc] = l; }
+                    weight[cc * kJoinStep + lane] = exp2_fast(m0 - base);
                 }
-                float top = m;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-                const float base = top == kNoScore ? 0.0f : top;
-                l *= exp2_fast(m - base);
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
-                if (lane == 0) { stats[cc] = base; stats[16 + cc] = l; }
-                weight[cc * kJoinStep + lane] = exp2_fast(m0 - base);
+            } else if (n > kJoinStep) {
+                for (int k = tid; k < cols * kJoinStep; k += 256) {
+                    const int cc = k / kJoinStep, g = from + k % kJoinStep;
+                    weight[k] = g < n ? exp2_fast(get_pair(part_at(g) + 2 * cc).f[0] - stats[cc]) : 0.0f;
+                }
             }
             __syncthreads();
-        }
-        float o0 = 0.0f, o1 = 0.0f;
-        for (uint32_t from = 0; from < n; from += kJoinStep) {
-            if (from > 0 || j0 > 0) {                      // the weights of other parts than the first
-                if (n > kJoinStep) {
-                    __syncthreads();
-                    for (int k = tid; k < cols * kJoinStep; k += 256) {
-                        const int cc = k / kJoinStep;
-                        const uint32_t g = from + k % kJoinStep;
-                        if (g < n) weight[k] = exp2_fast(get_pair(part_at(g) + 2 * cc).f[0] - stats[cc]);
-                    }
-                    __syncthreads();
-                }
-            }
-            // this thread's parts among from .. from + kJoinStep
-            const int i0 = from == 0 ? 0 : ((int)from - team + teams - 1) / teams, i1 = min(mine, ((int)from + kJoinStep - team + teams - 1) / teams);
-            int i = i0;
-            if (from == 0) {
+            const int here = min(kJoinStep, n - from);
+            for (int k0 = team; k0 < here; k0 += kAhead * teams) {
+                if (k0 != team) {
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-                    if (k < i1) {
-                        const float w = weight[c * kJoinStep + team + k * teams];
-                        o0 = __builtin_fmaf(first[k].f[0], w, o0);
-                        o1 = __builtin_fmaf(first[k].f[1], w, o1);
-                    }
-                i = min(kAhead, i1);
-            }
-#pragma unroll 16
-            for (; i < i1; ++i) {
-                const Pair v = get_pair(mine_at(i));
-                const float w = weight[c * kJoinStep + team + i * teams - (int)from];
-                o0 = __builtin_fmaf(v.f[0], w, o0);
-                o1 = __builtin_fmaf(v.f[1], w, o1);
+                    for (int i = 0; i < kAhead; ++i) v[i] = get(from + k0 + i * teams);
+                }
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int k = k0 + i * teams;
+                    const bool one = k < here;
+                    const float w = one ? weight[c * kJoinStep + k] : 0.0f;
+                    o0 = __builtin_fmaf(one ? v[i].f[0] : 0.0f, w, o0);
+                    o1 = __builtin_fmaf(one ? v[i].f[1] : 0.0f, w, o1);
+                }
             }
         }
         if (teams > 1) {
@@ -929,7 +918,6 @@ static Shares shares_at_once(const kvtc_cache& c, int n_seqs, int parts, int64_t
     Shares s;
     const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2);
     s.waves = pieces <= kShortPieces && (int64_t)n_seqs * c.n_heads * parts >= 4 * places ? 1 : 4;
-    if (const char* e = std::getenv("KVTC_W")) s.waves = std::atoi(e);
     const int64_t tiles = (pieces + s.waves - 1) / s.waves, at_once = places * (4 / s.waves), most = at_once < kAttendMaxShares ? at_once : kAttendMaxShares;
     const __int128 all = (__int128)tiles * n_seqs * c.n_heads * parts;
     s.n = (int)(all < most ? (int64_t)all : most);
