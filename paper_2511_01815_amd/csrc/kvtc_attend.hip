@@ -48,12 +48,27 @@ struct AttendPlan {                                        // what the host work
     int32_t group, parts, cols;                            // query heads of a KV head; items that share them; of each, at most
     int32_t in_page;                                       // 16 tokens from a multiple of 16 on lie in one page
     int32_t seqs_each;                                     // sequences whose lengths a lane adds up
+    uint32_t max_tokens, sinks, window;                    // those of `a`, at most 2^31 - 1
+    int64_t scale_stride;                                  // bytes of a page's scales
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
 };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// The larger of what lanes 16 and 32 apart hold, in all lanes.
+__device__ __forceinline__ float max_over_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_over_quarters(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 // the high halves of two words (bf16 by cutting), first one low
 __device__ __forceinline__ uint32_t high_halves(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x07060302u); }
 __device__ __forceinline__ uint32_t low_halves(uint32_t first, uint32_t second) { return __builtin_amdgcn_perm(second, first, 0x05040100u); }
@@ -89,39 +104,34 @@ __device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS])
     }
 }
 
+// Constants whose values the compiler is not told, so that they are in registers and one instruction takes what would be two with literals: (w & mask) | base, and v * half + zero.
+struct Constants { uint32_t mask, base; float zero; };
+__device__ __forceinline__ Constants constants() {
+    Constants c{0x000f000fu, 0x43004300u, 0.0f};
+    asm volatile("" : "+s"(c.mask), "+v"(c.base), "+s"(c.zero));
+    return c;
+}
+
 // ---- the tokens in hand --------------------------------------------------------------------------------------------------------
 
-// N dwords (or half of one) from a row, by an address of the lane's own or by an offset from what the wave has in common.
+#define KVTC_GLOBAL __attribute__((address_space(1)))
+typedef const KVTC_GLOBAL uint8_t* Bytes;                  // (said to be global memory, so that a place kept in scalar registers stays known as that)
+__device__ __forceinline__ Bytes bytes_at(const void* p) { return reinterpret_cast<Bytes>(reinterpret_cast<uintptr_t>(p)); }
+// BYTES of a row, in dwords (or half of one).
 template <int BYTES>
-__device__ __forceinline__ void from_pointer(const uint8_t* p, uint32_t* w) {
-    if constexpr (BYTES == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
-    else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
-    else if constexpr (BYTES == 8) { const u32x2 v = *reinterpret_cast<const u32x2*>(p); w[0] = v[0]; w[1] = v[1]; }
+__device__ __forceinline__ void load(Bytes p, uint32_t* w) {
+    if constexpr (BYTES == 2) w[0] = *reinterpret_cast<const KVTC_GLOBAL uint16_t*>(p);
+    else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const KVTC_GLOBAL uint32_t*>(p);
+    else if constexpr (BYTES == 8) { const u32x2 v = *reinterpret_cast<const KVTC_GLOBAL u32x2*>(p); w[0] = v[0]; w[1] = v[1]; }
     else {
 #pragma unroll
         for (int i = 0; i < BYTES / 16; ++i) {
-            const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+            const u32x4 v = reinterpret_cast<const KVTC_GLOBAL u32x4*>(p)[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
         }
     }
 }
-typedef __amdgpu_buffer_rsrc_t Rsrc;
-template <int BYTES>
-__device__ __forceinline__ void from_buffer(Rsrc r, uint32_t lane_off, uint32_t off, uint32_t* w) {
-    if constexpr (BYTES == 2) w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, lane_off, off, 0);
-    else if constexpr (BYTES == 4) w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, lane_off, off, 0);
-    else if constexpr (BYTES == 8) { const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, lane_off, off, 0); w[0] = v[0]; w[1] = v[1]; }
-    else {
-#pragma unroll
-        for (int i = 0; i < BYTES / 16; ++i) {
-            const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, lane_off + 16 * i, off, 0);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
-        }
-    }
-}
-
 // (a division of 64 bits costs several times one of 32)
 __device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) { return (n | d) >> 32 ? n / d : (uint32_t)n / (uint32_t)d; }
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
@@ -129,13 +139,26 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
 }
 
+// What the tokens of an item (a sequence, a KV head) have in common; the same in all lanes.  (Few words: with the call's arguments at hand instead, the scalar registers did not
+// do, and half of the vector unit's work in 8 bits was to keep and fetch theirs.)
+struct Item {
+    const int32_t* table;
+    Bytes k, v, k_scales, v_scales;                        // the head's, in page 0
+    uint32_t length, from, sinks, b;
+};
+// A place that is the same in all lanes, in scalar registers, and 32 bits of the lane's own.  (The compiler left to itself keeps these as 64 bits, and adds them up for every load.)
+__device__ __forceinline__ Bytes lane_at(Bytes base, int64_t offset, uint32_t lane) {
+    uint64_t p = reinterpret_cast<uint64_t>(base + offset);
+    asm("" : "+s"(p));
+    asm volatile("" : "+v"(lane));
+    return reinterpret_cast<Bytes>(p) + lane;
+}
 // Where a wave's 32 tokens are, and which of them are seen.
 template <bool IN_PAGE>
 struct Where {
     uint32_t seen;             // a bit each, the same in all lanes; none: nothing is loaded
-    int64_t row[IN_PAGE ? 2 : 1], scale[IN_PAGE ? 2 : 1];      // IN_PAGE: of the first token of each half (bytes; entries), the same in all lanes; else of token lane % 32
+    int64_t row[IN_PAGE ? 2 : 1], scale[IN_PAGE ? 2 : 1];      // bytes from the item's bases.  IN_PAGE: of the first token of each half, the same in all lanes; else of token lane % 32
 };
-
 // The same before the pages are known: their numbers are on their way, and are not waited for until the places are worked out, a step later.  (The vector
 // unit's loads come back in order: a look that is waited for at once waits for the keys and values before it.)  IN_PAGE: 16 tokens lie in one
 // page, and the numbers come through the scalar cache.
@@ -149,36 +172,39 @@ __device__ __forceinline__ int32_t scalar_at(const int32_t* p, int64_t i) { retu
 
 __device__ __forceinline__ uint32_t page_index(const AttendPlan& p, uint32_t token) { return (uint32_t)(((uint64_t)token * p.page_mul) >> p.page_shift); }
 
+// t: the first of the 32 tokens, below 2^31
 template <bool IN_PAGE>
-__device__ __forceinline__ Look<IN_PAGE> look_at(const AttendPlan& p, const int32_t* table, int64_t t, int64_t length, int64_t from) {
-    auto below = [](int64_t n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+__device__ __forceinline__ Look<IN_PAGE> look_at(const AttendPlan& p, const Item& item, uint32_t t) {
+    auto below = [&](uint32_t end) {                       // of the 32 tokens, those before `end`
+        const int32_t n = (int32_t)(end - t);
+        return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+    };
     Look<IN_PAGE> w;
-    w.seen = below(length - t) & (below(p.a.sinks - t) | ~below(from - t));
+    w.seen = below(item.length) & (below(item.sinks) | ~below(item.from));
     if constexpr (IN_PAGE) {
-        w.token = (uint32_t)t;
+        w.token = t;
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             w.page[n] = 0;
-            if (w.seen >> (16 * n) & 0xffffu) w.page[n] = scalar_at(table, page_index(p, w.token + 16 * n));
+            if (w.seen >> (16 * n) & 0xffffu) w.page[n] = scalar_at(item.table, page_index(p, w.token + 16 * n));
         }
     } else {
         const int mine = (int)(threadIdx.x & 31);
-        w.token = (uint32_t)t + mine;
+        w.token = t + mine;
         w.page[0] = 0;
-        if (w.seen >> mine & 1u) w.page[0] = table[page_index(p, w.token)];
+        if (w.seen >> mine & 1u) w.page[0] = item.table[page_index(p, w.token)];
     }
     return w;
 }
 
-template <bool IN_PAGE>
-__device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, int b, int h, const Look<IN_PAGE>& l) {
-    const AttendArgs& a = p.a;
+template <int SW, bool IN_PAGE>
+__device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, const Item& item, const Look<IN_PAGE>& l) {
     Where<IN_PAGE> w;
     w.seen = l.seen;
     auto place = [&](uint32_t token, int32_t page, int64_t& row, int64_t& scale) {
-        const uint32_t in = token - page_index(p, token) * (uint32_t)a.c.page_tokens;
-        row = (int64_t)page * a.c.page_stride + (int64_t)h * a.c.head_stride + (int64_t)in * a.c.token_stride;
-        scale = ((int64_t)page * a.c.n_heads + h) * a.c.page_tokens + in;
+        const uint32_t in = token - page_index(p, token) * (uint32_t)p.a.c.page_tokens;
+        row = (int64_t)page * p.a.c.page_stride + (uint32_t)(in * (uint32_t)p.a.c.token_stride);
+        scale = (int64_t)page * p.scale_stride + (int64_t)((uint64_t)in * (4 * SW));
     };
     if constexpr (IN_PAGE) {
 #pragma unroll
@@ -186,18 +212,18 @@ __device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, int b, int 
             const uint32_t mine = 0xffffu << (16 * n);
             w.row[n] = w.scale[n] = 0;
             if ((l.seen & mine) == 0u) continue;
-            if ((uint32_t)l.page[n] < (uint32_t)a.c.n_pages) {
+            if ((uint32_t)l.page[n] < (uint32_t)p.a.c.n_pages) {
                 place(l.token + 16 * n, l.page[n], w.row[n], w.scale[n]);
             } else {
-                if ((threadIdx.x & 63) == 0) report_lowest(a.status, (uint32_t)b);
+                if ((threadIdx.x & 63) == 0) report_lowest(p.a.status, item.b);
                 w.seen &= ~mine;
             }
         }
     } else {
         w.row[0] = w.scale[0] = 0;
-        const bool mine = l.seen >> (threadIdx.x & 31) & 1u, is = mine && (uint32_t)l.page[0] < (uint32_t)a.c.n_pages;
+        const bool mine = l.seen >> (threadIdx.x & 31) & 1u, is = mine && (uint32_t)l.page[0] < (uint32_t)p.a.c.n_pages;
         if (is) place(l.token, l.page[0], w.row[0], w.scale[0]);
-        else if (mine) report_lowest(a.status, (uint32_t)b);
+        else if (mine) report_lowest(p.a.status, item.b);
         w.seen = (uint32_t)__ballot(is);
     }
     return w;
@@ -228,36 +254,28 @@ struct Values {
 // the k-th of the lane's 8 tokens, among the wave's 32
 __device__ __forceinline__ int token_of(int k, int quarter) { return (k < 4 ? k : 12 + k) + 4 * quarter; }
 
-// What a half's 16 tokens have in common: `bytes` from the first one's on; a half without a seen token has none, and its loads give zeros.
-template <bool IN_PAGE>
-__device__ __forceinline__ Rsrc half_at(const void* pool, int64_t offset, uint32_t bytes, uint32_t seen, int n) {
-    return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(const_cast<void*>(pool)) + offset, 0, (seen >> (16 * n) & 0xffffu) != 0u ? (int)bytes : 0, 0x00027000);
-}
-
 template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_scales(const void* scales, const Where<IN_PAGE>& at, int quarter, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
+__device__ __forceinline__ void load_scales(Bytes scales, const Where<IN_PAGE>& at, int quarter, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
     constexpr int SW = Shape<F, D>::SW;
     if constexpr (SW > 0) {
         if constexpr (IN_PAGE) {                           // the four tokens' scales lie side by side
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const Rsrc r = half_at<IN_PAGE>(scales, at.scale[n] * (4 * SW), 16 * 4 * SW, at.seen, n);
                 uint32_t w[4 * SW];
-                from_buffer<16 * SW>(r, (uint32_t)(quarter * 16 * SW), 0, w);
+                load<16 * SW>(lane_at(scales, at.scale[n], quarter * 16 * SW), w);
 #pragma unroll
                 for (int i = 0; i < 4 * SW; ++i) out[4 * n + i / SW][i % SW] = w[i];
             }
         } else {
-            const uint8_t* base = static_cast<const uint8_t*>(scales);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) from_pointer<4 * SW>(base + shfl64(at.scale[0], token_of(k, quarter)) * (4 * SW), out[k]);
+            for (int k = 0; k < 8; ++k) load<4 * SW>(scales + shfl64(at.scale[0], token_of(k, quarter)), out[k]);
         }
     }
 }
 
-// (single tokens that are not seen: IN_PAGE, rows of the same page, which exist; else the pool's first row)
+// (Tokens that are not seen: IN_PAGE, rows of the same page or, of halves without a seen token, the first rows of page 0, which exist; else the first row of page 0.)
 template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_keys(const kvtc_cache& c, const Where<IN_PAGE>& at, Keys<F, D>& k) {
+__device__ __forceinline__ void load_keys(const Item& item, uint32_t ts, const Where<IN_PAGE>& at, Keys<F, D>& k) {
     using S = Shape<F, D>;
     if (at.seen == 0u) return;
     const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
@@ -265,38 +283,28 @@ __device__ __forceinline__ void load_keys(const kvtc_cache& c, const Where<IN_PA
     const uint32_t mine = quarter * kPiece;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-        if constexpr (IN_PAGE) {
-            const uint32_t ts = (uint32_t)c.token_stride;
-            const Rsrc r = half_at<IN_PAGE>(c.k_dev, at.row[n], 15u * ts + (uint32_t)cache_row_bytes(F, D), at.seen, n);
+        Bytes p;
+        if constexpr (IN_PAGE) p = lane_at(item.k, at.row[n], (uint32_t)row * ts + mine);
+        else p = item.k + shfl64(at.row[0], 16 * n + row) + mine;
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) from_buffer<kPiece>(r, (uint32_t)row * ts + mine + i * kStep, 0, &k.w[n][i * kPiece / 4]);
-        } else {
-            const uint8_t* p = static_cast<const uint8_t*>(c.k_dev) + shfl64(at.row[0], 16 * n + row) + mine;
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) from_pointer<kPiece>(p + i * kStep, &k.w[n][i * kPiece / 4]);
-        }
+        for (int i = 0; i < kPieces; ++i) load<kPiece>(p + i * kStep, &k.w[n][i * kPiece / 4]);
     }
-    load_scales<F, D, IN_PAGE>(c.k_scales_dev, at, quarter, k.scale);
+    load_scales<F, D, IN_PAGE>(item.k_scales, at, quarter, k.scale);
 }
 
 template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_values(const kvtc_cache& c, const Where<IN_PAGE>& at, Values<F, D>& v) {
+__device__ __forceinline__ void load_values(const Item& item, uint32_t ts, const Where<IN_PAGE>& at, Values<F, D>& v) {
     using S = Shape<F, D>;
     if (at.seen == 0u) return;
     const int lane = threadIdx.x & 63, mine = (lane & 15) * S::VB, quarter = lane >> 4;
-    if constexpr (IN_PAGE) {
-        const uint32_t ts = (uint32_t)c.token_stride;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const Rsrc r = half_at<IN_PAGE>(c.v_dev, at.row[n], 15u * ts + (uint32_t)cache_row_bytes(F, D), at.seen, n);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) from_buffer<S::VB>(r, (uint32_t)(4 * quarter) * ts + mine, (uint32_t)k * ts, v.w[4 * n + k]);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) from_pointer<S::VB>(static_cast<const uint8_t*>(c.v_dev) + shfl64(at.row[0], token_of(k, quarter)) + mine, v.w[k]);
+    for (int k = 0; k < 8; ++k) {
+        Bytes p;
+        if constexpr (IN_PAGE) p = lane_at(item.v, at.row[k / 4], (uint32_t)(4 * quarter + k % 4) * ts + mine);
+        else p = item.v + shfl64(at.row[0], token_of(k, quarter)) + mine;
+        load<S::VB>(p, v.w[k]);
     }
-    load_scales<F, D, IN_PAGE>(c.v_scales_dev, at, quarter, v.scale);
+    load_scales<F, D, IN_PAGE>(item.v_scales, at, quarter, v.scale);
     if (at.seen != 0xffffffffu) {                          // what is not seen counts for nothing, whatever it holds
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -351,9 +359,7 @@ __device__ __forceinline__ void load_query(const XT* q, bool is, Query<XT, F, D>
         }
         if constexpr (F == KVTC_CACHE_INT4) {
             float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-            sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
-            out.sum[s] = sum;
+            out.sum[s] = sum_over_quarters(sum);
             const float o[8] = {v[0], v[2], v[1], v[3], v[4], v[6], v[5], v[7]};          // the order in which codes come out of their bytes
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = o[i];
@@ -363,10 +369,10 @@ __device__ __forceinline__ void load_query(const XT* q, bool is, Query<XT, F, D>
 }
 
 // bf16 patterns of 128 + code: of the low (even features) and the high four bits of byte `at` of one and of another run of dwords
-__device__ __forceinline__ void nibbles(uint32_t first, uint32_t second, int at_first, int at_second, uint32_t& even, uint32_t& odd) {
+__device__ __forceinline__ void nibbles(uint32_t first, uint32_t second, int at_first, int at_second, const Constants& c, uint32_t& even, uint32_t& odd) {
     const uint32_t u = __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
-    even = (u & 0x000f000fu) | 0x43004300u;
-    odd = (u >> 4 & 0x000f000fu) | 0x43004300u;
+    even = (u & c.mask) | c.base;
+    odd = (u >> 4 & c.mask) | c.base;
 }
 // bf16 patterns of the codes themselves
 __device__ __forceinline__ void nibbles_exact(uint32_t first, uint32_t second, int at_first, int at_second, uint32_t& even, uint32_t& odd) {
@@ -381,7 +387,7 @@ __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) { return __builtin_
 
 // Scores (without the common factor) of the lane's query head and 8 tokens.
 template <typename XT, int F, int D>
-__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D>& k, float (&s)[8]) {
+__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D>& k, const Constants& k_of, float (&s)[8]) {
     constexpr int NK = D / 32, QP = Parts<XT>::q;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -391,10 +397,11 @@ __device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D
             for (int g = 0; g < NK; ++g) {
                 uint32_t w[4];
                 auto at = [&](int pair) { return pair * NK + g; };                        // byte of the lane's run
-                nibbles(k.w[n][at(0) / 4], k.w[n][at(1) / 4], at(0) % 4, at(1) % 4, w[0], w[1]);
-                nibbles(k.w[n][at(2) / 4], k.w[n][at(3) / 4], at(2) % 4, at(3) % 4, w[2], w[3]);
-                const float start = -128.0f * q.sum[g];
-                f32x4 c = {start, start, start, start};
+                nibbles(k.w[n][at(0) / 4], k.w[n][at(1) / 4], at(0) % 4, at(1) % 4, k_of, w[0], w[1]);
+                nibbles(k.w[n][at(2) / 4], k.w[n][at(3) / 4], at(2) % 4, at(3) % 4, k_of, w[2], w[3]);
+                f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = QP - 1; j >= 0; --j) c = mfma(operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u), q.w[g][j], c);      // -128 times the sum of the query
 #pragma unroll
                 for (int j = QP - 1; j >= 0; --j) c = mfma(operand(w[0], w[1], w[2], w[3]), q.w[g][j], c);
 #pragma unroll
@@ -441,7 +448,7 @@ __device__ __forceinline__ int feature_of(int i, int r, int quarter) {
 }
 
 template <typename XT, int F, int D>
-__device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<F, D>& v, float (&s)[8], uint32_t seen, float factor) {
+__device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<F, D>& v, float (&s)[8], uint32_t seen, float factor, const Constants& c) {
     constexpr int NO = D / 16, G = D / 32, P = Parts<XT>::p;
     constexpr bool kExact = sizeof(XT) == 4;               // fp32 results: codes without the 128 that bf16 results can bear in their sums
     const int quarter = (threadIdx.x & 63) >> 4;
@@ -452,8 +459,7 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
         for (int i = 0; i < 8; ++i) s[i] = seen >> token_of(i, quarter) & 1u ? s[i] : kNoScore;
     }
     float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    top = max_over_quarters(top);
     if (__any(top > run.m)) {
         const float now = fmaxf(top, run.m), keep = exp2_fast(run.m - (now == kNoScore ? 0.0f : now));
         run.l *= keep;
@@ -477,20 +483,24 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t header = v.scale[i][g];
-                ps[i] = p[i] * half_of(header, 1);
+                ps[i] = __builtin_fmaf(half_of(header, 1), p[i], c.zero);
                 run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
             }
-            if constexpr (!kExact) run.low[g] = __builtin_fmaf(-128.0f, ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7])), run.low[g]);
             bf16x8 b[P];
             split<P, false>(ps, b);
             uint32_t even[4], odd[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (kExact) nibbles_exact(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, even[i], odd[i]);
-                else nibbles(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, even[i], odd[i]);
+                else nibbles(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, c, even[i], odd[i]);
             }
 #pragma unroll
             for (int j = P - 1; j >= 0; --j) {
+                if constexpr (!kExact) {                   // the 128s of the codes, taken off first
+                    const bf16x8 less = operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u);
+                    run.o[2 * g] = mfma(less, b[j], run.o[2 * g]);
+                    run.o[2 * g + 1] = mfma(less, b[j], run.o[2 * g + 1]);
+                }
                 run.o[2 * g] = mfma(operand(even[0], even[1], even[2], even[3]), b[j], run.o[2 * g]);
                 run.o[2 * g + 1] = mfma(operand(odd[0], odd[1], odd[2], odd[3]), b[j], run.o[2 * g + 1]);
             }
@@ -535,16 +545,15 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 
 // The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles, a piece to each of WAVES waves.  (At least one: every
 // row has a result.)
-struct Tiles { uint32_t n, pieces, sinks, window0; int64_t length, from; };
+struct Tiles { uint32_t n, pieces, sinks, window0, length, from; };
 template <int WAVES>
-__device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int64_t length) {
-    if (length < 0 || length > a.max_tokens) length = 0;
+__device__ __forceinline__ Tiles tiles_of(const AttendPlan& p, int32_t length) {
     Tiles t;
-    t.length = length;
-    t.from = a.window && length > a.window ? length - a.window : 0;
-    const uint32_t all = (uint32_t)((length + 31) / 32);
-    t.sinks = a.window ? (uint32_t)((a.sinks < length ? a.sinks : length) + 31) / 32 : 0u;
-    t.window0 = max(t.sinks, (uint32_t)(t.from / 32));
+    t.length = (uint32_t)length <= p.max_tokens ? (uint32_t)length : 0u;
+    t.from = p.window && t.length > p.window ? t.length - p.window : 0u;
+    const uint32_t all = (t.length + 31) / 32;
+    t.sinks = p.window ? (min(p.sinks, t.length) + 31) / 32 : 0u;
+    t.window0 = max(t.sinks, t.from / 32);
     t.pieces = t.sinks + (all > t.window0 ? all - t.window0 : 0u);
     t.n = max(1u, (t.pieces + WAVES - 1) / WAVES);
     return t;
@@ -707,9 +716,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     uint32_t mine = 0;
     const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
     for (int b = first; b < last; ++b) {
-        const int64_t length = a.lengths[b];
-        if (me == 0 && (length < 0 || length > a.max_tokens)) report_lowest(a.status, (uint32_t)b);
-        mine += tiles_of<WAVES>(a, length).n;
+        const int32_t length = a.lengths[b];
+        if (me == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
+        mine += tiles_of<WAVES>(p, length).n;
     }
     const uint32_t upto = wave_inclusive_scan(mine);
     const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
@@ -723,12 +732,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
     int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
     uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
-    Tiles t = tiles_of<WAVES>(a, scalar_at(a.lengths, b));
+    Tiles t = tiles_of<WAVES>(p, scalar_at(a.lengths, b));
     while (share0 >= seq0 + (uint64_t)t.n * heads) {
         seq0 += (uint64_t)t.n * heads;
-        t = tiles_of<WAVES>(a, scalar_at(a.lengths, ++b));
+        t = tiles_of<WAVES>(p, scalar_at(a.lengths, ++b));
     }
     uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
+    const Constants known = constants();
     const float factor = a.scale * 1.44269504088896340736f;
 
     uint64_t at = share0;
@@ -741,7 +751,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         if (item == heads) {
             item = 0;
             seq0 += (uint64_t)t.n * heads;
-            t = tiles_of<WAVES>(a, scalar_at(a.lengths, ++b));
+            t = tiles_of<WAVES>(p, scalar_at(a.lengths, ++b));
         }
         const uint32_t tile1 = WAVES > 1 ? (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at)) : t.n;
         const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
@@ -749,10 +759,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
 
         Query<XT, F, D> q;
         load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (col < cols ? col : 0)) * a.q_head_stride, col < cols, q);
-        const int32_t* table = a.pages + (int64_t)b * a.pages_stride;
+        const int64_t scale_head = (int64_t)h * a.c.page_tokens * (4 * Shape<F, D>::SW);
+        const int64_t row_head = (int64_t)h * a.c.head_stride;
+        const Item of{a.pages + (int64_t)b * a.pages_stride, bytes_at(a.c.k_dev) + row_head, bytes_at(a.c.v_dev) + row_head, bytes_at(a.c.k_scales_dev) + scale_head, bytes_at(a.c.v_scales_dev) + scale_head,
+                      t.length, t.from, p.window ? p.sinks : 0u, (uint32_t)b};
+        const uint32_t ts = (uint32_t)a.c.token_stride;
         auto look = [&](uint32_t i) {
             const uint32_t k = WAVES > 1 ? WAVES * i + wave : i, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
-            return look_at<IN_PAGE>(p, table, i < tile1 && k < t.pieces ? (int64_t)piece * 32 : t.length, t.length, t.from);
+            return look_at<IN_PAGE>(p, of, i < tile1 && k < t.pieces ? piece * 32 : t.length);
         };
         Running<XT, F, D> run;
 #pragma unroll
@@ -765,29 +779,25 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         Keys<F, D> keys;
         Values<F, D> values;
         Look<IN_PAGE> ahead = look(tile0);
-        Where<IN_PAGE> now = where<IN_PAGE>(p, b, h, ahead);
+        Where<IN_PAGE> now = where<Shape<F, D>::SW, IN_PAGE>(p, of, ahead);
         ahead = look(tile0 + 1);
-        load_keys<F, D, IN_PAGE>(a.c, now, keys);
-        load_values<F, D, IN_PAGE>(a.c, now, values);
+        load_keys<F, D, IN_PAGE>(of, ts, now, keys);
+        load_values<F, D, IN_PAGE>(of, ts, now, values);
         for (uint32_t i = tile0; i < tile1; ++i) {
-            const Where<IN_PAGE> next = where<IN_PAGE>(p, b, h, ahead);
+            const Where<IN_PAGE> next = where<Shape<F, D>::SW, IN_PAGE>(p, of, ahead);
             ahead = look(i + 2);
             float s[8];
-            if (now.seen != 0u) scores<XT, F, D>(q, keys, s);
-            load_keys<F, D, IN_PAGE>(a.c, next, keys);
-            if (now.seen != 0u) add_tokens<XT, F, D>(run, values, s, now.seen, factor);
-            load_values<F, D, IN_PAGE>(a.c, next, values);
+            if (now.seen != 0u) scores<XT, F, D>(q, keys, known, s);
+            load_keys<F, D, IN_PAGE>(of, ts, next, keys);
+            if (now.seen != 0u) add_tokens<XT, F, D>(run, values, s, now.seen, factor, known);
+            load_values<F, D, IN_PAGE>(of, ts, next, values);
             now = next;
         }
 
-        run.l += __shfl_xor(run.l, 16, 64);
-        run.l += __shfl_xor(run.l, 32, 64);
+        run.l = sum_over_quarters(run.l);
         if constexpr (F == KVTC_CACHE_INT4) {
 #pragma unroll
-            for (int g = 0; g < D / 32; ++g) {
-                run.low[g] += __shfl_xor(run.low[g], 16, 64);
-                run.low[g] += __shfl_xor(run.low[g], 32, 64);
-            }
+            for (int g = 0; g < D / 32; ++g) run.low[g] = sum_over_quarters(run.low[g]);
         }
         const int64_t row0 = (int64_t)b * a.n_q_heads + col0;
         if constexpr (WAVES == 1) {
@@ -943,6 +953,11 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     p.cols = cols;
     p.in_page = a.c.page_tokens % 16 == 0;
     p.seqs_each = (a.n_seqs + 63) / 64;
+    auto in_31 = [](int64_t v) { return (uint32_t)(v < 0x7fffffffLL ? v : 0x7fffffffLL); };
+    p.max_tokens = in_31(a.max_tokens);
+    p.sinks = in_31(a.sinks);
+    p.window = in_31(a.window);
+    p.scale_stride = (int64_t)a.c.n_heads * a.c.page_tokens * cache_scale_bytes(a.c.format, a.c.d_head);
     uint32_t s = 0;                                        // (n < 2^31: m = ceil(2^(31 + s) / d) is near enough)
     while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
     p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);
