@@ -148,10 +148,10 @@ struct Item {
 };
 // A place that is the same in all lanes, in scalar registers, and 32 bits of the lane's own.  (The compiler left to itself keeps these as 64 bits, and adds them up for every load.)
 __device__ __forceinline__ Bytes lane_at(Bytes base, int64_t offset, uint32_t lane) {
-    uint64_t p = reinterpret_cast<uint64_t>(base + offset);
-    asm("" : "+s"(p));
+    const uint64_t p = reinterpret_cast<uint64_t>(base + offset);
+    const uint64_t q = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
     asm volatile("" : "+v"(lane));
-    return reinterpret_cast<Bytes>(p) + lane;
+    return reinterpret_cast<Bytes>(q) + lane;
 }
 // Where a wave's 32 tokens are, and which of them are seen.
 template <bool IN_PAGE>
@@ -239,82 +239,97 @@ struct Shape {
     static constexpr int NO = D / 16;                                          // products for the features
 };
 
-// A lane's part of the keys of tokens lane % 16 and 16 + lane % 16, and the scales of its 8 tokens' scores.
-template <int F, int D>
+// A lane's parts of J pieces of 32 tokens.  Of a row's 16 columns a group of few query heads fills few, and what the vector unit does to scores and probabilities it does to
+// all: with J > 1 the columns come in J sets of 16 / J, each with all the heads, and a set keeps the scores of its own piece only.  Then a lane has its 8 tokens' scales of
+// one piece, the softmax is worked out once for 32 J tokens, and each set has its own maximum and sums, joined at the end like those of waves.
+// Keys: of tokens lane % 16 and 16 + lane % 16 of each piece, and the scales of the lane's 8 tokens.
+template <int F, int D, int J>
 struct Keys {
     using S = Shape<F, D>;
-    uint32_t w[2][S::KW], scale[8][S::SW > 0 ? S::SW : 1];
+    uint32_t w[J][2][S::KW], scale[8][S::SW > 0 ? S::SW : 1];
 };
-template <int F, int D>
+template <int F, int D, int J>
 struct Values {
     using S = Shape<F, D>;
-    uint32_t w[8][S::VW], scale[8][S::SW > 0 ? S::SW : 1];
+    uint32_t w[J][8][S::VW], scale[8][S::SW > 0 ? S::SW : 1];
 };
+// the set of a column
+template <int J> __device__ __forceinline__ int set_of(int col) { return col / (kAttendCols / J); }
+template <int J, bool IN_PAGE>
+__device__ __forceinline__ uint32_t any_seen(const Where<IN_PAGE> (&at)[J]) {
+    uint32_t seen = 0u;
+#pragma unroll
+    for (int j = 0; j < J; ++j) seen |= at[j].seen;
+    return seen;
+}
 
 // the k-th of the lane's 8 tokens, among the wave's 32
 __device__ __forceinline__ int token_of(int k, int quarter) { return (k < 4 ? k : 12 + k) + 4 * quarter; }
 
-template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_scales(Bytes scales, const Where<IN_PAGE>& at, int quarter, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
+template <int F, int D, bool IN_PAGE, int J>
+__device__ __forceinline__ void load_scales(Bytes scales, const Where<IN_PAGE> (&at)[J], int lane, uint32_t (&out)[8][Shape<F, D>::SW > 0 ? Shape<F, D>::SW : 1]) {
     constexpr int SW = Shape<F, D>::SW;
+    const int quarter = lane >> 4;
     if constexpr (SW > 0) {
         if constexpr (IN_PAGE) {                           // the four tokens' scales lie side by side
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 uint32_t w[4 * SW];
-                load<16 * SW>(lane_at(scales, at.scale[n], quarter * 16 * SW), w);
+                if constexpr (J == 1) {
+                    load<16 * SW>(lane_at(scales, at[0].scale[n], quarter * 16 * SW), w);
+                } else {
+                    int64_t mine = at[0].scale[n];
+#pragma unroll
+                    for (int j = 1; j < J; ++j) mine = set_of<J>(lane & 15) == j ? at[j].scale[n] : mine;
+                    load<16 * SW>(scales + mine + quarter * 16 * SW, w);
+                }
 #pragma unroll
                 for (int i = 0; i < 4 * SW; ++i) out[4 * n + i / SW][i % SW] = w[i];
             }
         } else {
+            static_assert(IN_PAGE || J == 1, "");
 #pragma unroll
-            for (int k = 0; k < 8; ++k) load<4 * SW>(scales + shfl64(at.scale[0], token_of(k, quarter)), out[k]);
+            for (int k = 0; k < 8; ++k) load<4 * SW>(scales + shfl64(at[0].scale[0], token_of(k, quarter)), out[k]);
         }
     }
 }
 
 // (Tokens that are not seen: IN_PAGE, rows of the same page or, of halves without a seen token, the first rows of page 0, which exist; else the first row of page 0.)
-template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_keys(const Item& item, uint32_t ts, const Where<IN_PAGE>& at, Keys<F, D>& k) {
+template <int F, int D, bool IN_PAGE, int J>
+__device__ __forceinline__ void load_keys(const Item& item, uint32_t ts, const Where<IN_PAGE> (&at)[J], Keys<F, D, J>& k) {
     using S = Shape<F, D>;
-    if (at.seen == 0u) return;
+    if (any_seen(at) == 0u) return;
     const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
     constexpr int kPiece = F == KVTC_CACHE_INT4 ? 4 * S::KW : 16, kPieces = 4 * S::KW / kPiece, kStep = F == KVTC_CACHE_INT4 ? 0 : 64;
     const uint32_t mine = quarter * kPiece;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        Bytes p;
-        if constexpr (IN_PAGE) p = lane_at(item.k, at.row[n], (uint32_t)row * ts + mine);
-        else p = item.k + shfl64(at.row[0], 16 * n + row) + mine;
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) load<kPiece>(p + i * kStep, &k.w[n][i * kPiece / 4]);
-    }
-    load_scales<F, D, IN_PAGE>(item.k_scales, at, quarter, k.scale);
+        for (int n = 0; n < 2; ++n) {
+            Bytes p;
+            if constexpr (IN_PAGE) p = lane_at(item.k, at[j].row[n], (uint32_t)row * ts + mine);
+            else p = item.k + shfl64(at[j].row[0], 16 * n + row) + mine;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) load<kPiece>(p + i * kStep, &k.w[j][n][i * kPiece / 4]);
+        }
+    load_scales<F, D, IN_PAGE, J>(item.k_scales, at, lane, k.scale);
 }
 
-template <int F, int D, bool IN_PAGE>
-__device__ __forceinline__ void load_values(const Item& item, uint32_t ts, const Where<IN_PAGE>& at, Values<F, D>& v) {
+template <int F, int D, bool IN_PAGE, int J>
+__device__ __forceinline__ void load_values(const Item& item, uint32_t ts, const Where<IN_PAGE> (&at)[J], Values<F, D, J>& v) {
     using S = Shape<F, D>;
-    if (at.seen == 0u) return;
+    if (any_seen(at) == 0u) return;
     const int lane = threadIdx.x & 63, mine = (lane & 15) * S::VB, quarter = lane >> 4;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        Bytes p;
-        if constexpr (IN_PAGE) p = lane_at(item.v, at.row[k / 4], (uint32_t)(4 * quarter + k % 4) * ts + mine);
-        else p = item.v + shfl64(at.row[0], token_of(k, quarter)) + mine;
-        load<S::VB>(p, v.w[k]);
-    }
-    load_scales<F, D, IN_PAGE>(item.v_scales, at, quarter, v.scale);
-    if (at.seen != 0xffffffffu) {                          // what is not seen counts for nothing, whatever it holds
+    for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const bool is = at.seen >> token_of(k, quarter) & 1u;
-#pragma unroll
-            for (int i = 0; i < S::VW; ++i) v.w[k][i] = is ? v.w[k][i] : 0u;
-#pragma unroll
-            for (int i = 0; i < S::SW; ++i) v.scale[k][i] = is ? v.scale[k][i] : 0u;
+            Bytes p;
+            if constexpr (IN_PAGE) p = lane_at(item.v, at[j].row[k / 4], (uint32_t)(4 * quarter + k % 4) * ts + mine);
+            else p = item.v + shfl64(at[j].row[0], token_of(k, quarter)) + mine;
+            load<S::VB>(p, v.w[j][k]);
         }
-    }
+    load_scales<F, D, IN_PAGE, J>(item.v_scales, at, lane, v.scale);
 }
 
 // ---- queries and scores --------------------------------------------------------------------------------------------------------
@@ -385,39 +400,58 @@ __device__ __forceinline__ void nibbles_exact(uint32_t first, uint32_t second, i
 template <bool HIGH>
 __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH)); }
 
-// Scores (without the common factor) of the lane's query head and 8 tokens.
-template <typename XT, int F, int D>
-__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D>& k, const Constants& k_of, float (&s)[8]) {
+// Scores (without the common factor) of the lane's query head and 8 tokens of its set's piece.
+template <typename XT, int F, int D, int J>
+__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D, J>& k, const Constants& known, float (&s)[8]) {
     constexpr int NK = D / 32, QP = Parts<XT>::q;
+    const int set = set_of<J>(threadIdx.x & 15);
+    auto own = [&](int j, f32x4& kept, const f32x4& now) { // the set's own piece among J products
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kept[i] = j == 0 || set == j ? now[i] : kept[i];
+    };
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (F == KVTC_CACHE_INT4) {
 #pragma unroll
             for (int g = 0; g < NK; ++g) {
-                uint32_t w[4];
-                auto at = [&](int pair) { return pair * NK + g; };                        // byte of the lane's run
-                nibbles(k.w[n][at(0) / 4], k.w[n][at(1) / 4], at(0) % 4, at(1) % 4, k_of, w[0], w[1]);
-                nibbles(k.w[n][at(2) / 4], k.w[n][at(3) / 4], at(2) % 4, at(3) % 4, k_of, w[2], w[3]);
-                f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+                f32x4 c;
 #pragma unroll
-                for (int j = QP - 1; j >= 0; --j) c = mfma(operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u), q.w[g][j], c);      // -128 times the sum of the query
+                for (int j = 0; j < J; ++j) {
+                    uint32_t w[4];
+                    auto at = [&](int pair) { return pair * NK + g; };                    // byte of the lane's run
+                    nibbles(k.w[j][n][at(0) / 4], k.w[j][n][at(1) / 4], at(0) % 4, at(1) % 4, known, w[0], w[1]);
+                    nibbles(k.w[j][n][at(2) / 4], k.w[j][n][at(3) / 4], at(2) % 4, at(3) % 4, known, w[2], w[3]);
+                    f32x4 now = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if constexpr (J == 1) {                // -128 times the sum of the query
 #pragma unroll
-                for (int j = QP - 1; j >= 0; --j) c = mfma(operand(w[0], w[1], w[2], w[3]), q.w[g][j], c);
+                        for (int i = QP - 1; i >= 0; --i) now = mfma(operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u), q.w[g][i], now);
+                    }
+#pragma unroll
+                    for (int i = QP - 1; i >= 0; --i) now = mfma(operand(w[0], w[1], w[2], w[3]), q.w[g][i], now);
+                    own(j, c, now);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t header = k.scale[4 * n + i][g];
-                    sum[i] = __builtin_fmaf(half_of(header, 1), c[i], __builtin_fmaf(half_of(header, 0), q.sum[g], sum[i]));
+                    const float codes = J == 1 ? c[i] : __builtin_fmaf(-128.0f, q.sum[g], c[i]);
+                    sum[i] = __builtin_fmaf(half_of(header, 1), codes, __builtin_fmaf(half_of(header, 0), q.sum[g], sum[i]));
                 }
             }
         } else {
 #pragma unroll
-            for (int t = 0; t < NK; ++t) {
-                bf16x8 a;
-                if constexpr (F == KVTC_CACHE_BF16) a = operand(k.w[n][4 * t], k.w[n][4 * t + 1], k.w[n][4 * t + 2], k.w[n][4 * t + 3]);
-                else a = operand(e4m3_to_bf16<false>(k.w[n][2 * t]), e4m3_to_bf16<true>(k.w[n][2 * t]), e4m3_to_bf16<false>(k.w[n][2 * t + 1]), e4m3_to_bf16<true>(k.w[n][2 * t + 1]));
+            for (int j = 0; j < J; ++j) {
+                f32x4 now = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int j = QP - 1; j >= 0; --j) sum = mfma(a, q.w[t][j], sum);
+                for (int t = 0; t < NK; ++t) {
+                    const uint32_t* w = k.w[j][n];
+                    bf16x8 a;
+                    if constexpr (F == KVTC_CACHE_BF16) a = operand(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
+                    else a = operand(e4m3_to_bf16<false>(w[2 * t]), e4m3_to_bf16<true>(w[2 * t]), e4m3_to_bf16<false>(w[2 * t + 1]), e4m3_to_bf16<true>(w[2 * t + 1]));
+#pragma unroll
+                    for (int i = QP - 1; i >= 0; --i) now = mfma(a, q.w[t][i], now);
+                }
+                own(j, sum, now);
             }
             if constexpr (F == KVTC_CACHE_FP8) {
 #pragma unroll
@@ -437,7 +471,7 @@ struct Running {
     static constexpr int NO = D / 16, G = D / 32;
     f32x4 o[NO];
     float m, l;
-    float low[F == KVTC_CACHE_INT4 ? G : 1];               // 4 bits: of p * shift (and the 128s), per group
+    float low[F == KVTC_CACHE_INT4 ? G : 1];               // 4 bits: of p * shift, per group
 };
 
 // the feature of o[i][r]
@@ -447,17 +481,40 @@ __device__ __forceinline__ int feature_of(int i, int r, int quarter) {
     return F == KVTC_CACHE_INT4 ? i / 2 * 32 + 2 * c + i % 2 : c * (D / 16) + i;
 }
 
-template <typename XT, int F, int D>
-__device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<F, D>& v, float (&s)[8], uint32_t seen, float factor, const Constants& c) {
+template <typename XT, int F, int D, bool IN_PAGE, int J>
+__device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, J>& v, float (&s)[8], const Where<IN_PAGE> (&at)[J], float factor, const Constants& known) {
     constexpr int NO = D / 16, G = D / 32, P = Parts<XT>::p;
     constexpr bool kExact = sizeof(XT) == 4;               // fp32 results: codes without the 128 that bf16 results can bear in their sums
-    const int quarter = (threadIdx.x & 63) >> 4;
+    const int quarter = (threadIdx.x & 63) >> 4, set = set_of<J>(threadIdx.x & 15);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] *= factor;
-    if (seen != 0xffffffffu) {
+    uint32_t all = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = seen >> token_of(i, quarter) & 1u ? s[i] : kNoScore;
+    for (int j = 0; j < J; ++j) all &= at[j].seen;
+    if (all != 0xffffffffu) {                              // what is not seen counts for nothing, whatever it holds
+        uint32_t mine = at[0].seen;
+#pragma unroll
+        for (int j = 1; j < J; ++j) mine = set == j ? at[j].seen : mine;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool is = mine >> token_of(k, quarter) & 1u;
+            s[k] = is ? s[k] : kNoScore;
+#pragma unroll
+            for (int i = 0; i < Shape<F, D>::SW; ++i) v.scale[k][i] = is ? v.scale[k][i] : 0u;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < Shape<F, D>::VW; ++i) v.w[j][k][i] = at[j].seen >> token_of(k, quarter) & 1u ? v.w[j][k][i] : 0u;
+        }
     }
+    // a set's probabilities go with its own piece's values only
+    auto own = [&](int j, const bf16x8& b) {
+        if constexpr (J == 1) return b;
+        u32x4 w = __builtin_bit_cast(u32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = set == j ? w[i] : 0u;
+        return __builtin_bit_cast(bf16x8, w);
+    };
     float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     top = max_over_quarters(top);
     if (__any(top > run.m)) {
@@ -483,26 +540,34 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t header = v.scale[i][g];
-                ps[i] = __builtin_fmaf(half_of(header, 1), p[i], c.zero);
+                ps[i] = __builtin_fmaf(half_of(header, 1), p[i], known.zero);
                 run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
             }
             bf16x8 b[P];
             split<P, false>(ps, b);
-            uint32_t even[4], odd[4];
+            if constexpr (!kExact) {                       // the 128s of the codes, taken off first
+                const bf16x8 less = operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (kExact) nibbles_exact(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, even[i], odd[i]);
-                else nibbles(v.w[2 * i][g / 4], v.w[2 * i + 1][g / 4], g % 4, g % 4, c, even[i], odd[i]);
+                for (int i = P - 1; i >= 0; --i) {
+                    run.o[2 * g] = mfma(less, b[i], run.o[2 * g]);
+                    run.o[2 * g + 1] = mfma(less, b[i], run.o[2 * g + 1]);
+                }
             }
 #pragma unroll
-            for (int j = P - 1; j >= 0; --j) {
-                if constexpr (!kExact) {                   // the 128s of the codes, taken off first
-                    const bf16x8 less = operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u);
-                    run.o[2 * g] = mfma(less, b[j], run.o[2 * g]);
-                    run.o[2 * g + 1] = mfma(less, b[j], run.o[2 * g + 1]);
+            for (int j = 0; j < J; ++j) {
+                uint32_t even[4], odd[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t first = v.w[j][2 * i][g / 4], second = v.w[j][2 * i + 1][g / 4];
+                    if constexpr (kExact) nibbles_exact(first, second, g % 4, g % 4, even[i], odd[i]);
+                    else nibbles(first, second, g % 4, g % 4, known, even[i], odd[i]);
                 }
-                run.o[2 * g] = mfma(operand(even[0], even[1], even[2], even[3]), b[j], run.o[2 * g]);
-                run.o[2 * g + 1] = mfma(operand(odd[0], odd[1], odd[2], odd[3]), b[j], run.o[2 * g + 1]);
+#pragma unroll
+                for (int i = P - 1; i >= 0; --i) {
+                    const bf16x8 mine = own(j, b[i]);
+                    run.o[2 * g] = mfma(operand(even[0], even[1], even[2], even[3]), mine, run.o[2 * g]);
+                    run.o[2 * g + 1] = mfma(operand(odd[0], odd[1], odd[2], odd[3]), mine, run.o[2 * g + 1]);
+                }
             }
         }
     } else {
@@ -510,31 +575,36 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] *= __uint_as_float(v.scale[i][0]);
         }
-        bf16x8 b[P];
-        split<P, F == KVTC_CACHE_BF16>(p, b);
-        if constexpr (F == KVTC_CACHE_BF16) {
+        bf16x8 all_sets[P], b[P];
+        split<P, F == KVTC_CACHE_BF16>(p, all_sets);
 #pragma unroll
-            for (int i = 0; i < NO; ++i) {
-                uint32_t w[4];
+        for (int j = 0; j < J; ++j) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = i % 2 ? high_halves(v.w[2 * j][i / 2], v.w[2 * j + 1][i / 2]) : low_halves(v.w[2 * j][i / 2], v.w[2 * j + 1][i / 2]);
+            for (int i = 0; i < P; ++i) b[i] = own(j, all_sets[i]);
+            if constexpr (F == KVTC_CACHE_BF16) {
 #pragma unroll
-                for (int j = P - 1; j >= 0; --j) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[j], run.o[i]);
-            }
-        } else {
+                for (int i = 0; i < NO; ++i) {
+                    uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < NO; i += 2) {
-                uint32_t w[4], x[4];
+                    for (int k = 0; k < 4; ++k) w[k] = i % 2 ? high_halves(v.w[j][2 * k][i / 2], v.w[j][2 * k + 1][i / 2]) : low_halves(v.w[j][2 * k][i / 2], v.w[j][2 * k + 1][i / 2]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {                                 // features i and i + 1 of two tokens: [i, i, i + 1, i + 1]
-                    const uint32_t at = (uint32_t)(i % 4), u = __builtin_amdgcn_perm(v.w[2 * j + 1][i / 4], v.w[2 * j][i / 4], at | (at + 4) << 8 | (at + 1) << 16 | (at + 5) << 24);
-                    w[j] = e4m3_to_bf16<false>(u);
-                    x[j] = e4m3_to_bf16<true>(u);
+                    for (int k = P - 1; k >= 0; --k) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
                 }
+            } else {
 #pragma unroll
-                for (int j = P - 1; j >= 0; --j) {
-                    run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[j], run.o[i]);
-                    run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[j], run.o[i + 1]);
+                for (int i = 0; i < NO; i += 2) {
+                    uint32_t w[4], x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {                             // features i and i + 1 of two tokens: [i, i, i + 1, i + 1]
+                        const uint32_t from = (uint32_t)(i % 4), u = __builtin_amdgcn_perm(v.w[j][2 * k + 1][i / 4], v.w[j][2 * k][i / 4], from | (from + 4) << 8 | (from + 1) << 16 | (from + 5) << 24);
+                        w[k] = e4m3_to_bf16<false>(u);
+                        x[k] = e4m3_to_bf16<true>(u);
+                    }
+#pragma unroll
+                    for (int k = P - 1; k >= 0; --k) {
+                        run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
+                        run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[k], run.o[i + 1]);
+                    }
                 }
             }
         }
@@ -543,10 +613,10 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, const Values<
 
 // ---- the shares ----------------------------------------------------------------------------------------------------------------
 
-// The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles, a piece to each of WAVES waves.  (At least one: every
+// The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles of PIECES of them.  (At least one: every
 // row has a result.)
 struct Tiles { uint32_t n, pieces, sinks, window0, length, from; };
-template <int WAVES>
+template <int PIECES>
 __device__ __forceinline__ Tiles tiles_of(const AttendPlan& p, int32_t length) {
     Tiles t;
     t.length = (uint32_t)length <= p.max_tokens ? (uint32_t)length : 0u;
@@ -555,7 +625,7 @@ __device__ __forceinline__ Tiles tiles_of(const AttendPlan& p, int32_t length) {
     t.sinks = p.window ? (min(p.sinks, t.length) + 31) / 32 : 0u;
     t.window0 = max(t.sinks, t.from / 32);
     t.pieces = t.sinks + (all > t.window0 ? all - t.window0 : 0u);
-    t.n = max(1u, (t.pieces + WAVES - 1) / WAVES);
+    t.n = max(1u, (t.pieces + PIECES - 1) / PIECES);
     return t;
 }
 
@@ -702,9 +772,9 @@ __device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
     for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(x + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
-// WAVES = 4: the waves of a workgroup take a piece each of the same tile, and their results are joined in the LDS.  WAVES = 1, for many short rows: every wave has a
+// WAVES = 4: the waves of a workgroup take J pieces each of the same tile, and their results are joined in the LDS.  WAVES = 1, for many short rows: every wave has a
 // share of its own, of whole items (those whose first piece falls into it), and nothing is joined.
-template <typename XT, int F, int D, bool IN_PAGE, int WAVES>
+template <typename XT, int F, int D, bool IN_PAGE, int WAVES, int J>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
     const AttendArgs& a = p.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
@@ -712,17 +782,22 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     __shared__ uint32_t s_last;
 
     // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
-    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = WAVES > 1 ? blockIdx.x : blockIdx.x * 4 + wave, most = WAVES > 1 ? gridDim.x : gridDim.x * 4;
+    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, most = WAVES > 1 ? gridDim.x : gridDim.x * 4;
     uint32_t mine = 0;
     const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
     for (int b = first; b < last; ++b) {
         const int32_t length = a.lengths[b];
-        if (me == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
-        mine += tiles_of<WAVES>(p, length).n;
+        if (blockIdx.x == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
+        mine += tiles_of<WAVES * J>(p, length).n;
     }
     const uint32_t upto = wave_inclusive_scan(mine);
     const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
     const uint32_t groups = all < most ? (uint32_t)all : most;       // (no share is empty: each of an item's workgroups is waited for)
+    // Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares, the heads of a sequence one after another, so that where several heads' rows are in one cache line its
+    // L2 has it for all of them (4 bits, token-major, 128 features: 64 bytes; 16 rows of 32768 tokens with the shares in turn 193 us).
+    const uint32_t blocks = WAVES > 1 ? groups : (groups + 3) / 4, block = blockIdx.x;
+    if (block >= blocks) return;
+    const uint32_t turn = (block & 7u) * (blocks / 8) + min(block & 7u, blocks % 8) + block / 8, me = WAVES > 1 ? turn : turn * 4 + wave;
     if (me >= groups) return;
     // me * all / groups, by the quotient and the remainder of all / groups
     const uint64_t each = quotient(all, groups);
@@ -732,10 +807,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
     int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
     uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
-    Tiles t = tiles_of<WAVES>(p, scalar_at(a.lengths, b));
+    Tiles t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, b));
     while (share0 >= seq0 + (uint64_t)t.n * heads) {
         seq0 += (uint64_t)t.n * heads;
-        t = tiles_of<WAVES>(p, scalar_at(a.lengths, ++b));
+        t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, ++b));
     }
     uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
     const Constants known = constants();
@@ -751,22 +826,31 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
         if (item == heads) {
             item = 0;
             seq0 += (uint64_t)t.n * heads;
-            t = tiles_of<WAVES>(p, scalar_at(a.lengths, ++b));
+            t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, ++b));
         }
         const uint32_t tile1 = WAVES > 1 ? (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at)) : t.n;
         const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
         const int col0 = h * p.group + part * p.cols, cols = min(p.cols, p.group - part * p.cols);
 
+        constexpr int kSet = kAttendCols / J;
+        const int mine = col % kSet;                       // the head of the lane's column
         Query<XT, F, D> q;
-        load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (col < cols ? col : 0)) * a.q_head_stride, col < cols, q);
+        load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (mine < cols ? mine : 0)) * a.q_head_stride, mine < cols, q);
         const int64_t scale_head = (int64_t)h * a.c.page_tokens * (4 * Shape<F, D>::SW);
         const int64_t row_head = (int64_t)h * a.c.head_stride;
         const Item of{a.pages + (int64_t)b * a.pages_stride, bytes_at(a.c.k_dev) + row_head, bytes_at(a.c.v_dev) + row_head, bytes_at(a.c.k_scales_dev) + scale_head, bytes_at(a.c.v_scales_dev) + scale_head,
                       t.length, t.from, p.window ? p.sinks : 0u, (uint32_t)b};
         const uint32_t ts = (uint32_t)a.c.token_stride;
-        auto look = [&](uint32_t i) {
-            const uint32_t k = WAVES > 1 ? WAVES * i + wave : i, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
-            return look_at<IN_PAGE>(p, of, i < tile1 && k < t.pieces ? piece * 32 : t.length);
+        auto look = [&](uint32_t i, Look<IN_PAGE> (&l)[J]) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const uint32_t k = (WAVES > 1 ? WAVES * i + wave : i) * J + j, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
+                l[j] = look_at<IN_PAGE>(p, of, i < tile1 && k < t.pieces ? piece * 32 : t.length);
+            }
+        };
+        auto places = [&](const Look<IN_PAGE> (&l)[J], Where<IN_PAGE> (&w)[J]) {
+#pragma unroll
+            for (int j = 0; j < J; ++j) w[j] = where<Shape<F, D>::SW, IN_PAGE>(p, of, l[j]);
         };
         Running<XT, F, D> run;
 #pragma unroll
@@ -776,22 +860,26 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
 #pragma unroll
         for (int g = 0; g < (F == KVTC_CACHE_INT4 ? D / 32 : 1); ++g) run.low[g] = 0.0f;
 
-        Keys<F, D> keys;
-        Values<F, D> values;
-        Look<IN_PAGE> ahead = look(tile0);
-        Where<IN_PAGE> now = where<Shape<F, D>::SW, IN_PAGE>(p, of, ahead);
-        ahead = look(tile0 + 1);
-        load_keys<F, D, IN_PAGE>(of, ts, now, keys);
-        load_values<F, D, IN_PAGE>(of, ts, now, values);
+        Keys<F, D, J> keys;
+        Values<F, D, J> values;
+        Look<IN_PAGE> ahead[J];
+        Where<IN_PAGE> now[J], next[J];
+        look(tile0, ahead);
+        places(ahead, now);
+        look(tile0 + 1, ahead);
+        load_keys<F, D, IN_PAGE, J>(of, ts, now, keys);
+        load_values<F, D, IN_PAGE, J>(of, ts, now, values);
         for (uint32_t i = tile0; i < tile1; ++i) {
-            const Where<IN_PAGE> next = where<Shape<F, D>::SW, IN_PAGE>(p, of, ahead);
-            ahead = look(i + 2);
+            places(ahead, next);
+            look(i + 2, ahead);
             float s[8];
-            if (now.seen != 0u) scores<XT, F, D>(q, keys, known, s);
-            load_keys<F, D, IN_PAGE>(of, ts, next, keys);
-            if (now.seen != 0u) add_tokens<XT, F, D>(run, values, s, now.seen, factor, known);
-            load_values<F, D, IN_PAGE>(of, ts, next, values);
-            now = next;
+            const bool some = any_seen(now) != 0u;
+            if (some) scores<XT, F, D, J>(q, keys, known, s);
+            load_keys<F, D, IN_PAGE, J>(of, ts, next, keys);
+            if (some) add_tokens<XT, F, D, IN_PAGE, J>(run, values, s, now, factor, known);
+            load_values<F, D, IN_PAGE, J>(of, ts, next, values);
+#pragma unroll
+            for (int j = 0; j < J; ++j) now[j] = next[j];
         }
 
         run.l = sum_over_quarters(run.l);
@@ -816,8 +904,8 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
             float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxShares * 4);
             const int slot_floats = part_floats(p.cols, D);
             float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
-            // the waves' results, joined
-            if (col < cols) {
+            // the waves' and the sets' results, joined
+            if (mine < cols) {
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -829,15 +917,16 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
                 const int c = 2 * j / D, f = 2 * j % D;
                 float top = s_m[0][c];
 #pragma unroll
-                for (int w = 1; w < 4; ++w) top = fmaxf(top, s_m[w][c]);
+                for (int k = 1; k < WAVES * J; ++k) top = fmaxf(top, s_m[k / J][k % J * kSet + c]);
                 const float base = top == kNoScore ? 0.0f : top;
                 float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const float keep = exp2_fast(s_m[w][c] - base);
-                    l = __builtin_fmaf(s_l[w][c], keep, l);
-                    o0 = __builtin_fmaf(s_o[w][c][f], keep, o0);
-                    o1 = __builtin_fmaf(s_o[w][c][f + 1], keep, o1);
+                for (int k = 0; k < WAVES * J; ++k) {
+                    const int w = k / J, from = k % J * kSet + c;
+                    const float keep = exp2_fast(s_m[w][from] - base);
+                    l = __builtin_fmaf(s_l[w][from], keep, l);
+                    o0 = __builtin_fmaf(s_o[w][from][f], keep, o0);
+                    o1 = __builtin_fmaf(s_o[w][from][f + 1], keep, o1);
                 }
                 if (whole) {
                     XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
@@ -876,12 +965,18 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 
 // What runs: shares, a wave's or a workgroup's each.
-struct Shares { int waves, n; };
+struct Shares { int waves, pieces, n; };
+// Whether there is a kernel of two pieces to a wave's step: of 4 bits, which is bound by the vector unit (64 rows of 4096 tokens, us, one piece and two: 104 and 90; in 8 bits
+// 102 and 105; four pieces do not fit the registers: 243).
+constexpr bool two_pieces(int format, bool bf16, int d, bool in_page) { return format == KVTC_CACHE_INT4 && bf16 && d <= 128 && in_page; }
 
 template <typename XT, int F, int D, bool IN_PAGE>
 static void launch_shares(const AttendPlan& p, const Shares& s, hipStream_t stream) {
-    if (s.waves == 1) hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1>), dim3((s.n + 3) / 4), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4>), dim3(s.n), dim3(256), 0, stream, p);
+    if constexpr (two_pieces(F, sizeof(XT) == 2, D, IN_PAGE)) {
+        if (s.pieces == 2) { hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4, 2>), dim3(s.n), dim3(256), 0, stream, p); return; }
+    }
+    if (s.waves == 1) hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1, 1>), dim3((s.n + 3) / 4), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4, 1>), dim3(s.n), dim3(256), 0, stream, p);
 }
 template <typename XT, int F, int D>
 static void launch_pages(const AttendPlan& p, const Shares& s, hipStream_t stream) {
@@ -919,17 +1014,20 @@ static void heads_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) 
 }
 
 // Shares, a wave's or a workgroup's each: as many as run at once (two workgroups to a compute unit, one of wide heads), no more than there can be tiles.
-static Shares shares_at_once(const kvtc_cache& c, int n_seqs, int parts, int64_t max_tokens, int64_t sinks, int64_t window) {
+static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int parts, int cols, int64_t max_tokens, int64_t sinks, int64_t window) {
     int64_t pieces = (max_tokens + 31) / 32;
     if (window) {
         const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / 32 + (window < max_tokens ? window : max_tokens) / 32 + 3;
         pieces = some < pieces ? some : pieces;
     }
+    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), items = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
-    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2);
-    s.waves = pieces <= kShortPieces && (int64_t)n_seqs * c.n_heads * parts >= 4 * places ? 1 : 4;
-    const int64_t tiles = (pieces + s.waves - 1) / s.waves, at_once = places * (4 / s.waves), most = at_once < kAttendMaxShares ? at_once : kAttendMaxShares;
-    const __int128 all = (__int128)tiles * n_seqs * c.n_heads * parts;
+    s.waves = pieces <= kShortPieces && items >= 4 * places ? 1 : 4;
+    // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 10.7 and 12.5, of 4096
+    // 13.5 and 13.0, of 131072 70 and 62)
+    s.pieces = s.waves == 4 && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * items >= 2 * places ? 2 : 1;
+    const int64_t tile = (int64_t)s.waves * s.pieces, tiles = (pieces + tile - 1) / tile, at_once = places * (4 / s.waves), most = at_once < kAttendMaxShares ? at_once : kAttendMaxShares;
+    const __int128 all = (__int128)tiles * items;
     s.n = (int)(all < most ? (int64_t)all : most);
     return s;
 }
@@ -937,10 +1035,11 @@ static Shares shares_at_once(const kvtc_cache& c, int n_seqs, int parts, int64_t
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {
     int parts, cols;
     heads_of(c, n_q_heads, parts, cols);
-    // (a window may make for smaller tiles, and never for more shares of them than there are waves at once)
-    const int n = n_seqs < 1 ? 1 : n_seqs;
-    const Shares s = shares_at_once(c, n, parts, max_tokens, 0, 0), small = shares_at_once(c, n, parts, max_tokens < 32 * kShortPieces ? max_tokens : 32 * kShortPieces, 0, 0);
-    return (size_t)kAttendMaxShares * 4 + (size_t)(s.n > small.n ? s.n : small.n) * 2 * part_floats(cols, c.d_head) * sizeof(float);
+    // (types, windows and short rows make for other tiles, and none for more shares that are joined than this)
+    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), tiles = (max_tokens + 127) / 128;
+    const __int128 all = (__int128)tiles * (n_seqs < 1 ? 1 : n_seqs) * c.n_heads * parts;
+    const int64_t most = places < kAttendMaxShares ? places : kAttendMaxShares, n = all < most ? (int64_t)all : most;
+    return (size_t)kAttendMaxShares * 4 + (size_t)n * 2 * part_floats(cols, c.d_head) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream) {
@@ -962,7 +1061,7 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     while ((1ull << s) < (uint64_t)a.c.page_tokens) ++s;
     p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);
     p.page_shift = 31 + s;
-    const Shares shares = shares_at_once(a.c, a.n_seqs, parts, a.max_tokens, a.sinks, a.window);
+    const Shares shares = shares_at_once(a.c, dtype == KVTC_BF16, a.n_seqs, parts, cols, a.max_tokens, a.sinks, a.window);
     static void (*const launch[6])(const AttendPlan&, const Shares&, hipStream_t) = {launch_attend_0, launch_attend_1, launch_attend_2, launch_attend_3, launch_attend_4, launch_attend_5};
     launch[(dtype == KVTC_BF16 ? 0 : 3) + a.c.format](p, shares, stream);
     return hipGetLastError();
