@@ -39,7 +39,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttendCols = 16;                            // query heads of an item, at most
-constexpr int kAttendMaxShares = 4096;                     // shares of a launch, at most: a counter each in the workspace
+constexpr int kAttendMaxShares = 1024;                     // shares of a launch, at most: a counter each in the workspace
 constexpr int kShortPieces = 16;                          // rows of so many pieces at most are a wave's each
 constexpr float kNoScore = -__builtin_huge_valf();
 
@@ -772,33 +772,102 @@ __device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
     for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(x + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
-// WAVES = 4: the waves of a workgroup take J pieces each of the same tile, and their results are joined in the LDS.  WAVES = 1, for many short rows: every wave has a
-// share of its own, of whole items (those whose first piece falls into it), and nothing is joined.
+// The query heads of an item.
+struct Heads { int h, col0, cols; };
+__device__ __forceinline__ Heads heads_of_item(const AttendPlan& p, uint32_t item) {
+    const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
+    return {h, h * p.group + part * p.cols, min(p.cols, p.group - part * p.cols)};
+}
+
+// What wave `wave` of WAVES has to do with the tiles tile0 .. tile1 of an item, J pieces to a step.
 template <typename XT, int F, int D, bool IN_PAGE, int WAVES, int J>
+__device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const Heads& part, const Tiles& t, uint32_t tile0, uint32_t tile1, uint32_t wave, const Constants& known, Running<XT, F, D>& run) {
+    const AttendArgs& a = p.a;
+    const int col = threadIdx.x & 15;
+    const float factor = a.scale * 1.44269504088896340736f;
+    constexpr int kSet = kAttendCols / J;
+    const int mine = col % kSet;                       // the head of the lane's column
+    Query<XT, F, D> q;
+    load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(part.col0 + (mine < part.cols ? mine : 0)) * a.q_head_stride, mine < part.cols, q);
+    const int64_t scale_head = (int64_t)part.h * a.c.page_tokens * (4 * Shape<F, D>::SW);
+    const int64_t row_head = (int64_t)part.h * a.c.head_stride;
+    const Item of{a.pages + (int64_t)b * a.pages_stride, bytes_at(a.c.k_dev) + row_head, bytes_at(a.c.v_dev) + row_head, bytes_at(a.c.k_scales_dev) + scale_head, bytes_at(a.c.v_scales_dev) + scale_head,
+                  t.length, t.from, p.window ? p.sinks : 0u, (uint32_t)b};
+    const uint32_t ts = (uint32_t)a.c.token_stride;
+    auto look = [&](uint32_t i, Look<IN_PAGE> (&l)[J]) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const uint32_t k = (WAVES * i + wave) * J + j, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
+            l[j] = look_at<IN_PAGE>(p, of, i < tile1 && k < t.pieces ? piece * 32 : t.length);
+        }
+    };
+    auto places = [&](const Look<IN_PAGE> (&l)[J], Where<IN_PAGE> (&w)[J]) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) w[j] = where<Shape<F, D>::SW, IN_PAGE>(p, of, l[j]);
+    };
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) run.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    run.m = kNoScore;
+    run.l = 0.0f;
+#pragma unroll
+    for (int g = 0; g < (F == KVTC_CACHE_INT4 ? D / 32 : 1); ++g) run.low[g] = 0.0f;
+
+    Keys<F, D, J> keys;
+    Values<F, D, J> values;
+    Look<IN_PAGE> ahead[J];
+    Where<IN_PAGE> now[J], next[J];
+    look(tile0, ahead);
+    places(ahead, now);
+    look(tile0 + 1, ahead);
+    load_keys<F, D, IN_PAGE, J>(of, ts, now, keys);
+    load_values<F, D, IN_PAGE, J>(of, ts, now, values);
+    for (uint32_t i = tile0; i < tile1; ++i) {
+        places(ahead, next);
+        look(i + 2, ahead);
+        float s[8];
+        const bool some = any_seen(now) != 0u;
+        if (some) scores<XT, F, D, J>(q, keys, known, s);
+        load_keys<F, D, IN_PAGE, J>(of, ts, next, keys);
+        if (some) add_tokens<XT, F, D, IN_PAGE, J>(run, values, s, now, factor, known);
+        load_values<F, D, IN_PAGE, J>(of, ts, next, values);
+#pragma unroll
+        for (int j = 0; j < J; ++j) now[j] = next[j];
+    }
+
+    run.l = sum_over_quarters(run.l);
+    if constexpr (F == KVTC_CACHE_INT4) {
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) run.low[g] = sum_over_quarters(run.low[g]);
+    }
+}
+
+// Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares of n, the heads of a sequence one after another, so that where several heads' rows are in one cache line its
+// L2 has it for all of them (4 bits, token-major, 128 features, 64 bytes to a row: 16 rows of 32768 tokens 185 us, with the shares in turn 193).
+__device__ __forceinline__ uint32_t neighbours_to_an_xcd(uint32_t block, uint32_t n) { return (block & 7u) * (n / 8) + min(block & 7u, n % 8) + block / 8; }
+
+// Long rows: shares of equal numbers of tiles, four waves to each.
+template <typename XT, int F, int D, bool IN_PAGE, int J>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
     const AttendArgs& a = p.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
-    __shared__ float s_o[WAVES][WAVES > 1 ? kAttendCols : 1][WAVES > 1 ? D + 4 : 1], s_m[WAVES][kAttendCols], s_l[WAVES][kAttendCols];
+    constexpr int kSet = kAttendCols / J;
+    __shared__ float s_o[4][kAttendCols][D + 4], s_m[4][kAttendCols], s_l[4][kAttendCols];
     __shared__ uint32_t s_last;
 
     // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
-    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, most = WAVES > 1 ? gridDim.x : gridDim.x * 4;
+    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts;
     uint32_t mine = 0;
     const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
     for (int b = first; b < last; ++b) {
         const int32_t length = a.lengths[b];
         if (blockIdx.x == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
-        mine += tiles_of<WAVES * J>(p, length).n;
+        mine += tiles_of<4 * J>(p, length).n;
     }
     const uint32_t upto = wave_inclusive_scan(mine);
     const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
-    const uint32_t groups = all < most ? (uint32_t)all : most;       // (no share is empty: each of an item's workgroups is waited for)
-    // Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares, the heads of a sequence one after another, so that where several heads' rows are in one cache line its
-    // L2 has it for all of them (4 bits, token-major, 128 features: 64 bytes; 16 rows of 32768 tokens with the shares in turn 193 us).
-    const uint32_t blocks = WAVES > 1 ? groups : (groups + 3) / 4, block = blockIdx.x;
-    if (block >= blocks) return;
-    const uint32_t turn = (block & 7u) * (blocks / 8) + min(block & 7u, blocks % 8) + block / 8, me = WAVES > 1 ? turn : turn * 4 + wave;
-    if (me >= groups) return;
+    const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
+    if (blockIdx.x >= groups) return;
+    const uint32_t me = neighbours_to_an_xcd(blockIdx.x, groups);
     // me * all / groups, by the quotient and the remainder of all / groups
     const uint64_t each = quotient(all, groups);
     const uint32_t odd = (uint32_t)(all - each * groups);
@@ -807,165 +876,120 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
     const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
     int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
     uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
-    Tiles t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, b));
+    Tiles t = tiles_of<4 * J>(p, scalar_at(a.lengths, b));
     while (share0 >= seq0 + (uint64_t)t.n * heads) {
         seq0 += (uint64_t)t.n * heads;
-        t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, ++b));
+        t = tiles_of<4 * J>(p, scalar_at(a.lengths, ++b));
     }
     uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
     const Constants known = constants();
-    const float factor = a.scale * 1.44269504088896340736f;
 
     uint64_t at = share0;
-    if (WAVES == 1 && tile0 > 0) {
-        at += t.n - tile0;
-        tile0 = 0;
-        ++item;
-    }
     while (at < share1) {
         if (item == heads) {
             item = 0;
             seq0 += (uint64_t)t.n * heads;
-            t = tiles_of<WAVES * J>(p, scalar_at(a.lengths, ++b));
+            t = tiles_of<4 * J>(p, scalar_at(a.lengths, ++b));
         }
-        const uint32_t tile1 = WAVES > 1 ? (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at)) : t.n;
-        const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
-        const int col0 = h * p.group + part * p.cols, cols = min(p.cols, p.group - part * p.cols);
-
-        constexpr int kSet = kAttendCols / J;
-        const int mine = col % kSet;                       // the head of the lane's column
-        Query<XT, F, D> q;
-        load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(col0 + (mine < cols ? mine : 0)) * a.q_head_stride, mine < cols, q);
-        const int64_t scale_head = (int64_t)h * a.c.page_tokens * (4 * Shape<F, D>::SW);
-        const int64_t row_head = (int64_t)h * a.c.head_stride;
-        const Item of{a.pages + (int64_t)b * a.pages_stride, bytes_at(a.c.k_dev) + row_head, bytes_at(a.c.v_dev) + row_head, bytes_at(a.c.k_scales_dev) + scale_head, bytes_at(a.c.v_scales_dev) + scale_head,
-                      t.length, t.from, p.window ? p.sinks : 0u, (uint32_t)b};
-        const uint32_t ts = (uint32_t)a.c.token_stride;
-        auto look = [&](uint32_t i, Look<IN_PAGE> (&l)[J]) {
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const uint32_t k = (WAVES > 1 ? WAVES * i + wave : i) * J + j, piece = k < t.sinks ? k : t.window0 + (k - t.sinks);
-                l[j] = look_at<IN_PAGE>(p, of, i < tile1 && k < t.pieces ? piece * 32 : t.length);
-            }
-        };
-        auto places = [&](const Look<IN_PAGE> (&l)[J], Where<IN_PAGE> (&w)[J]) {
-#pragma unroll
-            for (int j = 0; j < J; ++j) w[j] = where<Shape<F, D>::SW, IN_PAGE>(p, of, l[j]);
-        };
+        const uint32_t tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at));
+        const Heads part = heads_of_item(p, item);
+        const int cols = part.cols;
         Running<XT, F, D> run;
+        attend_tiles<XT, F, D, IN_PAGE, 4, J>(p, b, part, t, tile0, tile1, wave, known, run);
+        const int64_t row0 = (int64_t)b * a.n_q_heads + part.col0;
+        const bool whole = tile0 == 0 && tile1 == t.n;
+        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxShares * 4);
+        const int slot_floats = part_floats(p.cols, D);
+        float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
+        // the waves' and the sets' results, joined
+        if (col % kSet < cols) {
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) run.o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        run.m = kNoScore;
-        run.l = 0.0f;
+            for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-        for (int g = 0; g < (F == KVTC_CACHE_INT4 ? D / 32 : 1); ++g) run.low[g] = 0.0f;
-
-        Keys<F, D, J> keys;
-        Values<F, D, J> values;
-        Look<IN_PAGE> ahead[J];
-        Where<IN_PAGE> now[J], next[J];
-        look(tile0, ahead);
-        places(ahead, now);
-        look(tile0 + 1, ahead);
-        load_keys<F, D, IN_PAGE, J>(of, ts, now, keys);
-        load_values<F, D, IN_PAGE, J>(of, ts, now, values);
-        for (uint32_t i = tile0; i < tile1; ++i) {
-            places(ahead, next);
-            look(i + 2, ahead);
-            float s[8];
-            const bool some = any_seen(now) != 0u;
-            if (some) scores<XT, F, D, J>(q, keys, known, s);
-            load_keys<F, D, IN_PAGE, J>(of, ts, next, keys);
-            if (some) add_tokens<XT, F, D, IN_PAGE, J>(run, values, s, now, factor, known);
-            load_values<F, D, IN_PAGE, J>(of, ts, next, values);
-#pragma unroll
-            for (int j = 0; j < J; ++j) now[j] = next[j];
+                for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
+            if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
         }
-
-        run.l = sum_over_quarters(run.l);
-        if constexpr (F == KVTC_CACHE_INT4) {
+        __syncthreads();
+        for (int j = tid; j < cols * D / 2; j += 256) {
+            const int c = 2 * j / D, f = 2 * j % D;
+            float top = s_m[0][c];
 #pragma unroll
-            for (int g = 0; g < D / 32; ++g) run.low[g] = sum_over_quarters(run.low[g]);
-        }
-        const int64_t row0 = (int64_t)b * a.n_q_heads + col0;
-        if constexpr (WAVES == 1) {
-            if (col < cols) {
-                const float l = run.l;
-                XT* out = static_cast<XT*>(a.out) + (row0 + col) * D;
-                in_runs<XT, F, D>(run, quarter, [&](int f, auto& v) {
+            for (int k = 1; k < 4 * J; ++k) top = fmaxf(top, s_m[k / J][k % J * kSet + c]);
+            const float base = top == kNoScore ? 0.0f : top;
+            float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll
-                    for (float& x : v) x = l == 0.0f ? 0.0f : x / l;
-                    put_run(out + f, v);
-                });
-                if (a.lse && quarter == 0) a.lse[row0 + col] = l == 0.0f ? kNoScore : (run.m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            for (int k = 0; k < 4 * J; ++k) {
+                const int w = k / J, from = k % J * kSet + c;
+                const float keep = exp2_fast(s_m[w][from] - base);
+                l = __builtin_fmaf(s_l[w][from], keep, l);
+                o0 = __builtin_fmaf(s_o[w][from][f], keep, o0);
+                o1 = __builtin_fmaf(s_o[w][from][f + 1], keep, o1);
             }
-        } else {
-            const bool whole = tile0 == 0 && tile1 == t.n;
-            float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxShares * 4);
-            const int slot_floats = part_floats(p.cols, D);
-            float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
-            // the waves' and the sets' results, joined
-            if (mine < cols) {
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
-                if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
+            if (whole) {
+                XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+                put_out(out, l == 0.0f ? 0.0f : o0 / l);
+                put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
+                if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            } else {
+                put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
+                if (f == 0) put_pair(slot + 2 * c, top, l);
+            }
+        }
+        if (!whole) {
+            // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
+            const uint64_t item0 = seq0 + (uint64_t)item * t.n;
+            const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
+            const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            uint32_t* counter = static_cast<uint32_t*>(a.work) + g0;
+            if (tid == 0) {
+                const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_last = came == g1 - g0;
+                if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            for (int j = tid; j < cols * D / 2; j += 256) {
-                const int c = 2 * j / D, f = 2 * j % D;
-                float top = s_m[0][c];
-#pragma unroll
-                for (int k = 1; k < WAVES * J; ++k) top = fmaxf(top, s_m[k / J][k % J * kSet + c]);
-                const float base = top == kNoScore ? 0.0f : top;
-                float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-#pragma unroll
-                for (int k = 0; k < WAVES * J; ++k) {
-                    const int w = k / J, from = k % J * kSet + c;
-                    const float keep = exp2_fast(s_m[w][from] - base);
-                    l = __builtin_fmaf(s_l[w][from], keep, l);
-                    o0 = __builtin_fmaf(s_o[w][from][f], keep, o0);
-                    o1 = __builtin_fmaf(s_o[w][from][f + 1], keep, o1);
-                }
-                if (whole) {
-                    XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
-                    put_out(out, l == 0.0f ? 0.0f : o0 / l);
-                    put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-                    if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
-                } else {
-                    put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
-                    if (f == 0) put_pair(slot + 2 * c, top, l);
-                }
-            }
-            if (!whole) {
-                // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
-                const uint64_t item0 = seq0 + (uint64_t)item * t.n;
-                const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
-                const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                __syncthreads();
-                uint32_t* counter = static_cast<uint32_t*>(a.work) + g0;
-                if (tid == 0) {
-                    const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    s_last = came == g1 - g0;
-                    if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-                __syncthreads();
-                if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
-            }
-            __syncthreads();
+            if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
         }
+        __syncthreads();
         at += tile1 - tile0;
         tile0 = 0;
         ++item;
     }
 }
 
+// Many short rows: a wave, which is a workgroup, to an item, and nothing to be joined.
+template <typename XT, int F, int D, bool IN_PAGE>
+__global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const AttendPlan p) {
+    const AttendArgs& a = p.a;
+    const int lane = threadIdx.x, col = lane & 15, quarter = lane >> 4;
+    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = neighbours_to_an_xcd(blockIdx.x, gridDim.x);
+    const int b = (int)(me / heads);
+    const uint32_t item = me - (uint32_t)b * heads;
+    const int32_t length = scalar_at(a.lengths, b);
+    if (item == 0 && lane == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
+    const Tiles t = tiles_of<1>(p, length);
+    const Heads part = heads_of_item(p, item);
+    const Constants known = constants();
+    Running<XT, F, D> run;
+    attend_tiles<XT, F, D, IN_PAGE, 1, 1>(p, b, part, t, 0, t.n, 0, known, run);
+    if (col < part.cols) {
+        const int64_t row = (int64_t)b * a.n_q_heads + part.col0 + col;
+        const float l = run.l;
+        XT* out = static_cast<XT*>(a.out) + row * D;
+        in_runs<XT, F, D>(run, quarter, [&](int f, auto& v) {
+#pragma unroll
+            for (float& x : v) x = l == 0.0f ? 0.0f : x / l;
+            put_run(out + f, v);
+        });
+        if (a.lse && quarter == 0) a.lse[row] = l == 0.0f ? kNoScore : (run.m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    }
+}
+
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 
-// What runs: shares, a wave's or a workgroup's each.
-struct Shares { int waves, pieces, n; };
+// What runs: a wave to every item (rows), or shares of tiles; pieces to a wave's step; workgroups.
+struct Shares { bool rows; int pieces, n; };
 // Whether there is a kernel of two pieces to a wave's step: of 4 bits, which is bound by the vector unit (64 rows of 4096 tokens, us, one piece and two: 104 and 90; in 8 bits
 // 102 and 105; four pieces do not fit the registers: 243).
 constexpr bool two_pieces(int format, bool bf16, int d, bool in_page) { return format == KVTC_CACHE_INT4 && bf16 && d <= 128 && in_page; }
@@ -973,10 +997,10 @@ constexpr bool two_pieces(int format, bool bf16, int d, bool in_page) { return f
 template <typename XT, int F, int D, bool IN_PAGE>
 static void launch_shares(const AttendPlan& p, const Shares& s, hipStream_t stream) {
     if constexpr (two_pieces(F, sizeof(XT) == 2, D, IN_PAGE)) {
-        if (s.pieces == 2) { hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4, 2>), dim3(s.n), dim3(256), 0, stream, p); return; }
+        if (s.pieces == 2) { hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 2>), dim3(s.n), dim3(256), 0, stream, p); return; }
     }
-    if (s.waves == 1) hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1, 1>), dim3((s.n + 3) / 4), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 4, 1>), dim3(s.n), dim3(256), 0, stream, p);
+    if (s.rows) hipLaunchKernelGGL((attend_rows_kernel<XT, F, D, IN_PAGE>), dim3(s.n), dim3(64), 0, stream, p);
+    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1>), dim3(s.n), dim3(256), 0, stream, p);
 }
 template <typename XT, int F, int D>
 static void launch_pages(const AttendPlan& p, const Shares& s, hipStream_t stream) {
@@ -1013,7 +1037,7 @@ static void heads_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) 
     cols = (group + parts - 1) / parts;
 }
 
-// Shares, a wave's or a workgroup's each: as many as run at once (two workgroups to a compute unit, one of wide heads), no more than there can be tiles.
+// Shares: as many as run at once (two workgroups to a compute unit, one of wide heads), no more than there can be tiles.
 static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int parts, int cols, int64_t max_tokens, int64_t sinks, int64_t window) {
     int64_t pieces = (max_tokens + 31) / 32;
     if (window) {
@@ -1022,13 +1046,13 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     }
     const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), items = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
-    s.waves = pieces <= kShortPieces && items >= 4 * places ? 1 : 4;
+    s.rows = pieces <= kShortPieces && items >= 4 * places && items < (1 << 25);
     // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 10.7 and 12.5, of 4096
     // 13.5 and 13.0, of 131072 70 and 62)
-    s.pieces = s.waves == 4 && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * items >= 2 * places ? 2 : 1;
-    const int64_t tile = (int64_t)s.waves * s.pieces, tiles = (pieces + tile - 1) / tile, at_once = places * (4 / s.waves), most = at_once < kAttendMaxShares ? at_once : kAttendMaxShares;
+    s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * items >= 2 * places ? 2 : 1;
+    const int64_t tiles = (pieces + 4 * s.pieces - 1) / (4 * s.pieces), most = places < kAttendMaxShares ? places : kAttendMaxShares;
     const __int128 all = (__int128)tiles * items;
-    s.n = (int)(all < most ? (int64_t)all : most);
+    s.n = (int)(s.rows ? items : all < most ? (int64_t)all : most);
     return s;
 }
 
