@@ -6,8 +6,9 @@
 //   int4   per 32 features: shift = fp16 downwards of the least, scale = fp16 upwards of (most - shift) * (1/15), codes =
 //          clamp(rne((x - shift) * (1/scale)), 0, 15); byte pair * (d/32) + group of the row has the codes of features 2 pair, 2 pair + 1 of the
 //          group, so that d/32 neighbouring bytes are of one pair (what the attention's matrix products take in one piece)
-// Streaming kernels, bound by memory: a lane has 8 neighbouring features (16 bytes of bf16) of kRows rows, whose loads are on their way together; a row's d/8 lanes
-// find its extremes by lane exchanges.
+// Streaming kernels, bound by memory: a lane has 8 neighbouring features (16 bytes of bf16) of ROWS rows, whose loads are on their way together; a row's d/8 lanes
+// find its extremes by lane exchanges.  32768 tokens of 8 heads of 128 bf16 features, 192 MB in all: into 8 bits 45 us, 4.5 TB/s (a copy of as much 43), out of 4 bits 40; one token 1.9, a
+// launch's time.
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_numeric.h"
@@ -16,8 +17,6 @@ namespace kvtc {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kRows = 4;                                   // rows of a lane
 
 // n / d for n < 2^31, by one product (m = ceil(2^(31 + s) / d), s = ceil(log2 d): its excess over 2^(31 + s) / d is below 2^s / d, so n times it stays below the next quotient)
 struct Divisor { uint32_t d, mul, shift; };
@@ -110,19 +109,19 @@ __device__ __forceinline__ float over_lanes(float v, OP op) {
     return v;
 }
 
-template <typename XT, int F, int D>
+template <typename XT, int F, int D, int ROWS>
 __global__ void __launch_bounds__(256) cache_write_kernel(const TokenArgs a) {
     constexpr int L = D / 8, G = D / kCacheGroup;          // lanes of a row; groups of a row
     const int lane = threadIdx.x & 63, at = threadIdx.x % L;
     const bool side = blockIdx.y;
     const CacheTokenArgs& t = a.t;
-    const uint32_t rows = (uint32_t)t.n_tokens * (uint32_t)t.c.n_heads, row0 = blockIdx.x * (uint32_t)(kRows * 256 / L) + threadIdx.x / L;
+    const uint32_t rows = (uint32_t)t.n_tokens * (uint32_t)t.c.n_heads, row0 = blockIdx.x * (uint32_t)(ROWS * 256 / L) + threadIdx.x / L;
     const XT* x = static_cast<const XT*>(side ? t.v : t.k);
-    float v[kRows][8];
-    int64_t slot[kRows];
-    uint32_t token[kRows], head[kRows];
+    float v[ROWS][8];
+    int64_t slot[ROWS];
+    uint32_t token[ROWS], head[ROWS];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
         const uint32_t r = row0 + u * (256 / L), rr = r < rows ? r : 0;      // (past the end: the first row, not stored)
         token[u] = divide(rr, a.heads);
         head[u] = rr - token[u] * a.heads.d;
@@ -133,7 +132,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const TokenArgs a) {
     uint8_t* rows_out = static_cast<uint8_t*>(side ? t.c.v_dev : t.c.k_dev);
     void* scales_out = side ? t.c.v_scales_dev : t.c.k_scales_dev;
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
         const Place p = place_of(a, token[u], slot[u], at == 0 && head[u] == 0);
         uint8_t* row = rows_out + (int64_t)p.page * t.c.page_stride + (int64_t)head[u] * t.c.head_stride + (int64_t)p.in * t.c.token_stride;
         const int64_t scale_at = ((int64_t)p.page * t.c.n_heads + head[u]) * t.c.page_tokens + p.in;
@@ -192,17 +191,17 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const TokenArgs a) {
     }
 }
 
-template <typename XT, int F, int D>
+template <typename XT, int F, int D, int ROWS>
 __global__ void __launch_bounds__(256) cache_read_kernel(const TokenArgs a) {
     constexpr int L = D / 8, G = D / kCacheGroup;
     const int lane = threadIdx.x & 63, at = threadIdx.x % L;
     const bool side = blockIdx.y;
     const CacheTokenArgs& t = a.t;
-    const uint32_t rows = (uint32_t)t.n_tokens * (uint32_t)t.c.n_heads, row0 = blockIdx.x * (uint32_t)(kRows * 256 / L) + threadIdx.x / L;
-    int64_t slot[kRows];
-    uint32_t token[kRows], head[kRows];
+    const uint32_t rows = (uint32_t)t.n_tokens * (uint32_t)t.c.n_heads, row0 = blockIdx.x * (uint32_t)(ROWS * 256 / L) + threadIdx.x / L;
+    int64_t slot[ROWS];
+    uint32_t token[ROWS], head[ROWS];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
         const uint32_t r = row0 + u * (256 / L), rr = r < rows ? r : 0;
         token[u] = divide(rr, a.heads);
         head[u] = rr - token[u] * a.heads.d;
@@ -210,11 +209,11 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const TokenArgs a) {
     }
     const uint8_t* rows_in = static_cast<const uint8_t*>(side ? t.c.v_dev : t.c.k_dev);
     const void* scales_in = side ? t.c.v_scales_dev : t.c.k_scales_dev;
-    u32x4 held[kRows];
-    uint32_t scale[kRows];
-    bool is[kRows];
+    u32x4 held[ROWS];
+    uint32_t scale[ROWS];
+    bool is[ROWS];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
         const Place p = place_of(a, token[u], slot[u], at == 0 && head[u] == 0);
         is[u] = p.is;
         // (no place: the pool's first row, not used)
@@ -235,7 +234,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const TokenArgs a) {
     }
     XT* x = static_cast<XT*>(side ? t.v : t.k);
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+    for (int u = 0; u < ROWS; ++u) {
         float v[8];
         if constexpr (F == KVTC_CACHE_BF16) {
 #pragma unroll
@@ -264,9 +263,19 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const TokenArgs a) {
     }
 }
 
+template <bool kWrite, typename XT, int F, int D, int ROWS>
+void launch_rows(const TokenArgs& a, hipStream_t stream) {
+    constexpr int64_t kEach = ROWS * 256 / (D / 8);        // rows of a workgroup
+    const dim3 grid((uint32_t)((a.t.n_tokens * a.t.c.n_heads + kEach - 1) / kEach), 2), block(256);
+    if constexpr (kWrite) hipLaunchKernelGGL((cache_write_kernel<XT, F, D, ROWS>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((cache_read_kernel<XT, F, D, ROWS>), grid, block, 0, stream, a);
+}
+
+// Four rows to a lane, quantised bf16 only, from where they gain: with more to wait for per lane, and a quarter of the waves, a call that does not fill the chip many times over
+// is longer.  (us, one row and four.  Into 8 bits, 8 heads of 128: 64 tokens 2.2 and 3.8, 9001 12.9 and 14.0, 32768 49.6 and 45.3, 60000 81 and 73; out of 4 bits 2000 4.5 and 4.6, 9001 13.0 and
+// 11.4, 32768 59 and 40.  bf16 pages, in and out, 32768 49.5 and 50.6, fp32 features, 4 heads of 64, 60000 into 8 bits 30.0 and 31.8, out 37.6 and 43.4: never.)
 template <bool kWrite, typename XT, int F, int D>
 hipError_t launch_tokens(const CacheTokenArgs& all, hipStream_t stream) {
-    constexpr int64_t kEach = kRows * 256 / (D / 8);       // rows of a workgroup
     const int64_t most = 0x7fffffffLL / all.c.n_heads;     // tokens of a launch: rows are counted in 31 bits
     for (int64_t from = 0; from < all.n_tokens; from += most) {
         TokenArgs a{all, divisor_of((uint32_t)all.c.n_heads), divisor_of((uint32_t)all.c.page_tokens), (uint32_t)from};
@@ -274,9 +283,13 @@ hipError_t launch_tokens(const CacheTokenArgs& all, hipStream_t stream) {
         a.t.k = static_cast<XT*>(all.k) + from * all.token_stride;
         a.t.v = static_cast<XT*>(all.v) + from * all.token_stride;
         a.t.slots += from;
-        const dim3 grid((uint32_t)((a.t.n_tokens * all.c.n_heads + kEach - 1) / kEach), 2), block(256);
-        if constexpr (kWrite) hipLaunchKernelGGL((cache_write_kernel<XT, F, D>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((cache_read_kernel<XT, F, D>), grid, block, 0, stream, a);
+        const int64_t lanes = a.t.n_tokens * all.c.n_heads * (D / 8);
+        if constexpr (sizeof(XT) == 2 && F != KVTC_CACHE_BF16) {
+            if (lanes >= (kWrite ? 1 << 21 : 1 << 20)) launch_rows<kWrite, XT, F, D, 4>(a, stream);
+            else launch_rows<kWrite, XT, F, D, 1>(a, stream);
+        } else {
+            launch_rows<kWrite, XT, F, D, 1>(a, stream);
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
