@@ -41,6 +41,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kAttendCols = 16;                            // query heads of an item, at most
 constexpr int kAttendMaxShares = 1024;                     // shares of a launch, at most: a counter each in the workspace
 constexpr int kShortPieces = 16;                          // rows of so many pieces at most are a wave's each
+// Workgroups to a compute unit, by their registers.  (16-bit values of 64 features: 8 rows of 32768 tokens of 16 heads 199 us with three, 219 with two.  Two of 128 features: three have
+// registers enough in 8 bits, and 64 rows of 4096 tokens took 111 us for 101.)
+__host__ __device__ constexpr int groups_each(int format, int d) { return d == 256 ? 1 : d == 64 && format == KVTC_CACHE_BF16 ? 3 : 2; }
 constexpr float kNoScore = -__builtin_huge_valf();
 
 struct AttendPlan {                                        // what the host works out
@@ -52,6 +55,15 @@ struct AttendPlan {                                        // what the host work
     int64_t scale_stride;                                  // bytes of a page's scales
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
 };
+
+// The call's arguments once more, from memory: where they are used outside the loop over the tokens, that they need not be kept in scalar registers, nor, where these do not do, in lanes of
+// vector registers, through it.  (The kernels' first and only argument.)
+typedef const __attribute__((address_space(4))) AttendPlan& ScalarPlan;
+__device__ __forceinline__ ScalarPlan plan_again() {
+    uint64_t at = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+    asm volatile("" : "+s"(at));
+    return *reinterpret_cast<const __attribute__((address_space(4))) AttendPlan*>(at);
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bf16x8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
@@ -215,7 +227,7 @@ __device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, const Item&
             if ((uint32_t)l.page[n] < (uint32_t)p.a.c.n_pages) {
                 place(l.token + 16 * n, l.page[n], w.row[n], w.scale[n]);
             } else {
-                if ((threadIdx.x & 63) == 0) report_lowest(p.a.status, item.b);
+                if ((threadIdx.x & 63) == 0) report_lowest(plan_again().a.status, item.b);
                 w.seen &= ~mine;
             }
         }
@@ -223,7 +235,7 @@ __device__ __forceinline__ Where<IN_PAGE> where(const AttendPlan& p, const Item&
         w.row[0] = w.scale[0] = 0;
         const bool mine = l.seen >> (threadIdx.x & 31) & 1u, is = mine && (uint32_t)l.page[0] < (uint32_t)p.a.c.n_pages;
         if (is) place(l.token, l.page[0], w.row[0], w.scale[0]);
-        else if (mine) report_lowest(p.a.status, item.b);
+        else if (mine) report_lowest(plan_again().a.status, item.b);
         w.seen = (uint32_t)__ballot(is);
     }
     return w;
@@ -616,8 +628,8 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
 // The 32-token pieces of a sequence that hold a seen token -- those of the sinks, then those of the window -- and its tiles of PIECES of them.  (At least one: every
 // row has a result.)
 struct Tiles { uint32_t n, pieces, sinks, window0, length, from; };
-template <int PIECES>
-__device__ __forceinline__ Tiles tiles_of(const AttendPlan& p, int32_t length) {
+template <int PIECES, typename PLAN>
+__device__ __forceinline__ Tiles tiles_of(PLAN& p, int32_t length) {
     Tiles t;
     t.length = (uint32_t)length <= p.max_tokens ? (uint32_t)length : 0u;
     t.from = p.window && t.length > p.window ? t.length - p.window : 0u;
@@ -656,9 +668,9 @@ __device__ __forceinline__ Pair get_pair(const float* p) {
 // 64 parts took 17 us).  weight: [16][kJoinStep]; sum: [512]; stats: [32].
 constexpr int kJoinStep = 64, kAhead = 16;
 template <typename XT, int D>
-__device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* weight, float* sum,
+__device__ __forceinline__ void join_parts(ScalarPlan plan, int tid, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* weight, float* sum,
                                            float* stats) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lane = tid & 63, wave = tid >> 6;
     const int n = (int)(g1 - g0) + 1;
     auto part_at = [&](int k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
     const int pairs = cols * D / 2, teams = pairs < 256 ? 256 / pairs : 1;
@@ -732,10 +744,10 @@ __device__ __forceinline__ void join_parts(const AttendArgs& a, const float* slo
         if (is && team == 0) {
             const int f = 2 * j - c * D;
             const float l = stats[16 + c];
-            XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+            XT* out = static_cast<XT*>(plan.a.out) + (row0 + c) * D + f;
             put_out(out, l == 0.0f ? 0.0f : o0 / l);
             put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-            if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            if (plan.a.lse && f == 0) plan.a.lse[row0 + c] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
         }
     }
 }
@@ -774,7 +786,7 @@ __device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
 
 // The query heads of an item.
 struct Heads { int h, col0, cols; };
-__device__ __forceinline__ Heads heads_of_item(const AttendPlan& p, uint32_t item) {
+__device__ __forceinline__ Heads heads_of_item(ScalarPlan p, uint32_t item) {
     const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
     return {h, h * p.group + part * p.cols, min(p.cols, p.group - part * p.cols)};
 }
@@ -782,18 +794,18 @@ __device__ __forceinline__ Heads heads_of_item(const AttendPlan& p, uint32_t ite
 // What wave `wave` of WAVES has to do with the tiles tile0 .. tile1 of an item, J pieces to a step.
 template <typename XT, int F, int D, bool IN_PAGE, int WAVES, int J>
 __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const Heads& part, const Tiles& t, uint32_t tile0, uint32_t tile1, uint32_t wave, const Constants& known, Running<XT, F, D>& run) {
-    const AttendArgs& a = p.a;
+    ScalarPlan again = plan_again();
     const int col = threadIdx.x & 15;
-    const float factor = a.scale * 1.44269504088896340736f;
+    const float factor = again.a.scale * 1.44269504088896340736f;
     constexpr int kSet = kAttendCols / J;
     const int mine = col % kSet;                       // the head of the lane's column
     Query<XT, F, D> q;
-    load_query<XT, F, D>(static_cast<const XT*>(a.q) + (int64_t)b * a.q_seq_stride + (int64_t)(part.col0 + (mine < part.cols ? mine : 0)) * a.q_head_stride, mine < part.cols, q);
-    const int64_t scale_head = (int64_t)part.h * a.c.page_tokens * (4 * Shape<F, D>::SW);
-    const int64_t row_head = (int64_t)part.h * a.c.head_stride;
-    const Item of{a.pages + (int64_t)b * a.pages_stride, bytes_at(a.c.k_dev) + row_head, bytes_at(a.c.v_dev) + row_head, bytes_at(a.c.k_scales_dev) + scale_head, bytes_at(a.c.v_scales_dev) + scale_head,
-                  t.length, t.from, p.window ? p.sinks : 0u, (uint32_t)b};
-    const uint32_t ts = (uint32_t)a.c.token_stride;
+    load_query<XT, F, D>(static_cast<const XT*>(again.a.q) + (int64_t)b * again.a.q_seq_stride + (int64_t)(part.col0 + (mine < part.cols ? mine : 0)) * again.a.q_head_stride, mine < part.cols, q);
+    const int64_t scale_head = (int64_t)part.h * again.a.c.page_tokens * (4 * Shape<F, D>::SW);
+    const int64_t row_head = (int64_t)part.h * again.a.c.head_stride;
+    const Item of{again.a.pages + (int64_t)b * again.a.pages_stride, bytes_at(again.a.c.k_dev) + row_head, bytes_at(again.a.c.v_dev) + row_head, bytes_at(again.a.c.k_scales_dev) + scale_head, bytes_at(again.a.c.v_scales_dev) + scale_head,
+                  t.length, t.from, again.window ? again.sinks : 0u, (uint32_t)b};
+    const uint32_t ts = (uint32_t)p.a.c.token_stride;
     auto look = [&](uint32_t i, Look<IN_PAGE> (&l)[J]) {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
@@ -847,59 +859,85 @@ __device__ __forceinline__ uint32_t neighbours_to_an_xcd(uint32_t block, uint32_
 
 // Long rows: shares of equal numbers of tiles, four waves to each.
 template <typename XT, int F, int D, bool IN_PAGE, int J>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const AttendPlan p) {
-    const AttendArgs& a = p.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, quarter = lane >> 4;
+__global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const AttendPlan p) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int kSet = kAttendCols / J;
     __shared__ float s_o[4][kAttendCols][D + 4], s_m[4][kAttendCols], s_l[4][kAttendCols];
     __shared__ uint32_t s_last;
+    // what is not needed among the tokens: tiles of all items; the sequence's first tile, the share's next and end, counted over all items; ...
+    __shared__ struct { uint64_t all, seq0, at, end; uint32_t me, groups, item, tile0, b; } s_share;
 
-    // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
-    const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts;
-    uint32_t mine = 0;
-    const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
-    for (int b = first; b < last; ++b) {
-        const int32_t length = a.lengths[b];
-        if (blockIdx.x == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
-        mine += tiles_of<4 * J>(p, length).n;
-    }
-    const uint32_t upto = wave_inclusive_scan(mine);
-    const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
-    const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
-    if (blockIdx.x >= groups) return;
-    const uint32_t me = neighbours_to_an_xcd(blockIdx.x, groups);
-    // me * all / groups, by the quotient and the remainder of all / groups
-    const uint64_t each = quotient(all, groups);
-    const uint32_t odd = (uint32_t)(all - each * groups);
-    const uint64_t share0 = me * each + me * odd / groups, share1 = (me + 1) * each + (me + 1) * odd / groups;
-    // the lane whose sequences it falls among, and the sequence
-    const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
-    int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
-    uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;      // its first tile, counted over all items
-    Tiles t = tiles_of<4 * J>(p, scalar_at(a.lengths, b));
-    while (share0 >= seq0 + (uint64_t)t.n * heads) {
-        seq0 += (uint64_t)t.n * heads;
-        t = tiles_of<4 * J>(p, scalar_at(a.lengths, ++b));
-    }
-    uint32_t item = (uint32_t)quotient(share0 - seq0, t.n), tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
-    const Constants known = constants();
-
-    uint64_t at = share0;
-    while (at < share1) {
-        if (item == heads) {
-            item = 0;
+    {
+        // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
+        const AttendArgs& a = p.a;
+        const int tid = threadIdx.x, lane = tid & 63;
+        const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts;
+        uint32_t mine = 0;
+        const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
+        for (int b = first; b < last; ++b) {
+            const int32_t length = a.lengths[b];
+            if (blockIdx.x == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
+            mine += tiles_of<4 * J>(p, length).n;
+        }
+        const uint32_t upto = wave_inclusive_scan(mine);
+        const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
+        const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
+        if (blockIdx.x >= groups) return;
+        const uint32_t me = neighbours_to_an_xcd(blockIdx.x, groups);
+        // me * all / groups, by the quotient and the remainder of all / groups
+        const uint64_t each = quotient(all, groups);
+        const uint32_t odd = (uint32_t)(all - each * groups);
+        const uint64_t share0 = me * each + me * odd / groups, share1 = (me + 1) * each + (me + 1) * odd / groups;
+        // the lane whose sequences it falls among, and the sequence
+        const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
+        int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
+        uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;
+        Tiles t = tiles_of<4 * J>(p, scalar_at(a.lengths, b));
+        while (share0 >= seq0 + (uint64_t)t.n * heads) {
             seq0 += (uint64_t)t.n * heads;
             t = tiles_of<4 * J>(p, scalar_at(a.lengths, ++b));
         }
-        const uint32_t tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - at));
-        const Heads part = heads_of_item(p, item);
-        const int cols = part.cols;
+        const uint32_t item = (uint32_t)quotient(share0 - seq0, t.n);
+        if (tid == 0) {
+            s_share.all = all;
+            s_share.seq0 = seq0;
+            s_share.at = share0;
+            s_share.end = share1;
+            s_share.me = me;
+            s_share.groups = groups;
+            s_share.item = item;
+            s_share.tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
+            s_share.b = (uint32_t)b;
+        }
+    }
+    __syncthreads();
+    const Constants known = constants();
+
+    auto same = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    auto same64 = [&](uint64_t v) { return (uint64_t)same((uint32_t)(v >> 32)) << 32 | same((uint32_t)v); };
+    for (;;) {
+        const uint32_t b = same(s_share.b), tile0 = same(s_share.tile0);
         Running<XT, F, D> run;
-        attend_tiles<XT, F, D, IN_PAGE, 4, J>(p, b, part, t, tile0, tile1, wave, known, run);
-        const int64_t row0 = (int64_t)b * a.n_q_heads + part.col0;
-        const bool whole = tile0 == 0 && tile1 == t.n;
-        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.work) + kAttendMaxShares * 4);
-        const int slot_floats = part_floats(p.cols, D);
+        uint32_t tile1;
+        {
+            ScalarPlan plan = plan_again();
+            const Tiles t = tiles_of<4 * J>(plan, scalar_at(plan.a.lengths, b));
+            tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (same64(s_share.end) - same64(s_share.at)));
+            attend_tiles<XT, F, D, IN_PAGE, 4, J>(p, (int)b, heads_of_item(plan, same(s_share.item)), t, tile0, tile1, wave, known, run);
+        }
+
+        // (from here on the thread's number is said to be another one, lest what follows from it be worked out before the loop over the tokens and kept through it)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const int lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+        ScalarPlan plan = plan_again();
+        const uint32_t item = same(s_share.item), me = same(s_share.me), tiles = tiles_of<4 * J>(plan, scalar_at(plan.a.lengths, b)).n;
+        const Heads part = heads_of_item(plan, item);
+        const int cols = part.cols, cols_all = plan.cols;
+        const int64_t row0 = (int64_t)b * plan.a.n_q_heads + part.col0;
+        const bool whole = tile0 == 0 && tile1 == tiles;
+        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(plan.a.work) + kAttendMaxShares * 4);
+        const int slot_floats = part_floats(cols_all, D);
         float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
         // the waves' and the sets' results, joined
         if (col % kSet < cols) {
@@ -926,35 +964,47 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attend_kernel(const Att
                 o1 = __builtin_fmaf(s_o[w][from][f + 1], keep, o1);
             }
             if (whole) {
-                XT* out = static_cast<XT*>(a.out) + (row0 + c) * D + f;
+                XT* out = static_cast<XT*>(plan.a.out) + (row0 + c) * D + f;
                 put_out(out, l == 0.0f ? 0.0f : o0 / l);
                 put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-                if (a.lse && f == 0) a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                if (plan.a.lse && f == 0) plan.a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
             } else {
-                put_pair(slot + 2 * p.cols + c * D + f, o0, o1);
+                put_pair(slot + 2 * cols_all + c * D + f, o0, o1);
                 if (f == 0) put_pair(slot + 2 * c, top, l);
             }
         }
         if (!whole) {
             // the workgroups that the item's first and last tile fall to; the last of them to come here joins the parts
-            const uint64_t item0 = seq0 + (uint64_t)item * t.n;
+            const uint64_t item0 = same64(s_share.seq0) + (uint64_t)item * tiles, all = same64(s_share.all);
+            const uint32_t groups = same(s_share.groups);
             const uint32_t g0 = tile0 == 0 ? me : (uint32_t)quotient((item0 + 1) * groups - 1, all);
-            const uint32_t g1 = tile1 == t.n ? me : (uint32_t)quotient((item0 + t.n) * groups - 1, all);
+            const uint32_t g1 = tile1 == tiles ? me : (uint32_t)quotient((item0 + tiles) * groups - 1, all);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            uint32_t* counter = static_cast<uint32_t*>(a.work) + g0;
+            uint32_t* counter = static_cast<uint32_t*>(plan.a.work) + g0;
             if (tid == 0) {
                 const uint32_t came = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 s_last = came == g1 - g0;
                 if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            if (s_last) join_parts<XT, D>(a, slots, slot_floats, g0, g1, p.cols, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
+            if (s_last) join_parts<XT, D>(plan, tid, slots, slot_floats, g0, g1, cols_all, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
+        }
+        const uint64_t at = same64(s_share.at) + (tile1 - tile0);
+        if (at >= same64(s_share.end)) return;
+        const uint32_t heads = (uint32_t)plan.a.c.n_heads * (uint32_t)plan.parts;
+        __syncthreads();
+        if (tid == 0) {
+            const bool done = item + 1 == heads;           // the sequence's last item
+            s_share.at = at;
+            s_share.tile0 = 0;
+            s_share.item = done ? 0 : item + 1;
+            if (done) {
+                s_share.seq0 += (uint64_t)tiles * heads;
+                s_share.b = b + 1;
+            }
         }
         __syncthreads();
-        at += tile1 - tile0;
-        tile0 = 0;
-        ++item;
     }
 }
 
@@ -969,7 +1019,7 @@ __global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const
     const int32_t length = scalar_at(a.lengths, b);
     if (item == 0 && lane == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
     const Tiles t = tiles_of<1>(p, length);
-    const Heads part = heads_of_item(p, item);
+    const Heads part = heads_of_item(plan_again(), item);
     const Constants known = constants();
     Running<XT, F, D> run;
     attend_tiles<XT, F, D, IN_PAGE, 1, 1>(p, b, part, t, 0, t.n, 0, known, run);
@@ -1037,14 +1087,14 @@ static void heads_of(const kvtc_cache& c, int n_q_heads, int& parts, int& cols) 
     cols = (group + parts - 1) / parts;
 }
 
-// Shares: as many as run at once (two workgroups to a compute unit, one of wide heads), no more than there can be tiles.
+// Shares: as many as run at once, no more than there can be tiles.
 static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int parts, int cols, int64_t max_tokens, int64_t sinks, int64_t window) {
     int64_t pieces = (max_tokens + 31) / 32;
     if (window) {
         const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / 32 + (window < max_tokens ? window : max_tokens) / 32 + 3;
         pieces = some < pieces ? some : pieces;
     }
-    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), items = (int64_t)n_seqs * c.n_heads * parts;
+    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), items = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
     s.rows = pieces <= kShortPieces && items >= 4 * places && items < (1 << 25);
     // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 10.7 and 12.5, of 4096
@@ -1060,7 +1110,7 @@ size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t
     int parts, cols;
     heads_of(c, n_q_heads, parts, cols);
     // (types, windows and short rows make for other tiles, and none for more shares that are joined than this)
-    const int64_t places = (int64_t)compute_units() * (c.d_head == 256 ? 1 : 2), tiles = (max_tokens + 127) / 128;
+    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), tiles = (max_tokens + 127) / 128;
     const __int128 all = (__int128)tiles * (n_seqs < 1 ? 1 : n_seqs) * c.n_heads * parts;
     const int64_t most = places < kAttendMaxShares ? places : kAttendMaxShares, n = all < most ? (int64_t)all : most;
     return (size_t)kAttendMaxShares * 4 + (size_t)n * 2 * part_floats(cols, c.d_head) * sizeof(float);
