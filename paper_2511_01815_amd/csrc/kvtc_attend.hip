@@ -667,9 +667,16 @@ __device__ __forceinline__ Pair get_pair(const float* p) {
 // 512 outputs, several threads share the parts of one.  kAhead parts are on their way together, the first of them while the maxima are found (one after another
 // 64 parts took 17 us).  weight: [16][kJoinStep]; sum: [512]; stats: [32].
 constexpr int kJoinStep = 64, kAhead = 16;
+// An item's rows and their places in the output: the `cols` query heads of a KV head, and those of the next one.
+struct OutRows {
+    int64_t row0;
+    int n, cols, group;
+    __device__ __forceinline__ int64_t at(int c) const { return row0 + (c >= cols ? c / cols * (group - cols) : 0) + c; }
+};
 template <typename XT, int D>
-__device__ __forceinline__ void join_parts(ScalarPlan plan, int tid, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int cols_all, int cols, int64_t row0, float* weight, float* sum,
+__device__ __forceinline__ void join_parts(ScalarPlan plan, int tid, const float* slots, int slot_floats, uint32_t g0, uint32_t g1, int rows_all, const OutRows& rows, float* weight, float* sum,
                                            float* stats) {
+    const int cols = rows.n;
     const int lane = tid & 63, wave = tid >> 6;
     const int n = (int)(g1 - g0) + 1;
     auto part_at = [&](int k) { return slots + (int64_t)(2 * (g0 + k) + (k == 0 ? 1 : 0)) * slot_floats; };
@@ -678,7 +685,7 @@ __device__ __forceinline__ void join_parts(ScalarPlan plan, int tid, const float
         const int team = teams > 1 ? tid / pairs : 0, j = min(teams > 1 ? tid - team * pairs : j0 + tid, pairs - 1), c = 2 * j / D;
         const bool is = team < teams && (teams > 1 || j0 + tid < pairs);
         // parts team, team + teams, ...; those past the last are the last again, and count for nothing
-        auto get = [&](int k) { return get_pair(part_at(min(k, n - 1)) + 2 * cols_all + 2 * j); };
+        auto get = [&](int k) { return get_pair(part_at(min(k, n - 1)) + 2 * rows_all + 2 * j); };
         float o0 = 0.0f, o1 = 0.0f;
         for (int from = 0; from < n; from += kJoinStep) {
             Pair v[kAhead];
@@ -744,10 +751,10 @@ __device__ __forceinline__ void join_parts(ScalarPlan plan, int tid, const float
         if (is && team == 0) {
             const int f = 2 * j - c * D;
             const float l = stats[16 + c];
-            XT* out = static_cast<XT*>(plan.a.out) + (row0 + c) * D + f;
+            XT* out = static_cast<XT*>(plan.a.out) + rows.at(c) * D + f;
             put_out(out, l == 0.0f ? 0.0f : o0 / l);
             put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-            if (plan.a.lse && f == 0) plan.a.lse[row0 + c] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            if (plan.a.lse && f == 0) plan.a.lse[rows.at(c)] = l == 0.0f ? kNoScore : (stats[c] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
         }
     }
 }
@@ -784,10 +791,12 @@ __device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
     for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4*>(x + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
-// The query heads of an item.
+// The query heads of an item: of KV head `next` of the NEXT neighbouring ones that it is made of.
 struct Heads { int h, col0, cols; };
-__device__ __forceinline__ Heads heads_of_item(ScalarPlan p, uint32_t item) {
-    const int h = (int)(item / (uint32_t)p.parts), part = (int)(item - (uint32_t)h * (uint32_t)p.parts);
+template <int NEXT>
+__device__ __forceinline__ Heads heads_of_item(ScalarPlan p, uint32_t item, int next) {
+    const uint32_t of = item / (uint32_t)p.parts;
+    const int h = (int)of * NEXT + next, part = (int)(item - of * (uint32_t)p.parts);
     return {h, h * p.group + part * p.cols, min(p.cols, p.group - part * p.cols)};
 }
 
@@ -858,7 +867,7 @@ __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const H
 __device__ __forceinline__ uint32_t neighbours_to_an_xcd(uint32_t block, uint32_t n) { return (block & 7u) * (n / 8) + min(block & 7u, n % 8) + block / 8; }
 
 // Long rows: shares of equal numbers of tiles, four waves to each.
-template <typename XT, int F, int D, bool IN_PAGE, int J>
+template <typename XT, int F, int D, bool IN_PAGE, int J, int NEXT>
 __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const AttendPlan p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int kSet = kAttendCols / J;
@@ -871,13 +880,13 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
         const AttendArgs& a = p.a;
         const int tid = threadIdx.x, lane = tid & 63;
-        const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts;
+        const uint32_t heads = (uint32_t)a.c.n_heads / NEXT * (uint32_t)p.parts;
         uint32_t mine = 0;
         const int first = lane * p.seqs_each, last = min(first + p.seqs_each, a.n_seqs);
         for (int b = first; b < last; ++b) {
             const int32_t length = a.lengths[b];
             if (blockIdx.x == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
-            mine += tiles_of<4 * J>(p, length).n;
+            mine += tiles_of<4 / NEXT * J>(p, length).n;
         }
         const uint32_t upto = wave_inclusive_scan(mine);
         const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
@@ -892,10 +901,10 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
         int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
         uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;
-        Tiles t = tiles_of<4 * J>(p, scalar_at(a.lengths, b));
+        Tiles t = tiles_of<4 / NEXT * J>(p, scalar_at(a.lengths, b));
         while (share0 >= seq0 + (uint64_t)t.n * heads) {
             seq0 += (uint64_t)t.n * heads;
-            t = tiles_of<4 * J>(p, scalar_at(a.lengths, ++b));
+            t = tiles_of<4 / NEXT * J>(p, scalar_at(a.lengths, ++b));
         }
         const uint32_t item = (uint32_t)quotient(share0 - seq0, t.n);
         if (tid == 0) {
@@ -921,9 +930,9 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         uint32_t tile1;
         {
             ScalarPlan plan = plan_again();
-            const Tiles t = tiles_of<4 * J>(plan, scalar_at(plan.a.lengths, b));
+            const Tiles t = tiles_of<4 / NEXT * J>(plan, scalar_at(plan.a.lengths, b));
             tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (same64(s_share.end) - same64(s_share.at)));
-            attend_tiles<XT, F, D, IN_PAGE, 4, J>(p, (int)b, heads_of_item(plan, same(s_share.item)), t, tile0, tile1, wave, known, run);
+            attend_tiles<XT, F, D, IN_PAGE, 4 / NEXT, J>(p, (int)b, heads_of_item<NEXT>(plan, same(s_share.item), wave % NEXT), t, tile0, tile1, wave / NEXT, known, run);
         }
 
         // (from here on the thread's number is said to be another one, lest what follows from it be worked out before the loop over the tokens and kept through it)
@@ -931,13 +940,13 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63, col = lane & 15, quarter = lane >> 4;
         ScalarPlan plan = plan_again();
-        const uint32_t item = same(s_share.item), me = same(s_share.me), tiles = tiles_of<4 * J>(plan, scalar_at(plan.a.lengths, b)).n;
-        const Heads part = heads_of_item(plan, item);
-        const int cols = part.cols, cols_all = plan.cols;
-        const int64_t row0 = (int64_t)b * plan.a.n_q_heads + part.col0;
+        const uint32_t item = same(s_share.item), me = same(s_share.me), tiles = tiles_of<4 / NEXT * J>(plan, scalar_at(plan.a.lengths, b)).n;
+        const Heads part = heads_of_item<NEXT>(plan, item, 0);
+        const int cols = part.cols, rows_all = NEXT * plan.cols;
+        const OutRows rows{(int64_t)b * plan.a.n_q_heads + part.col0, NEXT * cols, cols, plan.group};
         const bool whole = tile0 == 0 && tile1 == tiles;
         float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(plan.a.work) + kAttendMaxShares * 4);
-        const int slot_floats = part_floats(cols_all, D);
+        const int slot_floats = part_floats(rows_all, D);
         float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
         // the waves' and the sets' results, joined
         if (col % kSet < cols) {
@@ -948,28 +957,32 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
             if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
         }
         __syncthreads();
-        for (int j = tid; j < cols * D / 2; j += 256) {
+        for (int j = tid; j < rows.n * D / 2; j += 256) {
             const int c = 2 * j / D, f = 2 * j % D;
-            float top = s_m[0][c];
+            const int next = NEXT > 1 ? c / cols : 0, head = c - next * cols;
+            auto wave_of = [&](int i) { return i / J * NEXT + next; };        // the waves of this KV head, and their sets
+            auto col_of = [&](int i) { return i % J * kSet + head; };
+            constexpr int kOf = 4 / NEXT * J;
+            float top = s_m[next][head];
 #pragma unroll
-            for (int k = 1; k < 4 * J; ++k) top = fmaxf(top, s_m[k / J][k % J * kSet + c]);
+            for (int i = 1; i < kOf; ++i) top = fmaxf(top, s_m[wave_of(i)][col_of(i)]);
             const float base = top == kNoScore ? 0.0f : top;
             float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 4 * J; ++k) {
-                const int w = k / J, from = k % J * kSet + c;
+            for (int i = 0; i < kOf; ++i) {
+                const int w = wave_of(i), from = col_of(i);
                 const float keep = exp2_fast(s_m[w][from] - base);
                 l = __builtin_fmaf(s_l[w][from], keep, l);
                 o0 = __builtin_fmaf(s_o[w][from][f], keep, o0);
                 o1 = __builtin_fmaf(s_o[w][from][f + 1], keep, o1);
             }
             if (whole) {
-                XT* out = static_cast<XT*>(plan.a.out) + (row0 + c) * D + f;
+                XT* out = static_cast<XT*>(plan.a.out) + rows.at(c) * D + f;
                 put_out(out, l == 0.0f ? 0.0f : o0 / l);
                 put_out(out + 1, l == 0.0f ? 0.0f : o1 / l);
-                if (plan.a.lse && f == 0) plan.a.lse[row0 + c] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                if (plan.a.lse && f == 0) plan.a.lse[rows.at(c)] = l == 0.0f ? kNoScore : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
             } else {
-                put_pair(slot + 2 * cols_all + c * D + f, o0, o1);
+                put_pair(slot + 2 * rows_all + c * D + f, o0, o1);
                 if (f == 0) put_pair(slot + 2 * c, top, l);
             }
         }
@@ -988,11 +1001,11 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
                 if (came == g1 - g0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
-            if (s_last) join_parts<XT, D>(plan, tid, slots, slot_floats, g0, g1, cols_all, cols, row0, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
+            if (s_last) join_parts<XT, D>(plan, tid, slots, slot_floats, g0, g1, rows_all, rows, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
         }
         const uint64_t at = same64(s_share.at) + (tile1 - tile0);
         if (at >= same64(s_share.end)) return;
-        const uint32_t heads = (uint32_t)plan.a.c.n_heads * (uint32_t)plan.parts;
+        const uint32_t heads = (uint32_t)plan.a.c.n_heads / NEXT * (uint32_t)plan.parts;
         __syncthreads();
         if (tid == 0) {
             const bool done = item + 1 == heads;           // the sequence's last item
@@ -1019,7 +1032,7 @@ __global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const
     const int32_t length = scalar_at(a.lengths, b);
     if (item == 0 && lane == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
     const Tiles t = tiles_of<1>(p, length);
-    const Heads part = heads_of_item(plan_again(), item);
+    const Heads part = heads_of_item<1>(plan_again(), item, 0);
     const Constants known = constants();
     Running<XT, F, D> run;
     attend_tiles<XT, F, D, IN_PAGE, 1, 1>(p, b, part, t, 0, t.n, 0, known, run);
@@ -1038,24 +1051,35 @@ __global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const
 
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 
-// What runs: a wave to every item (rows), or shares of tiles; pieces to a wave's step; workgroups.
-struct Shares { bool rows; int pieces, n; };
+// What runs: a wave to every item (rows), or shares of tiles; pieces to a wave's step; KV heads of an item; workgroups.
+struct Shares { bool rows; int pieces, next, n; };
+// KV heads whose rows of a token can lie in one cache line of 128 bytes.
+constexpr int heads_to_a_line(int format, int d, bool in_page) { return !in_page ? 1 : 128 / cache_row_bytes(format, d) < 1 ? 1 : 128 / cache_row_bytes(format, d); }
 // Whether there is a kernel of two pieces to a wave's step: of 4 bits, which is bound by the vector unit (64 rows of 4096 tokens, us, one piece and two: 104 and 90; in 8 bits
 // 102 and 105; four pieces do not fit the registers: 243).
 constexpr bool two_pieces(int format, bool bf16, int d, bool in_page) { return format == KVTC_CACHE_INT4 && bf16 && d <= 128 && in_page; }
 
-template <typename XT, int F, int D, bool IN_PAGE>
+template <typename XT, int F, int D, bool IN_PAGE, int J, int NEXT>
+static void launch_kernel(const AttendPlan& p, const Shares& s, hipStream_t stream) {
+    hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, J, NEXT>), dim3(s.n), dim3(256), 0, stream, p);
+}
+template <typename XT, int F, int D, bool IN_PAGE, int J>
 static void launch_shares(const AttendPlan& p, const Shares& s, hipStream_t stream) {
-    if constexpr (two_pieces(F, sizeof(XT) == 2, D, IN_PAGE)) {
-        if (s.pieces == 2) { hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 2>), dim3(s.n), dim3(256), 0, stream, p); return; }
-    }
-    if (s.rows) hipLaunchKernelGGL((attend_rows_kernel<XT, F, D, IN_PAGE>), dim3(s.n), dim3(64), 0, stream, p);
-    else hipLaunchKernelGGL((attend_kernel<XT, F, D, IN_PAGE, 1>), dim3(s.n), dim3(256), 0, stream, p);
+    constexpr int most = heads_to_a_line(F, D, IN_PAGE);
+    if constexpr (most >= 4) { if (s.next == 4) return launch_kernel<XT, F, D, IN_PAGE, J, 4>(p, s, stream); }
+    if constexpr (most >= 2) { if (s.next == 2) return launch_kernel<XT, F, D, IN_PAGE, J, 2>(p, s, stream); }
+    launch_kernel<XT, F, D, IN_PAGE, J, 1>(p, s, stream);
+}
+template <typename XT, int F, int D, bool IN_PAGE>
+static void launch_pieces(const AttendPlan& p, const Shares& s, hipStream_t stream) {
+    if (s.rows) { hipLaunchKernelGGL((attend_rows_kernel<XT, F, D, IN_PAGE>), dim3(s.n), dim3(64), 0, stream, p); return; }
+    if constexpr (two_pieces(F, sizeof(XT) == 2, D, IN_PAGE)) { if (s.pieces == 2) return launch_shares<XT, F, D, IN_PAGE, 2>(p, s, stream); }
+    launch_shares<XT, F, D, IN_PAGE, 1>(p, s, stream);
 }
 template <typename XT, int F, int D>
 static void launch_pages(const AttendPlan& p, const Shares& s, hipStream_t stream) {
-    if (p.in_page) launch_shares<XT, F, D, true>(p, s, stream);
-    else launch_shares<XT, F, D, false>(p, s, stream);
+    if (p.in_page) launch_pieces<XT, F, D, true>(p, s, stream);
+    else launch_pieces<XT, F, D, false>(p, s, stream);
 }
 template <typename XT, int F>
 static void launch_width(const AttendPlan& p, const Shares& s, hipStream_t stream) {
@@ -1094,26 +1118,37 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
         const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / 32 + (window < max_tokens ? window : max_tokens) / 32 + 3;
         pieces = some < pieces ? some : pieces;
     }
-    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), items = (int64_t)n_seqs * c.n_heads * parts;
+    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), rows = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
-    s.rows = pieces <= kShortPieces && items >= 4 * places && items < (1 << 25);
+    s.rows = pieces <= kShortPieces && rows >= (int64_t)compute_units() * (c.d_head == 256 ? 4 : 8) && rows < (1 << 25);
+    // Several KV heads to an item, the waves of a workgroup among them, where their rows of a token share a cache line, which they each fetch if apart; for caches that may be larger than the
+    // Infinity Cache, which has the line for the second as well, and of many items: fewer items are of more parts, and larger ones, to join.  (Token-major, 16 rows of 32768 tokens, us, apart and
+    // so: 4 bits, 8 heads of 128 175 and 167, 16 of 64 298 and 213; 8 bits, 16 of 64 292 and 252.  32 rows of 2000, 4 bits, 8 of 128, 30 and 33; one of 32768 28 and 46.  4 bits with fp32
+    // queries 247 and 251: the vector unit's work bounds it.)
+    s.next = 1;
+    const bool large = (__int128)pieces * 32 * rows * 2 * cache_row_bytes(c.format, c.d_head) >= 1 << 28;
+    if (!s.rows && large && (bf16 || c.format != KVTC_CACHE_INT4) && c.head_stride < c.token_stride && c.head_stride == cache_row_bytes(c.format, c.d_head))
+        for (int n = heads_to_a_line(c.format, c.d_head, c.page_tokens % 16 == 0); n > 1 && s.next == 1; n /= 2)
+            if (c.n_heads % n == 0 && n * cols <= kAttendCols && rows / n >= places / 8) s.next = n;
+    const int64_t items = rows / s.next;
     // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 10.7 and 12.5, of 4096
     // 13.5 and 13.0, of 131072 70 and 62)
-    s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * items >= 2 * places ? 2 : 1;
-    const int64_t tiles = (pieces + 4 * s.pieces - 1) / (4 * s.pieces), most = places < kAttendMaxShares ? places : kAttendMaxShares;
+    s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * rows >= 2 * places ? 2 : 1;
+    const int64_t tile = 4 / s.next * s.pieces, tiles = (pieces + tile - 1) / tile, most = places < kAttendMaxShares ? places : kAttendMaxShares;
     const __int128 all = (__int128)tiles * items;
-    s.n = (int)(s.rows ? items : all < most ? (int64_t)all : most);
+    s.n = (int)(s.rows ? rows : all < most ? (int64_t)all : most);
     return s;
 }
 
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {
     int parts, cols;
     heads_of(c, n_q_heads, parts, cols);
-    // (types, windows and short rows make for other tiles, and none for more shares that are joined than this)
+    // (types, windows and short rows make for other tiles, and none for more shares that are joined than this; an item of several KV heads has up to 16 rows)
     const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), tiles = (max_tokens + 127) / 128;
     const __int128 all = (__int128)tiles * (n_seqs < 1 ? 1 : n_seqs) * c.n_heads * parts;
     const int64_t most = places < kAttendMaxShares ? places : kAttendMaxShares, n = all < most ? (int64_t)all : most;
-    return (size_t)kAttendMaxShares * 4 + (size_t)n * 2 * part_floats(cols, c.d_head) * sizeof(float);
+    const int rows = heads_to_a_line(c.format, c.d_head, true) > 1 ? kAttendCols : cols;
+    return (size_t)kAttendMaxShares * 4 + (size_t)n * 2 * part_floats(rows, c.d_head) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream) {

@@ -100,3 +100,19 @@ def test_large_calls_are_small_ones_side_by_side(fmt, d, heads, n, page, order):
         want = host(kp.values(rows, scales, fmt, d).astype(np.float32), kv.KVTC_BF16)
         np.testing.assert_array_equal(outs[0][side][some].float().cpu().numpy(), want)
         assert bool((outs[0][side][5] == 0).all()) and bool((outs[0][side][n - 2] == 0).all())
+
+
+@pytest.mark.parametrize("fmt,dtype,d,heads,group,sinks,window", [("int4", kv.KVTC_BF16, 128, 8, 4, 0, 0), ("int4", kv.KVTC_BF16, 64, 8, 4, 0, 0), ("int4", kv.KVTC_BF16, 64, 6, 7, 9, 700), ("fp8", kv.KVTC_BF16, 64, 8, 5, 0, 0),
+                                                                  ("fp8", kv.KVTC_F32, 64, 4, 8, 0, 0), ("fp8", kv.KVTC_BF16, 64, 8, 16, 0, 0)])
+def test_token_major_heads_that_share_a_cache_line(fmt, dtype, d, heads, group, sinks, window):
+    """Rows of 32 and 64 bytes side by side, and a bound of tokens that makes the call a large one: several KV heads to a workgroup (as far as 16 columns hold their query heads)."""
+    lengths = EDGES + [64, 700, 0, 1025, 2000] * 5
+    case = Case(np.random.default_rng(d + heads + group), fmt, d, heads, group, 16, "tokens", lengths, dtype, sinks, window)
+    case.table = np.pad(case.table, ((0, 0), (0, 2100)))
+    case.table_dev = torch.from_numpy(case.table).to(DEV)
+    out, lse, status = case.run(max_tokens=33000)
+    again = case.run(max_tokens=33000)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    case.check(out, lse)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
