@@ -144,8 +144,14 @@ __device__ __forceinline__ void load(Bytes p, uint32_t* w) {
         }
     }
 }
-// (a division of 64 bits costs several times one of 32)
-__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) { return (n | d) >> 32 ? n / d : (uint32_t)n / (uint32_t)d; }
+// Values that are the same in all lanes, back in scalar registers.
+__device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ uint64_t same64(uint64_t v) { return (uint64_t)same((uint32_t)(v >> 32)) << 32 | same((uint32_t)v); }
+// Of such values (divisions are the vector unit's; one of 64 bits costs several times one of 32).
+__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) {
+    if ((n | d) >> 32) return same64(n / d);
+    return same((uint32_t)n / (uint32_t)d);
+}
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
@@ -357,41 +363,46 @@ struct Query {
     float sum[F == KVTC_CACHE_INT4 ? NK : 1];              // 4 bits: of the query over a group
 };
 
-// Of one query head (or none: zeros) the features that go with the lane's part of the keys.
+// Of one query head (or none: zeros) the features that go with the lane's part of the keys: on their way, and as operands.
+template <typename XT, int D>
+struct RawQuery { uint32_t w[D / 32][8 * sizeof(XT) / 4]; };
 template <typename XT, int F, int D>
-__device__ __forceinline__ void load_query(const XT* q, bool is, Query<XT, F, D>& out) {
-    constexpr int NK = D / 32;
+__device__ __forceinline__ void load_query(const XT* q, RawQuery<XT, D>& out) {
     const int quarter = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
+    for (int s = 0; s < D / 32; ++s) {
         // (8 bits: 16 bytes of keys are two products' worth)
         const int first = F == KVTC_CACHE_FP8 ? s / 2 * 64 + quarter * 16 + s % 2 * 8 : s * 32 + quarter * 8;
-        float v[8];
-        if (is) {
+        load<8 * sizeof(XT)>(bytes_at(q + first), out.w[s]);
+    }
+}
+template <typename XT, int F, int D>
+__device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is, Query<XT, F, D>& out) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+        uint32_t w[8 * sizeof(XT) / 4];
+#pragma unroll
+        for (int i = 0; i < (int)(8 * sizeof(XT) / 4); ++i) w[i] = is ? raw.w[s][i] : 0u;
+        if constexpr (sizeof(XT) == 2 && F != KVTC_CACHE_INT4) {
+            out.w[s][0] = operand(w[0], w[1], w[2], w[3]);
+        } else {
+            float v[8];
             if constexpr (sizeof(XT) == 2) {
-                const u32x4 w = *reinterpret_cast<const u32x4*>(q + first);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_f32(w[i] & 0xffffu); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
             } else {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x4 w = reinterpret_cast<const f32x4*>(q + first)[i];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[4 * i + j] = w[j];
-                }
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
             }
-        } else {
+            if constexpr (F == KVTC_CACHE_INT4) {
+                const float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+                out.sum[s] = sum_over_quarters(sum);
+                const float o[8] = {v[0], v[2], v[1], v[3], v[4], v[6], v[5], v[7]};      // the order in which codes come out of their bytes
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+                for (int i = 0; i < 8; ++i) v[i] = o[i];
+            }
+            split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v, out.w[s]);
         }
-        if constexpr (F == KVTC_CACHE_INT4) {
-            float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-            out.sum[s] = sum_over_quarters(sum);
-            const float o[8] = {v[0], v[2], v[1], v[3], v[4], v[6], v[5], v[7]};          // the order in which codes come out of their bytes
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = o[i];
-        }
-        split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v, out.w[s]);
     }
 }
 
@@ -795,7 +806,7 @@ __device__ __forceinline__ void put_run(float* x, const float (&v)[N]) {
 struct Heads { int h, col0, cols; };
 template <int NEXT>
 __device__ __forceinline__ Heads heads_of_item(ScalarPlan p, uint32_t item, int next) {
-    const uint32_t of = item / (uint32_t)p.parts;
+    const uint32_t of = p.parts == 1 ? item : (uint32_t)quotient(item, (uint32_t)p.parts);
     const int h = (int)of * NEXT + next, part = (int)(item - of * (uint32_t)p.parts);
     return {h, h * p.group + part * p.cols, min(p.cols, p.group - part * p.cols)};
 }
@@ -808,8 +819,8 @@ __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const H
     const float factor = again.a.scale * 1.44269504088896340736f;
     constexpr int kSet = kAttendCols / J;
     const int mine = col % kSet;                       // the head of the lane's column
-    Query<XT, F, D> q;
-    load_query<XT, F, D>(static_cast<const XT*>(again.a.q) + (int64_t)b * again.a.q_seq_stride + (int64_t)(part.col0 + (mine < part.cols ? mine : 0)) * again.a.q_head_stride, mine < part.cols, q);
+    RawQuery<XT, D> raw;
+    load_query<XT, F, D>(static_cast<const XT*>(again.a.q) + (int64_t)b * again.a.q_seq_stride + (int64_t)(part.col0 + (mine < part.cols ? mine : 0)) * again.a.q_head_stride, raw);
     const int64_t scale_head = (int64_t)part.h * again.a.c.page_tokens * (4 * Shape<F, D>::SW);
     const int64_t row_head = (int64_t)part.h * again.a.c.head_stride;
     const Item of{again.a.pages + (int64_t)b * again.a.pages_stride, bytes_at(again.a.c.k_dev) + row_head, bytes_at(again.a.c.v_dev) + row_head, bytes_at(again.a.c.k_scales_dev) + scale_head, bytes_at(again.a.c.v_scales_dev) + scale_head,
@@ -842,6 +853,8 @@ __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const H
     look(tile0 + 1, ahead);
     load_keys<F, D, IN_PAGE, J>(of, ts, now, keys);
     load_values<F, D, IN_PAGE, J>(of, ts, now, values);
+    Query<XT, F, D> q;
+    to_operands<XT, F, D>(raw, mine < part.cols, q);       // (the keys are on their way meanwhile)
     for (uint32_t i = tile0; i < tile1; ++i) {
         places(ahead, next);
         look(i + 2, ahead);
@@ -874,8 +887,10 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
     __shared__ float s_o[4][kAttendCols][D + 4], s_m[4][kAttendCols], s_l[4][kAttendCols];
     __shared__ uint32_t s_last;
     // what is not needed among the tokens: tiles of all items; the sequence's first tile, the share's next and end, counted over all items; ...
-    __shared__ struct { uint64_t all, seq0, at, end; uint32_t me, groups, item, tile0, b; } s_share;
+    __shared__ struct { uint64_t all, seq0, at, end; uint32_t me, groups; } s_share;
 
+    uint32_t b, item, tile0, tile1;
+    Tiles t;
     {
         // where the workgroup's share begins: a prefix sum over the sequences' tiles, in every wave
         const AttendArgs& a = p.a;
@@ -894,19 +909,25 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         if (blockIdx.x >= groups) return;
         const uint32_t me = neighbours_to_an_xcd(blockIdx.x, groups);
         // me * all / groups, by the quotient and the remainder of all / groups
-        const uint64_t each = quotient(all, groups);
-        const uint32_t odd = (uint32_t)(all - each * groups);
-        const uint64_t share0 = me * each + me * odd / groups, share1 = (me + 1) * each + (me + 1) * odd / groups;
+        uint64_t share0 = me, share1 = me + 1;
+        if (all != groups) {
+            const uint64_t each = quotient(all, groups);
+            const uint32_t odd = (uint32_t)(all - each * groups);
+            share0 = me * each + quotient(me * odd, groups);
+            share1 = (me + 1) * each + quotient((me + 1) * odd, groups);
+        }
         // the lane whose sequences it falls among, and the sequence
         const int holder = __popcll(__ballot((uint64_t)upto * heads <= share0));
-        int b = __builtin_amdgcn_readfirstlane(holder * p.seqs_each);
+        b = (uint32_t)__builtin_amdgcn_readfirstlane(holder * p.seqs_each);
         uint64_t seq0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), holder) * heads;
-        Tiles t = tiles_of<4 / NEXT * J>(p, scalar_at(a.lengths, b));
+        t = tiles_of<4 / NEXT * J>(p, scalar_at(a.lengths, b));
         while (share0 >= seq0 + (uint64_t)t.n * heads) {
             seq0 += (uint64_t)t.n * heads;
             t = tiles_of<4 / NEXT * J>(p, scalar_at(a.lengths, ++b));
         }
-        const uint32_t item = (uint32_t)quotient(share0 - seq0, t.n);
+        item = (uint32_t)quotient(share0 - seq0, t.n);
+        tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
+        tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (share1 - share0));
         if (tid == 0) {
             s_share.all = all;
             s_share.seq0 = seq0;
@@ -914,40 +935,27 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
             s_share.end = share1;
             s_share.me = me;
             s_share.groups = groups;
-            s_share.item = item;
-            s_share.tile0 = (uint32_t)(share0 - seq0 - (uint64_t)item * t.n);
-            s_share.b = (uint32_t)b;
         }
     }
-    __syncthreads();
     const Constants known = constants();
 
-    auto same = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
-    auto same64 = [&](uint64_t v) { return (uint64_t)same((uint32_t)(v >> 32)) << 32 | same((uint32_t)v); };
     for (;;) {
-        const uint32_t b = same(s_share.b), tile0 = same(s_share.tile0);
+        // (the compiler does not see that these are)
+        b = same(b), item = same(item), tile0 = same(tile0), tile1 = same(tile1);
+        t = {same(t.n), same(t.pieces), same(t.sinks), same(t.window0), same(t.length), same(t.from)};
         Running<XT, F, D> run;
-        uint32_t tile1;
-        {
-            ScalarPlan plan = plan_again();
-            const Tiles t = tiles_of<4 / NEXT * J>(plan, scalar_at(plan.a.lengths, b));
-            tile1 = (uint32_t)min((uint64_t)t.n, tile0 + (same64(s_share.end) - same64(s_share.at)));
-            attend_tiles<XT, F, D, IN_PAGE, 4 / NEXT, J>(p, (int)b, heads_of_item<NEXT>(plan, same(s_share.item), wave % NEXT), t, tile0, tile1, wave / NEXT, known, run);
-        }
+        const Heads part = heads_of_item<NEXT>(plan_again(), item, 0);
+        attend_tiles<XT, F, D, IN_PAGE, 4 / NEXT, J>(p, (int)b, {part.h + wave % NEXT, part.col0 + wave % NEXT * p.group, part.cols}, t, tile0, tile1, wave / NEXT, known, run);
 
         // (from here on the thread's number is said to be another one, lest what follows from it be worked out before the loop over the tokens and kept through it)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         const int lane = tid & 63, col = lane & 15, quarter = lane >> 4;
         ScalarPlan plan = plan_again();
-        const uint32_t item = same(s_share.item), me = same(s_share.me), tiles = tiles_of<4 / NEXT * J>(plan, scalar_at(plan.a.lengths, b)).n;
-        const Heads part = heads_of_item<NEXT>(plan, item, 0);
+        const uint32_t tiles = t.n;
         const int cols = part.cols, rows_all = NEXT * plan.cols;
         const OutRows rows{(int64_t)b * plan.a.n_q_heads + part.col0, NEXT * cols, cols, plan.group};
         const bool whole = tile0 == 0 && tile1 == tiles;
-        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(plan.a.work) + kAttendMaxShares * 4);
-        const int slot_floats = part_floats(rows_all, D);
-        float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
         // the waves' and the sets' results, joined
         if (col % kSet < cols) {
 #pragma unroll
@@ -957,6 +965,10 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
             if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
         }
         __syncthreads();
+        const uint32_t me = same(s_share.me);
+        float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(plan.a.work) + kAttendMaxShares * 4);
+        const int slot_floats = part_floats(rows_all, D);
+        float* slot = slots + (int64_t)(2 * me + (tile0 == 0 ? 1 : 0)) * slot_floats;
         for (int j = tid; j < rows.n * D / 2; j += 256) {
             const int c = 2 * j / D, f = 2 * j % D;
             const int next = NEXT > 1 ? c / cols : 0, head = c - next * cols;
@@ -1003,21 +1015,20 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
             __syncthreads();
             if (s_last) join_parts<XT, D>(plan, tid, slots, slot_floats, g0, g1, rows_all, rows, &s_o[0][0][0], &s_o[1][0][0], &s_m[0][0]);
         }
-        const uint64_t at = same64(s_share.at) + (tile1 - tile0);
-        if (at >= same64(s_share.end)) return;
+        const uint64_t at = same64(s_share.at) + (tile1 - tile0), end = same64(s_share.end);
+        if (at >= end) return;
         const uint32_t heads = (uint32_t)plan.a.c.n_heads / NEXT * (uint32_t)plan.parts;
+        tile0 = 0;
         __syncthreads();
         if (tid == 0) {
-            const bool done = item + 1 == heads;           // the sequence's last item
             s_share.at = at;
-            s_share.tile0 = 0;
-            s_share.item = done ? 0 : item + 1;
-            if (done) {
-                s_share.seq0 += (uint64_t)tiles * heads;
-                s_share.b = b + 1;
-            }
+            if (item + 1 == heads) s_share.seq0 += (uint64_t)tiles * heads;
         }
-        __syncthreads();
+        if (++item == heads) {                             // the sequence's last item: the next one's first
+            item = 0;
+            t = tiles_of<4 / NEXT * J>(plan, scalar_at(plan.a.lengths, ++b));
+        }
+        tile1 = (uint32_t)min((uint64_t)t.n, end - at);
     }
 }
 
@@ -1027,7 +1038,7 @@ __global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const
     const AttendArgs& a = p.a;
     const int lane = threadIdx.x, col = lane & 15, quarter = lane >> 4;
     const uint32_t heads = (uint32_t)a.c.n_heads * (uint32_t)p.parts, me = neighbours_to_an_xcd(blockIdx.x, gridDim.x);
-    const int b = (int)(me / heads);
+    const int b = (int)quotient(me, heads);
     const uint32_t item = me - (uint32_t)b * heads;
     const int32_t length = scalar_at(a.lengths, b);
     if (item == 0 && lane == 0 && (uint32_t)length > p.max_tokens) report_lowest(a.status, (uint32_t)b);
