@@ -40,7 +40,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttendCols = 16;                            // query heads of an item, at most
 constexpr int kAttendMaxShares = 1024;                     // shares of a launch, at most: a counter each in the workspace
-constexpr int kShortPieces = 16;                          // rows of so many pieces at most are a wave's each
+// Rows of at most so many pieces may be a wave's each, whole: no shares to find, nothing to join, and a workgroup takes the next row as it ends; but the last rows run alone, and in 4 bits
+// a step is of one piece.  (256 rows of 8 heads of 128 features, us, shares and so.  bf16: 40 tokens 20.4 and 13.5, 300 65.6 and 61.4, 100 to 1000 102 and 94, 200 to 2000 166 and 178; 8 bits: 300
+// 45.2 and 36.9, 100 to 1000 77.5 and 67.8, 200 to 2000 110 and 126; 4 bits: 300 49.6 and 38.8, 512 61.8 and 58.6, 1 to 600 41.9 and 53.9, 100 to 1000 76 and 92.)
+constexpr int short_pieces(int format) { return format == KVTC_CACHE_INT4 ? 16 : 32; }
 // Workgroups to a compute unit, by their registers.  (16-bit values of 64 features: 8 rows of 32768 tokens of 16 heads 199 us with three, 219 with two.  Two of 128 features: three have
 // registers enough in 8 bits, and 64 rows of 4096 tokens took 111 us for 101.)
 __host__ __device__ constexpr int groups_each(int format, int d) { return d == 256 ? 1 : d == 64 && format == KVTC_CACHE_BF16 ? 3 : 2; }
@@ -1131,7 +1134,7 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     }
     const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), rows = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
-    s.rows = pieces <= kShortPieces && rows >= (int64_t)compute_units() * (c.d_head == 256 ? 4 : 8) && rows < (1 << 25);
+    s.rows = pieces <= short_pieces(c.format) && rows >= (int64_t)compute_units() * (c.d_head == 256 ? 4 : 8) && rows < (1 << 25);
     // Several KV heads to an item, the waves of a workgroup among them, where their rows of a token share a cache line, which they each fetch if apart; for caches that may be larger than the
     // Infinity Cache, which has the line for the second as well, and of many items: fewer items are of more parts, and larger ones, to join.  (Token-major, 16 rows of 32768 tokens, us, apart and
     // so: 4 bits, 8 heads of 128 175 and 167, 16 of 64 298 and 213; 8 bits, 16 of 64 292 and 252.  32 rows of 2000, 4 bits, 8 of 128, 30 and 33; one of 32768 28 and 46.  4 bits with fp32
