@@ -2,12 +2,15 @@
 //
 // One pass over keys and values with the running maximum m and sum l of a softmax: for the scores s of some more tokens,
 //     m' = max(m, s),  l' = l e^(m - m') + sum e^(s - m'),  o' = o e^(m - m') + sum e^(s - m') v.
-// Bytes bound it: every key and value is used for the few query heads of its group only.
+// Bytes bound it: every key and value is used for the few query heads of its group only.  (64 ragged rows of 512 to 16384 tokens, 8 heads of 128 features, bf16:
+// 206 us for 1146 MB, 5.55 TB/s, the rate at which this card reads at all.  One row of 131072 tokens in 8 bits: 60.5 us, 4.6 TB/s.  4 bits: 16 rows of 32768 tokens 153 us, 4.2 TB/s, where the
+// vector unit's unpacking and scaling is in the way as well.)
 //
-// Work.  An item is (sequence, KV head, up to 16 of its query heads); its tokens come in tiles of 128, 32 to a wave.  The tiles of all
+// Work.  An item is (sequence, KV head, up to 16 of its query heads); its tokens come in tiles of four pieces of 32, one to a wave.  The tiles of all
 // items, one after another, are cut into as many equal shares as there are workgroups: whatever the lengths, all workgroups have
 // the same amount to read, and a share begins and ends inside an item where it happens to.  Parts of an item are left in the
-// workspace as (m, l, o); the last of its workgroups to arrive joins them, in their order.
+// workspace as (m, l, o); the last of its workgroups to arrive joins them, in their order.  Many short rows are a wave's each instead, whole.
+// (A tile has eight pieces where a step has two; and of an item made of several KV heads, whose rows share cache lines, a wave or two to each.)
 //
 // Products.  Matrix instructions of 16 x 16 x 32, tokens in the rows and query heads in the columns: S^T = K Q^T, O^T = V^T P^T.  Both sum over an
 // index whose order is free, so long as both operands have the same one, and so
@@ -19,10 +22,11 @@
 // Nothing goes through the LDS before the four waves' results are joined.
 //
 // 8 bits: E4M3 codes are bf16 values; scores and probabilities take the token's scale.  4 bits: byte pair * G + group of a row
-// (G = d / 32 groups) holds two neighbouring features, so that a lane's bytes are of one pair or four and of every group; a nibble over the bf16
-// pattern of 128 is 128 + code.  Scores: per group a product of its own, starting from -128 times the sum of the group's query,
-// times the token's scale, plus the sum times its shift.  Values: per group the probabilities times the tokens' scales; shifts and the 128s by
-// sums apart.
+// (G = d / 32 groups) holds two neighbouring features, so that a lane's bytes are of one pair or four and of every group.  A code as it stands is the bf16
+// pattern of a number below the normal ones, code * 2^-133, and the matrix unit takes such numbers for what they are: a code needs no conversion, but a mask; and the
+// high code of a byte, where it stands, is 16 of them.  Scores: per group a product of its own, times the token's scale, plus the query's sum times its shift.  Values:
+// per group the probabilities times the tokens' scales; low codes, and whole bytes, low + 16 high, from which the low ones' sums are taken in the end; shifts by
+// sums apart.  (With 128 + code from an or, and the 128s taken off by products of their own: 16 rows of 32768 tokens 164 us for 153, with fp32 queries 245 for 199.)
 // Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Parts are cut towards zero so that they have
 // one sign, and in 16 bits are at least 2^-120, so that an infinite value stays one.
 #include <hip/hip_runtime.h>
@@ -44,9 +48,10 @@ constexpr int kAttendMaxShares = 1024;                     // shares of a launch
 // a step is of one piece.  (256 rows of 8 heads of 128 features, us, shares and so.  bf16: 40 tokens 20.4 and 13.5, 300 65.6 and 61.4, 100 to 1000 102 and 94, 200 to 2000 166 and 178; 8 bits: 300
 // 45.2 and 36.9, 100 to 1000 77.5 and 67.8, 200 to 2000 110 and 126; 4 bits: 300 49.6 and 38.8, 512 61.8 and 58.6, 1 to 600 41.9 and 53.9, 100 to 1000 76 and 92.)
 constexpr int short_pieces(int format) { return format == KVTC_CACHE_INT4 ? 16 : 32; }
-// Workgroups to a compute unit, by their registers.  (16-bit values of 64 features: 8 rows of 32768 tokens of 16 heads 199 us with three, 219 with two.  Two of 128 features: three have
-// registers enough in 8 bits, and 64 rows of 4096 tokens took 111 us for 101.)
-__host__ __device__ constexpr int groups_each(int format, int d) { return d == 256 ? 1 : d == 64 && format == KVTC_CACHE_BF16 ? 3 : 2; }
+// Workgroups to a compute unit, by their registers.  (Three of 64 features, unless there are less than two tiles for each: 16 heads, 8 rows of 32768 tokens in bf16 219 us with two and 199 with three, 16
+// rows in 8 bits 251 and 216, in 4 bits 200 and 209, with fp32 queries 258 and 220; 24 rows of 0 to 4001 tokens of 12 heads in 8 bits, with two tiles for each of two workgroups, 15.3 and 18.0.  Two of 128 features: three have registers
+// enough in 8 bits, and 64 rows of 4096 tokens took 111 us for 101.)
+__host__ __device__ constexpr int groups_each(int format, int d, bool bf16) { return d == 256 ? 1 : d == 64 && !(bf16 && format == KVTC_CACHE_INT4) ? 3 : 2; }
 constexpr float kNoScore = -__builtin_huge_valf();
 
 struct AttendPlan {                                        // what the host works out
@@ -55,6 +60,8 @@ struct AttendPlan {                                        // what the host work
     int32_t in_page;                                       // 16 tokens from a multiple of 16 on lie in one page
     int32_t seqs_each;                                     // sequences whose lengths a lane adds up
     uint32_t max_tokens, sinks, window;                    // those of `a`, at most 2^31 - 1
+    int32_t in_turn;                                       // shares go to the XCDs in turn
+    uint32_t few;                                          // shares of less than two tiles: so many at most
     int64_t scale_stride;                                  // bytes of a page's scales
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
 };
@@ -119,11 +126,11 @@ __device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS])
     }
 }
 
-// Constants whose values the compiler is not told, so that they are in registers and one instruction takes what would be two with literals: (w & mask) | base, and v * half + zero.
-struct Constants { uint32_t mask, base; float zero; };
+// A constant whose value the compiler is not told, so that v * half + zero is one instruction.
+struct Constants { float zero; };
 __device__ __forceinline__ Constants constants() {
-    Constants c{0x000f000fu, 0x43004300u, 0.0f};
-    asm volatile("" : "+s"(c.mask), "+v"(c.base), "+s"(c.zero));
+    Constants c{0.0f};
+    asm volatile("" : "+s"(c.zero));
     return c;
 }
 
@@ -363,6 +370,7 @@ template <typename XT, int F, int D>
 struct Query {
     static constexpr int NK = D / 32;
     bf16x8 w[NK][Parts<XT>::q];
+    float factor;                                          // of a score
     float sum[F == KVTC_CACHE_INT4 ? NK : 1];              // 4 bits: of the query over a group
 };
 
@@ -379,105 +387,102 @@ __device__ __forceinline__ void load_query(const XT* q, RawQuery<XT, D>& out) {
         load<8 * sizeof(XT)>(bytes_at(q + first), out.w[s]);
     }
 }
+// 4 bits: a code as it stands is the bf16 pattern of code * 2^-133, a number below the normal ones, which the matrix unit takes for what it is; so is the whole byte of two codes, of low + 16 high.
+// The query is multiplied by 2^up, its largest magnitude to 2^64 (which a score's factor makes good; the factor itself stays finite), and odd features by 1 / 16.
+constexpr int kCodeUnit = -133;
+constexpr float kUp = 0x1p60f;                             // of probabilities times scales
 template <typename XT, int F, int D>
-__device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is, Query<XT, F, D>& out) {
+__device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is, float factor, Query<XT, F, D>& out) {
+    constexpr int NK = D / 32;
+    out.factor = factor;
+    if constexpr (F != KVTC_CACHE_INT4 && sizeof(XT) == 2) {
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-        uint32_t w[8 * sizeof(XT) / 4];
+        for (int s = 0; s < NK; ++s) out.w[s][0] = operand(is ? raw.w[s][0] : 0u, is ? raw.w[s][1] : 0u, is ? raw.w[s][2] : 0u, is ? raw.w[s][3] : 0u);
+    } else {
+        float v[NK][8];
 #pragma unroll
-        for (int i = 0; i < (int)(8 * sizeof(XT) / 4); ++i) w[i] = is ? raw.w[s][i] : 0u;
-        if constexpr (sizeof(XT) == 2 && F != KVTC_CACHE_INT4) {
-            out.w[s][0] = operand(w[0], w[1], w[2], w[3]);
+        for (int s = 0; s < NK; ++s)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t w;
+                if constexpr (sizeof(XT) == 2) w = i % 2 ? raw.w[s][i / 2] & 0xffff0000u : raw.w[s][i / 2] << 16;
+                else w = raw.w[s][i];
+                v[s][i] = __uint_as_float(is ? w : 0u);
+            }
+        if constexpr (F == KVTC_CACHE_INT4) {
+            float top = 0.0f;
+#pragma unroll
+            for (int s = 0; s < NK; ++s)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(v[s][i]));
+            top = max_over_quarters(top);
+            const int up = max(9, 64 + 127 - (int)(__float_as_uint(top) >> 23));
+            out.factor = __builtin_amdgcn_ldexpf(factor, -kCodeUnit - up);
+#pragma unroll
+            for (int s = 0; s < NK; ++s) {
+                float o[8];                                // the order in which codes come out of their bytes
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[s][i] = __builtin_amdgcn_ldexpf(v[s][i], up);
+                const float sum = ((v[s][0] + v[s][1]) + (v[s][2] + v[s][3])) + ((v[s][4] + v[s][5]) + (v[s][6] + v[s][7]));
+                out.sum[s] = __builtin_amdgcn_ldexpf(sum_over_quarters(sum), kCodeUnit);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = v[s][(i & 4) + (i & 1) * 2 + (i >> 1 & 1)] * (i & 2 ? 0.0625f : 1.0f);
+                split<Parts<XT>::q, false>(o, out.w[s]);
+            }
         } else {
-            float v[8];
-            if constexpr (sizeof(XT) == 2) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_f32(w[i] & 0xffffu); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-            }
-            if constexpr (F == KVTC_CACHE_INT4) {
-                const float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-                out.sum[s] = sum_over_quarters(sum);
-                const float o[8] = {v[0], v[2], v[1], v[3], v[4], v[6], v[5], v[7]};      // the order in which codes come out of their bytes
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = o[i];
-            }
-            split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v, out.w[s]);
+            for (int s = 0; s < NK; ++s) split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v[s], out.w[s]);
         }
     }
 }
 
-// bf16 patterns of 128 + code: of the low (even features) and the high four bits of byte `at` of one and of another run of dwords
-__device__ __forceinline__ void nibbles(uint32_t first, uint32_t second, int at_first, int at_second, const Constants& c, uint32_t& even, uint32_t& odd) {
-    const uint32_t u = __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
-    even = (u & c.mask) | c.base;
-    odd = (u >> 4 & c.mask) | c.base;
-}
-// bf16 patterns of the codes themselves
-__device__ __forceinline__ void nibbles_exact(uint32_t first, uint32_t second, int at_first, int at_second, uint32_t& even, uint32_t& odd) {
-    const uint32_t u = __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
-    const float a = (float)(u & 15u), b = (float)(u >> 16 & 15u), c = (float)(u >> 4 & 15u), d = (float)(u >> 20 & 15u);
-    even = high_halves(__float_as_uint(a), __float_as_uint(b));
-    odd = high_halves(__float_as_uint(c), __float_as_uint(d));
+// byte `at` of one and of another run of dwords, each in 16 bits
+__device__ __forceinline__ uint32_t bytes_of(uint32_t first, uint32_t second, int at_first, int at_second) {
+    return __builtin_amdgcn_perm(second, first, (uint32_t)at_first | 0x0c00u | (uint32_t)(at_second + 4) << 16 | 0x0c000000u);
 }
 // two E4M3 codes (the low or the high ones of a dword) as bf16
 template <bool HIGH>
 __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH)); }
 
-// Scores (without the common factor) of the lane's query head and 8 tokens of its set's piece.
+// Scores (without the query's factor) of the lane's query head and 8 tokens of its set's piece.
 template <typename XT, int F, int D, int J>
-__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D, J>& k, const Constants& known, float (&s)[8]) {
+__device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D, J>& k, float (&s)[8]) {
     constexpr int NK = D / 32, QP = Parts<XT>::q;
     const int set = set_of<J>(threadIdx.x & 15);
-    auto own = [&](int j, f32x4& kept, const f32x4& now) { // the set's own piece among J products
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kept[i] = j == 0 || set == j ? now[i] : kept[i];
-    };
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (F == KVTC_CACHE_INT4) {
 #pragma unroll
             for (int g = 0; g < NK; ++g) {
-                f32x4 c;
+                f32x4 codes;
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    uint32_t w[4];
                     auto at = [&](int pair) { return pair * NK + g; };                    // byte of the lane's run
-                    nibbles(k.w[j][n][at(0) / 4], k.w[j][n][at(1) / 4], at(0) % 4, at(1) % 4, known, w[0], w[1]);
-                    nibbles(k.w[j][n][at(2) / 4], k.w[j][n][at(3) / 4], at(2) % 4, at(3) % 4, known, w[2], w[3]);
+                    auto pairs = [&](int a, int b) { return bytes_of(k.w[j][n][at(a) / 4], k.w[j][n][at(b) / 4], at(a) % 4, at(b) % 4); };
                     f32x4 now = {0.0f, 0.0f, 0.0f, 0.0f};
-                    if constexpr (J == 1) {                // -128 times the sum of the query
+                    const uint32_t u = pairs(0, 1), v = pairs(2, 3);
+                    const bf16x8 w = operand(u & 0x000f000fu, u & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u);
 #pragma unroll
-                        for (int i = QP - 1; i >= 0; --i) now = mfma(operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u), q.w[g][i], now);
-                    }
+                    for (int i = QP - 1; i >= 0; --i) now = mfma(w, q.w[g][i], now);
 #pragma unroll
-                    for (int i = QP - 1; i >= 0; --i) now = mfma(operand(w[0], w[1], w[2], w[3]), q.w[g][i], now);
-                    own(j, c, now);
+                    for (int i = 0; i < 4; ++i) codes[i] = j == 0 || set == j ? now[i] : codes[i];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t header = k.scale[4 * n + i][g];
-                    const float codes = J == 1 ? c[i] : __builtin_fmaf(-128.0f, q.sum[g], c[i]);
-                    sum[i] = __builtin_fmaf(half_of(header, 1), codes, __builtin_fmaf(half_of(header, 0), q.sum[g], sum[i]));
+                    sum[i] = __builtin_fmaf(half_of(header, 1), codes[i], __builtin_fmaf(half_of(header, 0), q.sum[g], sum[i]));
                 }
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                f32x4 now = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < NK; ++t) {
+                const uint32_t* w = k.w[0][n];
+                bf16x8 a;
+                if constexpr (F == KVTC_CACHE_BF16) a = operand(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
+                else a = operand(e4m3_to_bf16<false>(w[2 * t]), e4m3_to_bf16<true>(w[2 * t]), e4m3_to_bf16<false>(w[2 * t + 1]), e4m3_to_bf16<true>(w[2 * t + 1]));
 #pragma unroll
-                for (int t = 0; t < NK; ++t) {
-                    const uint32_t* w = k.w[j][n];
-                    bf16x8 a;
-                    if constexpr (F == KVTC_CACHE_BF16) a = operand(w[4 * t], w[4 * t + 1], w[4 * t + 2], w[4 * t + 3]);
-                    else a = operand(e4m3_to_bf16<false>(w[2 * t]), e4m3_to_bf16<true>(w[2 * t]), e4m3_to_bf16<false>(w[2 * t + 1]), e4m3_to_bf16<true>(w[2 * t + 1]));
-#pragma unroll
-                    for (int i = QP - 1; i >= 0; --i) now = mfma(a, q.w[t][i], now);
-                }
-                own(j, sum, now);
+                for (int i = QP - 1; i >= 0; --i) sum = mfma(a, q.w[t][i], sum);
             }
             if constexpr (F == KVTC_CACHE_FP8) {
 #pragma unroll
@@ -510,7 +515,6 @@ __device__ __forceinline__ int feature_of(int i, int r, int quarter) {
 template <typename XT, int F, int D, bool IN_PAGE, int J>
 __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, J>& v, float (&s)[8], const Where<IN_PAGE> (&at)[J], float factor, const Constants& known) {
     constexpr int NO = D / 16, G = D / 32, P = Parts<XT>::p;
-    constexpr bool kExact = sizeof(XT) == 4;               // fp32 results: codes without the 128 that bf16 results can bear in their sums
     const int quarter = (threadIdx.x & 63) >> 4, set = set_of<J>(threadIdx.x & 15);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] *= factor;
@@ -527,20 +531,12 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
             s[k] = is ? s[k] : kNoScore;
 #pragma unroll
             for (int i = 0; i < Shape<F, D>::SW; ++i) v.scale[k][i] = is ? v.scale[k][i] : 0u;
+            if constexpr (F != KVTC_CACHE_INT4) {          // (4 bits are finite whatever they are)
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int i = 0; i < Shape<F, D>::VW; ++i) v.w[j][k][i] = at[j].seen >> token_of(k, quarter) & 1u ? v.w[j][k][i] : 0u;
+                for (int i = 0; i < Shape<F, D>::VW; ++i) v.w[0][k][i] = is ? v.w[0][k][i] : 0u;
+            }
         }
     }
-    // a set's probabilities go with its own piece's values only
-    auto own = [&](int j, const bf16x8& b) {
-        if constexpr (J == 1) return b;
-        u32x4 w = __builtin_bit_cast(u32x4, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = set == j ? w[i] : 0u;
-        return __builtin_bit_cast(bf16x8, w);
-    };
     float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
     top = max_over_quarters(top);
     if (__any(top > run.m)) {
@@ -560,39 +556,38 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
     for (int i = 0; i < 8; ++i) p[i] = exp2_fast(s[i] - base);
     run.l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     if constexpr (F == KVTC_CACHE_INT4) {
+        float up[8];                                       // (codes are small numbers)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) up[i] = p[i] * kUp;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
+            __builtin_amdgcn_sched_barrier(0);             // (one group after the other: all at once, the unpacked codes do not fit the registers, 330 us for 153)
             float ps[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t header = v.scale[i][g];
-                ps[i] = __builtin_fmaf(half_of(header, 1), p[i], known.zero);
+                ps[i] = __builtin_fmaf(half_of(header, 1), up[i], known.zero);
                 run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
             }
             bf16x8 b[P];
             split<P, false>(ps, b);
-            if constexpr (!kExact) {                       // the 128s of the codes, taken off first
-                const bf16x8 less = operand(0xc300c300u, 0xc300c300u, 0xc300c300u, 0xc300c300u);
-#pragma unroll
-                for (int i = P - 1; i >= 0; --i) {
-                    run.o[2 * g] = mfma(less, b[i], run.o[2 * g]);
-                    run.o[2 * g + 1] = mfma(less, b[i], run.o[2 * g + 1]);
-                }
-            }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                uint32_t even[4], odd[4];
+                uint32_t low[4], both[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t first = v.w[j][2 * i][g / 4], second = v.w[j][2 * i + 1][g / 4];
-                    if constexpr (kExact) nibbles_exact(first, second, g % 4, g % 4, even[i], odd[i]);
-                    else nibbles(first, second, g % 4, g % 4, known, even[i], odd[i]);
+                    both[i] = bytes_of(v.w[j][2 * i][g / 4], v.w[j][2 * i + 1][g / 4], g % 4, g % 4);
+                    low[i] = both[i] & 0x000f000fu;
                 }
 #pragma unroll
                 for (int i = P - 1; i >= 0; --i) {
-                    const bf16x8 mine = own(j, b[i]);
-                    run.o[2 * g] = mfma(operand(even[0], even[1], even[2], even[3]), mine, run.o[2 * g]);
-                    run.o[2 * g + 1] = mfma(operand(odd[0], odd[1], odd[2], odd[3]), mine, run.o[2 * g + 1]);
+                    u32x4 own = __builtin_bit_cast(u32x4, b[i]);               // (a set's probabilities go with its own piece's values only)
+                    if constexpr (J > 1) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) own[k] = set == j ? own[k] : 0u;
+                    }
+                    run.o[2 * g] = mfma(operand(low[0], low[1], low[2], low[3]), __builtin_bit_cast(bf16x8, own), run.o[2 * g]);
+                    run.o[2 * g + 1] = mfma(operand(both[0], both[1], both[2], both[3]), __builtin_bit_cast(bf16x8, own), run.o[2 * g + 1]);
                 }
             }
         }
@@ -601,37 +596,52 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] *= __uint_as_float(v.scale[i][0]);
         }
-        bf16x8 all_sets[P], b[P];
-        split<P, F == KVTC_CACHE_BF16>(p, all_sets);
+        bf16x8 b[P];
+        split<P, F == KVTC_CACHE_BF16>(p, b);
+        if constexpr (F == KVTC_CACHE_BF16) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
+            for (int i = 0; i < NO; ++i) {
+                uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < P; ++i) b[i] = own(j, all_sets[i]);
-            if constexpr (F == KVTC_CACHE_BF16) {
+                for (int k = 0; k < 4; ++k) w[k] = i % 2 ? high_halves(v.w[0][2 * k][i / 2], v.w[0][2 * k + 1][i / 2]) : low_halves(v.w[0][2 * k][i / 2], v.w[0][2 * k + 1][i / 2]);
 #pragma unroll
-                for (int i = 0; i < NO; ++i) {
-                    uint32_t w[4];
+                for (int k = P - 1; k >= 0; --k) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
+            }
+        } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] = i % 2 ? high_halves(v.w[j][2 * k][i / 2], v.w[j][2 * k + 1][i / 2]) : low_halves(v.w[j][2 * k][i / 2], v.w[j][2 * k + 1][i / 2]);
+            for (int i = 0; i < NO; i += 2) {
+                uint32_t w[4], x[4];
 #pragma unroll
-                    for (int k = P - 1; k >= 0; --k) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
+                for (int k = 0; k < 4; ++k) {                                 // features i and i + 1 of two tokens: [i, i, i + 1, i + 1]
+                    const uint32_t from = (uint32_t)(i % 4), u = __builtin_amdgcn_perm(v.w[0][2 * k + 1][i / 4], v.w[0][2 * k][i / 4], from | (from + 4) << 8 | (from + 1) << 16 | (from + 5) << 24);
+                    w[k] = e4m3_to_bf16<false>(u);
+                    x[k] = e4m3_to_bf16<true>(u);
                 }
-            } else {
 #pragma unroll
-                for (int i = 0; i < NO; i += 2) {
-                    uint32_t w[4], x[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {                             // features i and i + 1 of two tokens: [i, i, i + 1, i + 1]
-                        const uint32_t from = (uint32_t)(i % 4), u = __builtin_amdgcn_perm(v.w[j][2 * k + 1][i / 4], v.w[j][2 * k][i / 4], from | (from + 4) << 8 | (from + 1) << 16 | (from + 5) << 24);
-                        w[k] = e4m3_to_bf16<false>(u);
-                        x[k] = e4m3_to_bf16<true>(u);
-                    }
-#pragma unroll
-                    for (int k = P - 1; k >= 0; --k) {
-                        run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
-                        run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[k], run.o[i + 1]);
-                    }
+                for (int k = P - 1; k >= 0; --k) {
+                    run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
+                    run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[k], run.o[i + 1]);
                 }
+            }
+        }
+    }
+}
+
+// The sums as they are: 4 bits, of single codes, with their unit and shifts.
+template <typename XT, int F, int D>
+__device__ __forceinline__ void settle(Running<XT, F, D>& run) {
+    run.l = sum_over_quarters(run.l);
+    if constexpr (F == KVTC_CACHE_INT4) {
+        constexpr float kUnit = 0x1p73f;
+        static_assert((double)kUnit * kUp == 0x1p133, "2^-kCodeUnit");
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {
+            const float shift = sum_over_quarters(run.low[g]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float low = run.o[2 * g][r], high = (run.o[2 * g + 1][r] - low) * 0.0625f;
+                run.o[2 * g][r] = __builtin_fmaf(low, kUnit, shift);
+                run.o[2 * g + 1][r] = __builtin_fmaf(high, kUnit, shift);
             }
         }
     }
@@ -781,7 +791,7 @@ __device__ __forceinline__ void in_runs(const Running<XT, F, D>& run, int quarte
         for (int g = 0; g < D / 32; ++g) {
             float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = run.o[2 * g + i % 2][i / 2] + run.low[g];
+            for (int i = 0; i < 8; ++i) v[i] = run.o[2 * g + i % 2][i / 2];
             put(g * 32 + 8 * quarter, v);
         }
     } else {
@@ -857,34 +867,31 @@ __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const H
     load_keys<F, D, IN_PAGE, J>(of, ts, now, keys);
     load_values<F, D, IN_PAGE, J>(of, ts, now, values);
     Query<XT, F, D> q;
-    to_operands<XT, F, D>(raw, mine < part.cols, q);       // (the keys are on their way meanwhile)
+    to_operands<XT, F, D>(raw, mine < part.cols, factor, q);       // (the keys are on their way meanwhile)
     for (uint32_t i = tile0; i < tile1; ++i) {
         places(ahead, next);
         look(i + 2, ahead);
         float s[8];
         const bool some = any_seen(now) != 0u;
-        if (some) scores<XT, F, D, J>(q, keys, known, s);
+        if (some) scores<XT, F, D, J>(q, keys, s);
         load_keys<F, D, IN_PAGE, J>(of, ts, next, keys);
-        if (some) add_tokens<XT, F, D, IN_PAGE, J>(run, values, s, now, factor, known);
+        if (some) add_tokens<XT, F, D, IN_PAGE, J>(run, values, s, now, q.factor, known);
         load_values<F, D, IN_PAGE, J>(of, ts, next, values);
 #pragma unroll
         for (int j = 0; j < J; ++j) now[j] = next[j];
     }
 
-    run.l = sum_over_quarters(run.l);
-    if constexpr (F == KVTC_CACHE_INT4) {
-#pragma unroll
-        for (int g = 0; g < D / 32; ++g) run.low[g] = sum_over_quarters(run.low[g]);
-    }
+    settle<XT, F, D>(run);
 }
 
-// Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares of n, the heads of a sequence one after another, so that where several heads' rows are in one cache line its
-// L2 has it for all of them (4 bits, token-major, 128 features, 64 bytes to a row: 16 rows of 32768 tokens 185 us, with the shares in turn 193).
+// Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares of n, the heads of a sequence one after another, so that where several heads' rows or scales are in one cache line its
+// L2 has it for all of them (24 rows of 12 heads of 64 features, 8 bits, token-major, 15.6 us, with the shares in turn 16.9; 64 ragged rows in bf16 206.6 and 208.7).  Of few long items the shares that read
+// the same tokens lie far apart; there they go in turn, which has them meet in an L2 where an item's shares are a multiple of eight.
 __device__ __forceinline__ uint32_t neighbours_to_an_xcd(uint32_t block, uint32_t n) { return (block & 7u) * (n / 8) + min(block & 7u, n % 8) + block / 8; }
 
 // Long rows: shares of equal numbers of tiles, four waves to each.
 template <typename XT, int F, int D, bool IN_PAGE, int J, int NEXT>
-__global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const AttendPlan p) {
+__global__ void __launch_bounds__(256, groups_each(F, D, sizeof(XT) == 2)) attend_kernel(const AttendPlan p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int kSet = kAttendCols / J;
     __shared__ float s_o[4][kAttendCols][D + 4], s_m[4][kAttendCols], s_l[4][kAttendCols];
@@ -908,9 +915,10 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
         }
         const uint32_t upto = wave_inclusive_scan(mine);
         const uint64_t all = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * heads;
-        const uint32_t groups = all < gridDim.x ? (uint32_t)all : gridDim.x;       // (no share is empty: each of an item's workgroups is waited for)
+        // no share is empty: each of an item's workgroups is waited for
+        const uint32_t most = groups_each(F, D, sizeof(XT) == 2) > 2 && all < 2 * (uint64_t)gridDim.x ? min(p.few, gridDim.x) : gridDim.x, groups = all < most ? (uint32_t)all : most;
         if (blockIdx.x >= groups) return;
-        const uint32_t me = neighbours_to_an_xcd(blockIdx.x, groups);
+        const uint32_t me = p.in_turn ? blockIdx.x : neighbours_to_an_xcd(blockIdx.x, groups);
         // me * all / groups, by the quotient and the remainder of all / groups
         uint64_t share0 = me, share1 = me + 1;
         if (all != groups) {
@@ -964,7 +972,7 @@ __global__ void __launch_bounds__(256, groups_each(F, D)) attend_kernel(const At
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r] + (F == KVTC_CACHE_INT4 ? run.low[F == KVTC_CACHE_INT4 ? i / 2 : 0] : 0.0f);
+                for (int r = 0; r < 4; ++r) s_o[wave][col][feature_of<F, D>(i, r, quarter)] = run.o[i][r];
             if (quarter == 0) { s_m[wave][col] = run.m; s_l[wave][col] = run.l; }
         }
         __syncthreads();
@@ -1066,10 +1074,10 @@ __global__ void __launch_bounds__(64, D == 256 ? 1 : 2) attend_rows_kernel(const
 // ---- launches ------------------------------------------------------------------------------------------------------------------
 
 // What runs: a wave to every item (rows), or shares of tiles; pieces to a wave's step; KV heads of an item; workgroups.
-struct Shares { bool rows; int pieces, next, n; };
+struct Shares { bool rows, in_turn; int pieces, next, n; };
 // KV heads whose rows of a token can lie in one cache line of 128 bytes.
 constexpr int heads_to_a_line(int format, int d, bool in_page) { return !in_page ? 1 : 128 / cache_row_bytes(format, d) < 1 ? 1 : 128 / cache_row_bytes(format, d); }
-// Whether there is a kernel of two pieces to a wave's step: of 4 bits, which is bound by the vector unit (64 rows of 4096 tokens, us, one piece and two: 104 and 90; in 8 bits
+// Whether there is a kernel of two pieces to a wave's step: of 4 bits, which is bound by the vector unit (64 rows of 4096 tokens, us, one piece and two: 90.6 and 77.5; in 8 bits
 // 102 and 105; four pieces do not fit the registers: 243).
 constexpr bool two_pieces(int format, bool bf16, int d, bool in_page) { return format == KVTC_CACHE_INT4 && bf16 && d <= 128 && in_page; }
 
@@ -1132,21 +1140,25 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
         const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / 32 + (window < max_tokens ? window : max_tokens) / 32 + 3;
         pieces = some < pieces ? some : pieces;
     }
-    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), rows = (int64_t)n_seqs * c.n_heads * parts;
+    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head, bf16), rows = (int64_t)n_seqs * c.n_heads * parts;
     Shares s;
     s.rows = pieces <= short_pieces(c.format) && rows >= (int64_t)compute_units() * (c.d_head == 256 ? 4 : 8) && rows < (1 << 25);
     // Several KV heads to an item, the waves of a workgroup among them, where their rows of a token share a cache line, which they each fetch if apart; for caches that may be larger than the
     // Infinity Cache, which has the line for the second as well, and of many items: fewer items are of more parts, and larger ones, to join.  (Token-major, 16 rows of 32768 tokens, us, apart and
-    // so: 4 bits, 8 heads of 128 175 and 167, 16 of 64 298 and 213; 8 bits, 16 of 64 292 and 252.  32 rows of 2000, 4 bits, 8 of 128, 30 and 33; one of 32768 28 and 46.  4 bits with fp32
-    // queries 247 and 251: the vector unit's work bounds it.)
+    // so: 4 bits, 8 heads of 128 175 and 167, 16 of 64 298 and 213; 8 bits, 16 of 64 292 and 252; 4 bits with fp32 queries, 8 of 128 199 and 199, 16 of 64 302 and 220.  32 rows of
+    // 2000, 4 bits, 8 of 128, 30 and 33; one of 32768 28 and 46.)
     s.next = 1;
     const bool large = (__int128)pieces * 32 * rows * 2 * cache_row_bytes(c.format, c.d_head) >= 1 << 28;
-    if (!s.rows && large && (bf16 || c.format != KVTC_CACHE_INT4) && c.head_stride < c.token_stride && c.head_stride == cache_row_bytes(c.format, c.d_head))
-        for (int n = heads_to_a_line(c.format, c.d_head, c.page_tokens % 16 == 0); n > 1 && s.next == 1; n /= 2)
+    const int to_a_line = c.head_stride < c.token_stride && c.head_stride == cache_row_bytes(c.format, c.d_head) ? heads_to_a_line(c.format, c.d_head, c.page_tokens % 16 == 0) : 1;
+    if (!s.rows && large)
+        for (int n = to_a_line; n > 1 && s.next == 1; n /= 2)
             if (c.n_heads % n == 0 && n * cols <= kAttendCols && rows / n >= places / 8) s.next = n;
+    // (one row of 131072 tokens, neighbours to an XCD and in turn: 4 bits of 8 heads of 128 61.6 and 54.4, 8 bits of 12 heads of 64 63.5 and 52.5; four rows of 32768 of 4 heads of 64 in 4 bits 23.0 and 21.3,
+    // five of 20000 23.5 and 26.8)
+    s.in_turn = s.next == 1 && to_a_line > 1 && rows <= 16;
     const int64_t items = rows / s.next;
-    // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 10.7 and 12.5, of 4096
-    // 13.5 and 13.0, of 131072 70 and 62)
+    // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 9.5 and 12.5, of 4096
+    // 12.6 and 11.3; 16 of 32768 178 and 153)
     s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * rows >= 2 * places ? 2 : 1;
     const int64_t tile = 4 / s.next * s.pieces, tiles = (pieces + tile - 1) / tile, most = places < kAttendMaxShares ? places : kAttendMaxShares;
     const __int128 all = (__int128)tiles * items;
@@ -1157,8 +1169,8 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {
     int parts, cols;
     heads_of(c, n_q_heads, parts, cols);
-    // (types, windows and short rows make for other tiles, and none for more shares that are joined than this; an item of several KV heads has up to 16 rows)
-    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head), tiles = (max_tokens + 127) / 128;
+    // (types, windows and short rows make for other tiles and fewer workgroups, and none for more shares that are joined than this; an item of several KV heads has up to 16 rows)
+    const int64_t places = (int64_t)compute_units() * groups_each(c.format, c.d_head, false), tiles = (max_tokens + 127) / 128;
     const __int128 all = (__int128)tiles * (n_seqs < 1 ? 1 : n_seqs) * c.n_heads * parts;
     const int64_t most = places < kAttendMaxShares ? places : kAttendMaxShares, n = all < most ? (int64_t)all : most;
     const int rows = heads_to_a_line(c.format, c.d_head, true) > 1 ? kAttendCols : cols;
@@ -1174,6 +1186,7 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     p.parts = parts;
     p.cols = cols;
     p.in_page = a.c.page_tokens % 16 == 0;
+    p.few = 2 * (uint32_t)compute_units();
     p.seqs_each = (a.n_seqs + 63) / 64;
     auto in_31 = [](int64_t v) { return (uint32_t)(v < 0x7fffffffLL ? v : 0x7fffffffLL); };
     p.max_tokens = in_31(a.max_tokens);
@@ -1186,6 +1199,7 @@ hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stre
     p.page_shift = 31 + s;
     const Shares shares = shares_at_once(a.c, dtype == KVTC_BF16, a.n_seqs, parts, cols, a.max_tokens, a.sinks, a.window);
     static void (*const launch[6])(const AttendPlan&, const Shares&, hipStream_t) = {launch_attend_0, launch_attend_1, launch_attend_2, launch_attend_3, launch_attend_4, launch_attend_5};
+    p.in_turn = shares.in_turn;
     launch[(dtype == KVTC_BF16 ? 0 : 3) + a.c.format](p, shares, stream);
     return hipGetLastError();
 }

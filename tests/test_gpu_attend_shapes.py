@@ -116,3 +116,35 @@ def test_token_major_heads_that_share_a_cache_line(fmt, dtype, d, heads, group, 
     assert int(status.item()) == 0
     case.check(out, lse)
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("dtype", [kv.KVTC_BF16, kv.KVTC_F32])
+@pytest.mark.parametrize("d,group", [(64, 4), (128, 4), (128, 16), (256, 3)])
+@pytest.mark.parametrize("up,size", [(-60, 0), (50, 0), (100, 0), (0, -16), (-40, 10), (20, -12)])
+def test_four_bits_of_any_magnitude(dtype, d, group, up, size):
+    """Queries of 2^up and keys and values of 2^size (fp16 headers below the normal numbers among them), the scale such that scores are as ever; a query of zeros, and a feature far above the rest."""
+    rng = np.random.default_rng(d + group + up)
+    case = Case(rng, "int4", d, 2, group, 32, "heads", [1, 33, 700, 2100], dtype)
+    for b, slots in enumerate(case.slots):
+        for side in range(2):
+            case.pool.put(side, slots, (rng.standard_normal((len(slots), 2, d)) * 2.0 ** size).astype(np.float32))
+    case.cache = case.pool.upload()
+    case.q[0, 0] = 0
+    case.q[2, :, 5] *= 64
+    case.q = host((case.q * 2.0 ** up).astype(np.float32), dtype)
+    case.q_dev = to_dev(case.q, dtype)
+    case.scale = d ** -0.5 * 2.0 ** -(up + size)
+    out, lse, status = case.run()
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and bool(torch.isfinite(lse).all())
+    case.check(out, lse)
+
+
+@pytest.mark.parametrize("fmt,d,heads", [("int4", 128, 4), ("int4", 64, 4), ("fp8", 64, 3)])
+def test_few_long_token_major_rows(fmt, d, heads):
+    """Few items whose rows share cache lines: shares go to the XCDs in turn."""
+    case = Case(np.random.default_rng(d + heads), fmt, d, heads, 2, 64, "tokens", [9001, 0, 4097], kv.KVTC_BF16)
+    first, again = case.run(), case.run()
+    torch.cuda.synchronize()
+    case.check(first[0], first[1])
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
