@@ -475,8 +475,8 @@ size_t kvtc_cache_scale_bytes(kvtc_cache_format format, int d_head);    /* of th
  * 1 + the index of the lowest such token.  Two tokens with the same slot in one write leave either's rows, not
  * necessarily the same one's for all heads.  Quantisation looks at one token at a time: a write of many tokens leaves what
  * writes of single tokens leave.  fp32 features are not rounded before they are quantised.
- * kvtc_cache_read rounds once to dtype (nearest even).  Both are ordered on `stream`, allocate nothing and do not
- * synchronise; n_tokens == 0 is a no-op.
+ * kvtc_cache_read works values out in fp32 (rounded there once) and rounds these to dtype (nearest even).  Both calls are
+ * ordered on `stream`, allocate nothing and do not synchronise; n_tokens == 0 is a no-op.
  */
 kvtc_status kvtc_cache_write(const kvtc_cache* cache, const void* k_dev, const void* v_dev, kvtc_dtype dtype, int64_t n_tokens,
                              int64_t token_stride, int64_t head_stride, const int64_t* slots_dev, uint32_t* status_dev,
