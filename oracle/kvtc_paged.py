@@ -122,12 +122,12 @@ def attend(q: np.ndarray, k: np.ndarray, v: np.ndarray, scale: float):
 
 
 def sizes(rows: np.ndarray, scales, fmt: str, d: int) -> np.ndarray:
-    """Bound of the magnitudes a value is added up from: its own, or, of 4 bits, with a code offset by up to 128 on the way
-    (shift + code * scale as (128 + code) * scale + (shift - 128 * scale))."""
+    """Bound of the magnitudes a value is added up from: its own, or, of 4 bits, shift and code * scale apart, a code up to 17 on the way
+    (15, or of a byte's high code (whole byte - low code) / 16, up to (255 + 15) / 16)."""
     if fmt != "int4":
         return np.abs(values(rows, scales, fmt, d))
     header = np.abs(np.ascontiguousarray(scales).view(np.float16).astype(np.float64).reshape(*rows.shape[:-1], d // GROUP, 2))
-    return np.repeat(header[..., 0] + 272 * header[..., 1], GROUP, axis=-1)
+    return np.repeat(header[..., 0] + 17 * header[..., 1], GROUP, axis=-1)
 
 
 def attend_bound(q, k, v, k_size, v_size, scale: float, kept_bits: int, out_bits: int):
