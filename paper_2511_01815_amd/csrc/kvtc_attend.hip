@@ -827,6 +827,7 @@ __device__ __forceinline__ Heads heads_of_item(ScalarPlan p, uint32_t item, int 
 // What wave `wave` of WAVES has to do with the tiles tile0 .. tile1 of an item, J pieces to a step.
 template <typename XT, int F, int D, bool IN_PAGE, int WAVES, int J>
 __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const Heads& part, const Tiles& t, uint32_t tile0, uint32_t tile1, uint32_t wave, const Constants& known, Running<XT, F, D>& run) {
+    static_assert(J == 1 || F == KVTC_CACHE_INT4, "sets are made for 4 bits");
     ScalarPlan again = plan_again();
     const int col = threadIdx.x & 15;
     const float factor = again.a.scale * 1.44269504088896340736f;
