@@ -27,8 +27,9 @@
 // high code of a byte, where it stands, is 16 of them.  Scores: per group a product of its own, times the token's scale, plus the query's sum times its shift.  Values:
 // per group the probabilities times the tokens' scales; low codes, and whole bytes, low + 16 high, from which the low ones' sums are taken in the end; shifts by
 // sums apart.  (With 128 + code from an or, and the 128s taken off by products of their own: 16 rows of 32768 tokens 164 us for 153, with fp32 queries 245 for 199.)
-// Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Parts are cut towards zero so that they have
-// one sign, and in 16 bits are at least 2^-120, so that an infinite value stays one.
+// Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Of codes both of two are rounded to nearest, 18 bits in all: in 4 bits the error is
+// one of code * scale, which may be far larger than the value.  Of bf16 values, which may be infinite, parts are cut towards zero so that they have one sign, 16 bits, and are at least 2^-120, so that an
+// infinite value stays one.
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
@@ -103,18 +104,20 @@ __device__ __forceinline__ uint32_t round_pair(float first, float second) {
 }
 __device__ __forceinline__ float half_of(uint32_t w, int high) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(high ? w >> 16 : w)); }
 
-// Eight values as a sum of PARTS operands.
+// Eight values as a sum of PARTS operands.  (Two parts: nearest first, within 2^-18, or, with one sign, within 2^-16; three: all 24 bits.)
 template <int PARTS, bool KEEP_SIGN>
 __device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS]) {
+    constexpr bool kNearest = PARTS == 2 && !KEEP_SIGN;
     float rest[8];
     uint32_t w[4];
+    auto first = [&](int i) { return !kNearest ? cut(v[i]) : __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); };
     auto least = [](float r, float of) { return KEEP_SIGN ? __builtin_copysignf(fmaxf(__builtin_fabsf(r), 0x1p-120f), of) : r; };
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = PARTS > 1 ? high_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1])) : round_pair(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) w[i] = PARTS == 1 || kNearest ? round_pair(v[2 * i], v[2 * i + 1]) : high_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
     out[0] = operand(w[0], w[1], w[2], w[3]);
     if constexpr (PARTS > 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rest[i] = least(v[i] - cut(v[i]), v[i]);
+        for (int i = 0; i < 8; ++i) rest[i] = least(v[i] - first(i), v[i]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = PARTS > 2 ? high_halves(__float_as_uint(rest[2 * i]), __float_as_uint(rest[2 * i + 1])) : round_pair(rest[2 * i], rest[2 * i + 1]);
         out[1] = operand(w[0], w[1], w[2], w[3]);
