@@ -32,6 +32,10 @@ uint64_t kvtc_host_encode_pass_bytes(int tiles, kvtc_dtype dtype);
  * bases have this many bytes together, in one tensor's call (single) or a batch; UINT64_MAX: never. */
 uint64_t kvtc_host_decode_pass_bytes(int tiles, kvtc_dtype dtype, uint64_t bases, int single);
 
+/* How a kvtc_attend of these sizes runs, in route[0..4]: 1 where a wave takes a row, whole, 0 where workgroups take equal shares of all rows' tiles; 1 where
+ * shares go to the XCDs in turn; pieces of 32 tokens to a wave's step; KV heads to a workgroup; workgroups.  Returns what kvtc_attend's checks of these do. */
+kvtc_status kvtc_host_attend_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route);
+
 /* On the GPU, over all fp32 bit patterns: adds to counts_dev[0] how many of them are numbers, and to [1], [2] and [3] how many
  * roundings to fp16, group headers and codes of this many bits come out differently as the kernels work them out and as the
  * kvtc_host_* functions do. */

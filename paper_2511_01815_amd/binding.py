@@ -152,6 +152,8 @@ def lib() -> C.CDLL:
         L.kvtc_host_encode_pass_bytes.restype = C.c_uint64
         L.kvtc_host_decode_pass_bytes.argtypes = [C.c_int, C.c_int, C.c_uint64, C.c_int]
         L.kvtc_host_decode_pass_bytes.restype = C.c_uint64
+        L.kvtc_host_attend_route.argtypes = [cp, C.c_int, C.c_int, C.c_int, i64, i64, i64, C.POINTER(C.c_int32)]
+        L.kvtc_host_attend_route.restype = C.c_int
         L.kvtc_test_numeric.argtypes = [C.c_int, vp, vp]
         L.kvtc_test_numeric.restype = C.c_int
         L.kvtc_test_batch_passes.argtypes = [vp, vp, C.c_int, vp, sz, C.c_uint64, vp, vp]

@@ -1485,6 +1485,16 @@ size_t kvtc_attend_work_bytes(const kvtc_cache* cache, int n_seqs, int n_q_heads
     return check_attend("kvtc_attend_work_bytes", cache, n_seqs, n_q_heads, max_tokens) == KVTC_OK ? attend_work_bytes(*cache, n_seqs, n_q_heads, max_tokens) : 0;
 }
 
+kvtc_status kvtc_host_attend_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route) {
+    const kvtc_status st = check_attend("kvtc_host_attend_route", cache, n_seqs, n_q_heads, max_tokens);
+    if (st != KVTC_OK) return st;
+    if (!dtype_ok(dtype) || sinks < 0 || window < 0 || !route) return fail(KVTC_E_ARG, "kvtc_host_attend_route: bad argument");
+    const AttendRoute r = attend_route(*cache, dtype, n_seqs, n_q_heads, max_tokens, sinks, window);
+    const int32_t all[5] = {r.rows, r.in_turn, r.pieces, r.next, r.workgroups};
+    std::copy(all, all + 5, route);
+    return KVTC_OK;
+}
+
 kvtc_status kvtc_attend(const kvtc_cache* cache, const void* q_dev, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t q_seq_stride, int64_t q_head_stride,
                         const int32_t* pages_dev, int64_t pages_stride, const int32_t* lengths_dev, int64_t max_tokens, float scale, int64_t sinks,
                         int64_t window, void* out_dev, float* lse_dev, void* work_dev, size_t work_bytes, uint32_t* status_dev, kvtc_stream stream) {

@@ -1152,11 +1152,13 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     // so: 4 bits, 8 heads of 128 175 and 167, 16 of 64 298 and 213; 8 bits, 16 of 64 292 and 252; 4 bits with fp32 queries, 8 of 128 199 and 199, 16 of 64 302 and 220.  32 rows of
     // 2000, 4 bits, 8 of 128, 30 and 33; one of 32768 28 and 46.)
     s.next = 1;
+    // (The sequences' tiles are added up in 32 bits.  Tiles of four pieces, of which there are at most 2^31 by the checks of the call, always fit.)
+    auto counted = [&](int n) { return (pieces + 4 / n - 1) / (4 / n) * n_seqs <= 0xffffffffLL; };
     const bool large = (__int128)pieces * 32 * rows * 2 * cache_row_bytes(c.format, c.d_head) >= 1 << 28;
     const int to_a_line = c.head_stride < c.token_stride && c.head_stride == cache_row_bytes(c.format, c.d_head) ? heads_to_a_line(c.format, c.d_head, c.page_tokens % 16 == 0) : 1;
     if (!s.rows && large)
         for (int n = to_a_line; n > 1 && s.next == 1; n /= 2)
-            if (c.n_heads % n == 0 && n * cols <= kAttendCols && rows / n >= places / 8) s.next = n;
+            if (c.n_heads % n == 0 && n * cols <= kAttendCols && rows / n >= places / 8 && counted(n)) s.next = n;
     // (one row of 131072 tokens, neighbours to an XCD and in turn: 4 bits of 8 heads of 128 61.6 and 54.4, 8 bits of 12 heads of 64 63.5 and 52.5; four rows of 32768 of 4 heads of 64 in 4 bits 23.0 and 21.3,
     // five of 20000 23.5 and 26.8)
     s.in_turn = s.next == 1 && to_a_line > 1 && rows <= 16;
@@ -1168,6 +1170,13 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     const __int128 all = (__int128)tiles * items;
     s.n = (int)(s.rows ? rows : all < most ? (int64_t)all : most);
     return s;
+}
+
+AttendRoute attend_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window) {
+    int parts, cols;
+    heads_of(c, n_q_heads, parts, cols);
+    const Shares s = shares_at_once(c, dtype == KVTC_BF16, n_seqs, parts, cols, max_tokens, sinks, window);
+    return {s.rows, s.in_turn, s.pieces, s.next, s.n};
 }
 
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens) {

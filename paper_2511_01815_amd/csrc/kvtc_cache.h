@@ -53,6 +53,9 @@ __device__ __forceinline__ uint16_t f32_bf16(float v) { return __builtin_bit_cas
 hipError_t launch_cache_write(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream);
 hipError_t launch_cache_read(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream);
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream);
+// How a call runs: a wave to a row (1) or shares (0), shares to the XCDs in turn, pieces of 32 tokens to a wave's step, KV heads to a workgroup, workgroups.
+struct AttendRoute { int rows, in_turn, pieces, next, workgroups; };
+AttendRoute attend_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window);
 size_t attend_work_bytes(const kvtc_cache& c, int n_seqs, int n_q_heads, int64_t max_tokens);
 
 }  // namespace kvtc
