@@ -36,6 +36,13 @@ uint64_t kvtc_host_decode_pass_bytes(int tiles, kvtc_dtype dtype, uint64_t bases
  * shares go to the XCDs in turn; pieces of 32 tokens to a wave's step; KV heads to a workgroup; workgroups.  Returns what kvtc_attend's checks of these do. */
 kvtc_status kvtc_host_attend_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route);
 
+/* Tokens of 1 .. 1024 heads of 64, 128 or 256 features that kvtc_cache_write and kvtc_cache_read move in one launch, at most. */
+int64_t kvtc_host_cache_launch_tokens(int n_heads, int d_head);
+
+/* kvtc_cache_write (write != 0) or kvtc_cache_read in launches of at most launch_tokens tokens. */
+kvtc_status kvtc_test_cache_tokens(int write, const kvtc_cache* cache, void* k_dev, void* v_dev, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride, int64_t head_stride,
+                                   const int64_t* slots_dev, uint32_t* status_dev, int64_t launch_tokens, kvtc_stream stream);
+
 /* On the GPU, over all fp32 bit patterns: adds to counts_dev[0] how many of them are numbers, and to [1], [2] and [3] how many
  * roundings to fp16, group headers and codes of this many bits come out differently as the kernels work them out and as the
  * kvtc_host_* functions do. */

@@ -1450,24 +1450,33 @@ static kvtc_status check_tokens(const char* who, const kvtc_cache* c, const void
     return KVTC_OK;
 }
 
+// Tokens into the cache or out of it, launch_tokens at most at a time.
+static kvtc_status move_tokens(const char* who, bool write, const kvtc_cache* cache, void* k, void* v, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride, int64_t head_stride,
+                               const int64_t* slots, uint32_t* status, int64_t launch_tokens, kvtc_stream stream) {
+    const kvtc_status st = check_tokens(who, cache, k, v, dtype, n_tokens, token_stride, head_stride, slots, status);
+    if (st != KVTC_OK || n_tokens == 0) return st;
+    const int64_t most = cache_launch_tokens(cache->n_heads, cache->d_head);
+    const CacheTokenArgs a{*cache, k, v, token_stride, head_stride, slots, n_tokens, status};
+    const hipError_t e = (write ? launch_cache_write : launch_cache_read)(a, dtype, launch_tokens < most ? launch_tokens : most, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(KVTC_E_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
+    return KVTC_OK;
+}
+
 kvtc_status kvtc_cache_write(const kvtc_cache* cache, const void* k_dev, const void* v_dev, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride,
                              int64_t head_stride, const int64_t* slots_dev, uint32_t* status_dev, kvtc_stream stream) {
-    const kvtc_status st = check_tokens("kvtc_cache_write", cache, k_dev, v_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev);
-    if (st != KVTC_OK || n_tokens == 0) return st;
-    const CacheTokenArgs a{*cache, const_cast<void*>(k_dev), const_cast<void*>(v_dev), token_stride, head_stride, slots_dev, n_tokens, status_dev};
-    const hipError_t e = launch_cache_write(a, dtype, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return fail(KVTC_E_HIP, "kvtc_cache_write: launch failed: %s", hipGetErrorString(e));
-    return KVTC_OK;
+    return move_tokens("kvtc_cache_write", true, cache, const_cast<void*>(k_dev), const_cast<void*>(v_dev), dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev, INT64_MAX, stream);
 }
 
 kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, int64_t n_tokens, void* k_out_dev, void* v_out_dev, kvtc_dtype dtype,
                             int64_t token_stride, int64_t head_stride, uint32_t* status_dev, kvtc_stream stream) {
-    const kvtc_status st = check_tokens("kvtc_cache_read", cache, k_out_dev, v_out_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev);
-    if (st != KVTC_OK || n_tokens == 0) return st;
-    const CacheTokenArgs a{*cache, k_out_dev, v_out_dev, token_stride, head_stride, slots_dev, n_tokens, status_dev};
-    const hipError_t e = launch_cache_read(a, dtype, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return fail(KVTC_E_HIP, "kvtc_cache_read: launch failed: %s", hipGetErrorString(e));
-    return KVTC_OK;
+    return move_tokens("kvtc_cache_read", false, cache, k_out_dev, v_out_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev, INT64_MAX, stream);
+}
+
+int64_t kvtc_host_cache_launch_tokens(int n_heads, int d_head) { return cache_launch_tokens(n_heads, d_head); }
+kvtc_status kvtc_test_cache_tokens(int write, const kvtc_cache* cache, void* k_dev, void* v_dev, kvtc_dtype dtype, int64_t n_tokens, int64_t token_stride, int64_t head_stride,
+                                   const int64_t* slots_dev, uint32_t* status_dev, int64_t launch_tokens, kvtc_stream stream) {
+    if (launch_tokens < 1) return fail(KVTC_E_ARG, "kvtc_test_cache_tokens: launch_tokens=%lld", (long long)launch_tokens);
+    return move_tokens("kvtc_test_cache_tokens", write != 0, cache, k_dev, v_dev, dtype, n_tokens, token_stride, head_stride, slots_dev, status_dev, launch_tokens, stream);
 }
 
 static kvtc_status check_attend(const char* who, const kvtc_cache* c, int n_seqs, int n_q_heads, int64_t max_tokens) {

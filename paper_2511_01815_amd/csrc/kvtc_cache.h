@@ -50,8 +50,10 @@ __device__ __forceinline__ void report_lowest(uint32_t* status, uint32_t index) 
 __device__ __forceinline__ float bf16_f32(uint32_t bits) { return __uint_as_float(bits << 16); }
 __device__ __forceinline__ uint16_t f32_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 
-hipError_t launch_cache_write(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream);
-hipError_t launch_cache_read(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream);
+// Tokens of one launch, at most: a row is up to d / 8 work-items, in whole workgroups of 256, and a launch of 2^32 of them is refused.  (So rows fit 31 bits.)
+constexpr int64_t cache_launch_tokens(int n_heads, int d) { return ((1LL << 32) - 256) / (d / 8) / n_heads; }
+hipError_t launch_cache_write(const CacheTokenArgs& a, kvtc_dtype dtype, int64_t launch_tokens, hipStream_t stream);
+hipError_t launch_cache_read(const CacheTokenArgs& a, kvtc_dtype dtype, int64_t launch_tokens, hipStream_t stream);
 hipError_t launch_attend(const AttendArgs& a, kvtc_dtype dtype, hipStream_t stream);
 // How a call runs: a wave to a row (1) or shares (0), shares to the XCDs in turn, pieces of 32 tokens to a wave's step, KV heads to a workgroup, workgroups.
 struct AttendRoute { int rows, in_turn, pieces, next, workgroups; };

@@ -275,8 +275,7 @@ void launch_rows(const TokenArgs& a, hipStream_t stream) {
 // is longer.  (us, one row and four.  Into 8 bits, 8 heads of 128: 64 tokens 2.2 and 3.8, 9001 12.9 and 14.0, 32768 49.6 and 45.3, 60000 81 and 73; out of 4 bits 2000 4.5 and 4.6, 9001 13.0 and
 // 11.4, 32768 59 and 40.  bf16 pages, in and out, 32768 49.5 and 50.6, fp32 features, 4 heads of 64, 60000 into 8 bits 30.0 and 31.8, out 37.6 and 43.4: never.)
 template <bool kWrite, typename XT, int F, int D>
-hipError_t launch_tokens(const CacheTokenArgs& all, hipStream_t stream) {
-    const int64_t most = 0x7fffffffLL / all.c.n_heads;     // tokens of a launch: rows are counted in 31 bits
+hipError_t launch_tokens(const CacheTokenArgs& all, int64_t most, hipStream_t stream) {
     for (int64_t from = 0; from < all.n_tokens; from += most) {
         TokenArgs a{all, divisor_of((uint32_t)all.c.n_heads), divisor_of((uint32_t)all.c.page_tokens), (uint32_t)from};
         a.t.n_tokens = all.n_tokens - from < most ? all.n_tokens - from : most;
@@ -296,23 +295,23 @@ hipError_t launch_tokens(const CacheTokenArgs& all, hipStream_t stream) {
     return hipSuccess;
 }
 template <bool kWrite, typename XT, int F>
-hipError_t launch_width(const CacheTokenArgs& a, hipStream_t stream) {
-    if (a.c.d_head == 64) return launch_tokens<kWrite, XT, F, 64>(a, stream);
-    if (a.c.d_head == 128) return launch_tokens<kWrite, XT, F, 128>(a, stream);
-    return launch_tokens<kWrite, XT, F, 256>(a, stream);
+hipError_t launch_width(const CacheTokenArgs& a, int64_t most, hipStream_t stream) {
+    if (a.c.d_head == 64) return launch_tokens<kWrite, XT, F, 64>(a, most, stream);
+    if (a.c.d_head == 128) return launch_tokens<kWrite, XT, F, 128>(a, most, stream);
+    return launch_tokens<kWrite, XT, F, 256>(a, most, stream);
 }
 template <bool kWrite, typename XT>
-hipError_t launch_format(const CacheTokenArgs& a, hipStream_t stream) {
-    if (a.c.format == KVTC_CACHE_BF16) return launch_width<kWrite, XT, KVTC_CACHE_BF16>(a, stream);
-    if (a.c.format == KVTC_CACHE_FP8) return launch_width<kWrite, XT, KVTC_CACHE_FP8>(a, stream);
-    return launch_width<kWrite, XT, KVTC_CACHE_INT4>(a, stream);
+hipError_t launch_format(const CacheTokenArgs& a, int64_t most, hipStream_t stream) {
+    if (a.c.format == KVTC_CACHE_BF16) return launch_width<kWrite, XT, KVTC_CACHE_BF16>(a, most, stream);
+    if (a.c.format == KVTC_CACHE_FP8) return launch_width<kWrite, XT, KVTC_CACHE_FP8>(a, most, stream);
+    return launch_width<kWrite, XT, KVTC_CACHE_INT4>(a, most, stream);
 }
 
-hipError_t launch_cache_write(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream) {
-    return dtype == KVTC_BF16 ? launch_format<true, uint16_t>(a, stream) : launch_format<true, float>(a, stream);
+hipError_t launch_cache_write(const CacheTokenArgs& a, kvtc_dtype dtype, int64_t launch_tokens, hipStream_t stream) {
+    return dtype == KVTC_BF16 ? launch_format<true, uint16_t>(a, launch_tokens, stream) : launch_format<true, float>(a, launch_tokens, stream);
 }
-hipError_t launch_cache_read(const CacheTokenArgs& a, kvtc_dtype dtype, hipStream_t stream) {
-    return dtype == KVTC_BF16 ? launch_format<false, uint16_t>(a, stream) : launch_format<false, float>(a, stream);
+hipError_t launch_cache_read(const CacheTokenArgs& a, kvtc_dtype dtype, int64_t launch_tokens, hipStream_t stream) {
+    return dtype == KVTC_BF16 ? launch_format<false, uint16_t>(a, launch_tokens, stream) : launch_format<false, float>(a, launch_tokens, stream);
 }
 
 }  // namespace kvtc
