@@ -28,8 +28,8 @@
 // per group the probabilities times the tokens' scales; low codes, and whole bytes, low + 16 high, from which the low ones' sums are taken in the end; shifts by
 // sums apart.  (With 128 + code from an or, and the 128s taken off by products of their own: 16 rows of 32768 tokens 164 us for 153, with fp32 queries 245 for 199.)
 // Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Of codes both of two are rounded to nearest, 18 bits in all: in 4 bits the error is
-// one of code * scale, which may be far larger than the value.  Of bf16 values, which may be infinite, parts are cut towards zero so that they have one sign, 16 bits, and are at least 2^-120, so that an
-// infinite value stays one.
+// one of code * scale, which may be far larger than the value.  Of bf16 values, which may be infinite, parts are cut towards zero so that they have one sign, 16 bits, and none is zero, so that an
+// infinite value stays one; where its probability is zero, e^-88 and less in fp32, it makes NaN, as zero times infinity does.
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
@@ -104,14 +104,21 @@ __device__ __forceinline__ uint32_t round_pair(float first, float second) {
 }
 __device__ __forceinline__ float half_of(uint32_t w, int high) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(high ? w >> 16 : w)); }
 
-// Eight values as a sum of PARTS operands.  (Two parts: nearest first, within 2^-18, or, with one sign, within 2^-16; three: all 24 bits.)
-template <int PARTS, bool KEEP_SIGN>
+// Eight values as a sum of PARTS operands.  (Two parts: nearest first, within 2^-18, or, with one sign, within 2^-16; three: all 24 bits, of values of at least 2^-109.)
+// One sign, for what goes with bf16 features, which may be infinite: all parts have the value's sign, and none is zero where the value is not, lest an infinity times zero make NaN of another part's
+// infinity.  The least part that there is, 2^-133, is below what a probability may be off by in fp32 (2^-126), whatever feature it meets; a value of zero has parts of zero.
+enum class Signs { kAny, kOne, kPositive };                // (kPositive: kOne of values that are not negative)
+template <int PARTS, Signs SIGNS>
 __device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS]) {
-    constexpr bool kNearest = PARTS == 2 && !KEEP_SIGN;
+    constexpr bool kNearest = PARTS == 2 && SIGNS == Signs::kAny;
     float rest[8];
     uint32_t w[4];
     auto first = [&](int i) { return !kNearest ? cut(v[i]) : __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); };
-    auto least = [](float r, float of) { return KEEP_SIGN ? __builtin_copysignf(fmaxf(__builtin_fabsf(r), 0x1p-120f), of) : r; };
+    auto least = [](float r, float of) {
+        if constexpr (SIGNS == Signs::kAny) return r;
+        else if constexpr (SIGNS == Signs::kPositive) return fmaxf(r, fminf(of, 0x1p-133f));
+        else return __builtin_copysignf(fmaxf(__builtin_fabsf(r), fminf(__builtin_fabsf(of), 0x1p-133f)), of);
+    };
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = PARTS == 1 || kNearest ? round_pair(v[2 * i], v[2 * i + 1]) : high_halves(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
     out[0] = operand(w[0], w[1], w[2], w[3]);
@@ -430,11 +437,11 @@ __device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is,
                 out.sum[s] = __builtin_amdgcn_ldexpf(sum_over_quarters(sum), kCodeUnit);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = v[s][(i & 4) + (i & 1) * 2 + (i >> 1 & 1)] * (i & 2 ? 0.0625f : 1.0f);
-                split<Parts<XT>::q, false>(o, out.w[s]);
+                split<Parts<XT>::q, Signs::kAny>(o, out.w[s]);
             }
         } else {
 #pragma unroll
-            for (int s = 0; s < NK; ++s) split<Parts<XT>::q, F == KVTC_CACHE_BF16>(v[s], out.w[s]);
+            for (int s = 0; s < NK; ++s) split<Parts<XT>::q, F == KVTC_CACHE_BF16 ? Signs::kOne : Signs::kAny>(v[s], out.w[s]);
         }
     }
 }
@@ -573,7 +580,7 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
                 run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
             }
             bf16x8 b[P];
-            split<P, false>(ps, b);
+            split<P, Signs::kAny>(ps, b);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 uint32_t low[4], both[4];
@@ -600,7 +607,7 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
             for (int i = 0; i < 8; ++i) p[i] *= __uint_as_float(v.scale[i][0]);
         }
         bf16x8 b[P];
-        split<P, F == KVTC_CACHE_BF16>(p, b);
+        split<P, F == KVTC_CACHE_BF16 ? Signs::kPositive : Signs::kAny>(p, b);
         if constexpr (F == KVTC_CACHE_BF16) {
 #pragma unroll
             for (int i = 0; i < NO; ++i) {

@@ -97,3 +97,76 @@ def test_probabilities_of_codes_have_18_bits(fmt, d):
     out, lse = rows.run()
     tol = ((2.0 ** -18 + 2.0 ** -21) * size[0] + (n + 4) * 2.0 ** -24 * size[1]) / weight.sum() + 2.0 ** -9 * np.abs(want)
     assert (np.abs(out - want) <= tol).all(), (np.abs(out - want).max(), tol.min())
+
+
+DTYPES = [kv.KVTC_BF16, kv.KVTC_F32]
+LARGEST = float(kp.bf16_value(np.array([0x7F7F], np.uint16))[0])
+
+
+def spread(d, weights, dtype):
+    """Rows whose softmax weights relative to the first token's are 2^weights (d features, one query head): keys of one feature."""
+    q = np.zeros(d)
+    q[0] = 1.0
+    rows = Rows("bf16", d, len(weights), q, dtype, scale=float(np.log(2.0)))
+    for t, w in enumerate(weights):
+        k = np.zeros(d)
+        k[0] = w
+        rows.values(0, t, k)
+        rows.values(1, t, 0.0)
+    return rows
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("weight,value,keeps", [(-300, LARGEST, False), (-300, -LARGEST, False), (-1000, LARGEST, False), (-118, 2.0 ** 120, True), (-110, -2.0 ** 112, True), (-20, 2.0 ** 30, True)])
+def test_a_large_value_counts_by_its_weight(dtype, d, weight, value, keeps):
+    """A token whose weight is zero in fp32 counts for nothing, whatever its finite value; one of small weight for what it is.  Parts of a probability may be off by 2^-133 each in place of zero."""
+    rows = spread(d, [0, weight, -3], dtype)
+    rows.values(1, 0, 1.0)
+    rows.values(1, 1, value)
+    want, want_lse = kp.attend(rows.q, rows.held(0), rows.held(1), rows.scale)
+    assert (abs(want[0, 0] - 1 / 1.125) > 0.5) == keeps
+    tol, tol_lse = kp.attend_bound(rows.q, rows.held(0), rows.held(1), np.abs(rows.held(0)), np.abs(rows.held(1)), rows.scale, 17 if dtype == kv.KVTC_BF16 else 22, 8 if dtype == kv.KVTC_BF16 else 22)
+    out, lse = rows.run()
+    assert (np.abs(out - want) <= tol + (2 * 2.0 ** -133 * abs(value) if keeps else 0.0)).all(), (out[0, 0], want[0, 0])
+    assert np.abs(lse - want_lse).max() <= tol_lse.max()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("weight", [0, -1, -7, -10.5, -100, -120])
+def test_an_infinite_value_stays_one(dtype, d, weight):
+    """Whether its probability has parts of zero (powers of two) or not, in its own feature alone; two of opposite signs are none, and nor is one of no weight."""
+    rows = spread(d, [0, weight, -300], dtype)
+    v = np.ones(d)
+    v[3], v[d - 1], v[9] = np.inf, -np.inf, np.inf
+    rows.values(1, 1, v)
+    v[:] = 1.0
+    v[9] = -np.inf
+    rows.values(1, 0, v)
+    v[:] = 1.0
+    v[20] = np.inf
+    rows.values(1, 2, v)
+    out, lse = rows.run()
+    assert np.isposinf(out[0, 3]) and np.isneginf(out[0, d - 1]) and np.isnan(out[0, 9]) and np.isnan(out[0, 20])
+    rest = np.delete(out[0], [3, 9, 20, d - 1])
+    assert (np.abs(rest - 1.0) <= 2.0 ** -8).all() and np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("up", [-105, -97, -60, 60, 100])
+def test_fp32_queries_of_any_magnitude(d, up):
+    """Queries of 2^up over bf16 pages, the keys as much the other way; scores are as ever, and so is their precision."""
+    rng = np.random.default_rng(d + up + 200)
+    n = 77
+    rows = Rows("bf16", d, n, rng.standard_normal((4, d)) * 2.0 ** up, kv.KVTC_F32, scale=d ** -0.5)
+    rows.q[0, ::2] = np.float32(2.0 ** up)                       # (parts of zero)
+    for t in range(n):
+        rows.values(0, t, rng.standard_normal(d) * 4 * 2.0 ** -up)
+        rows.values(1, t, rng.standard_normal(d))
+    args = rows.q, rows.held(0), rows.held(1)
+    want, want_lse = kp.attend(*args, rows.scale)
+    tol, tol_lse = kp.attend_bound(*args, np.abs(args[1]), np.abs(args[2]), rows.scale, 22, 22)
+    out, lse = rows.run()
+    assert (np.abs(out - want) <= tol).all(), np.abs((out - want) / tol).max()
+    assert (np.abs(lse - want_lse) <= tol_lse).all()
