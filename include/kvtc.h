@@ -505,7 +505,7 @@ kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, i
  *   status_dev    as above: 1 + the lowest sequence whose length is negative or above max_tokens (its rows become 0 and minus infinity) or
  *                 one of whose pages with seen tokens is not in the pool (those tokens are not seen)
  * Sums and softmax statistics are fp32, products of bf16 values and codes are exact in them; probabilities enter their
- * product with the values as two bf16 parts (16 bits, of codes 18), for fp32 queries and outputs as three (24 bits), queries as one or three.
+ * product with the values as three bf16 parts (24 bits; with bf16 outputs and 4-bit codes as two, 18 bits), fp32 queries as three.
  * The result is rounded once to dtype.  A fixed split and order of summation: results are reproducible.
  * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 is a no-op.
  */

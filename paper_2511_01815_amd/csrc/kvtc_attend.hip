@@ -27,9 +27,10 @@
 // high code of a byte, where it stands, is 16 of them.  Scores: per group a product of its own, times the token's scale, plus the query's sum times its shift.  Values:
 // per group the probabilities times the tokens' scales; low codes, and whole bytes, low + 16 high, from which the low ones' sums are taken in the end; shifts by
 // sums apart.  (With 128 + code from an or, and the 128s taken off by products of their own: 16 rows of 32768 tokens 164 us for 153, with fp32 queries 245 for 199.)
-// Probabilities have 24 bits and their operand 8: they enter as a sum of two operands (fp32 outputs: three).  Of codes both of two are rounded to nearest, 18 bits in all: in 4 bits the error is
-// one of code * scale, which may be far larger than the value.  Of bf16 values, which may be infinite, parts are cut towards zero so that they have one sign, 16 bits, and none is zero, so that an
-// infinite value stays one; where its probability is zero, e^-88 and less in fp32, it makes NaN, as zero times infinity does.
+// Probabilities have 24 bits and their operand 8: they enter as a sum of three operands.  In 4 bits with bf16 outputs, where the vector unit has no time to spare, of two, both to nearest, 18 bits: the error
+// is one of code * scale, larger than the value where a group lies around zero, but 32 times below the output's rounding.  (16 rows of 32768 tokens 154 us with two and 161 with three, head-major pages 144 and 154;
+// in bf16 64 ragged rows 206.4 and 207.0, in 8 bits 212 and 210.)  With bf16 values, which may be infinite, all parts have one sign and none is zero, so that an infinite value stays one; where its
+// probability is zero, e^-88 and less in fp32, it makes NaN, as zero times infinity does.
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
@@ -104,13 +105,14 @@ __device__ __forceinline__ uint32_t round_pair(float first, float second) {
 }
 __device__ __forceinline__ float half_of(uint32_t w, int high) { return (float)__builtin_bit_cast(_Float16, (uint16_t)(high ? w >> 16 : w)); }
 
-// Eight values as a sum of PARTS operands.  (Two parts: nearest first, within 2^-18, or, with one sign, within 2^-16; three: all 24 bits, of values of at least 2^-109.)
+// Eight values as a sum of PARTS operands.  (Two parts, each to nearest: within 2^-18; three: all 24 bits, of values of at least 2^-109.)
 // One sign, for what goes with bf16 features, which may be infinite: all parts have the value's sign, and none is zero where the value is not, lest an infinity times zero make NaN of another part's
 // infinity.  The least part that there is, 2^-133, is below what a probability may be off by in fp32 (2^-126), whatever feature it meets; a value of zero has parts of zero.
 enum class Signs { kAny, kOne, kPositive };                // (kPositive: kOne of values that are not negative)
 template <int PARTS, Signs SIGNS>
 __device__ __forceinline__ void split(const float (&v)[8], bf16x8 (&out)[PARTS]) {
-    constexpr bool kNearest = PARTS == 2 && SIGNS == Signs::kAny;
+    static_assert(PARTS != 2 || SIGNS == Signs::kAny, "the second of two may have another sign");
+    constexpr bool kNearest = PARTS == 2;
     float rest[8];
     uint32_t w[4];
     auto first = [&](int i) { return !kNearest ? cut(v[i]) : __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); };
@@ -372,14 +374,14 @@ __device__ __forceinline__ void load_values(const Item& item, uint32_t ts, const
 
 // ---- queries and scores --------------------------------------------------------------------------------------------------------
 
-template <typename XT> struct Parts;
-template <> struct Parts<uint16_t> { static constexpr int q = 1, p = 2; };
-template <> struct Parts<float> { static constexpr int q = 3, p = 3; };
+// Operands of a query, and of a probability.
+template <typename XT> constexpr int query_parts() { return sizeof(XT) == 2 ? 1 : 3; }
+template <typename XT, int F> constexpr int probability_parts() { return sizeof(XT) == 2 && F == KVTC_CACHE_INT4 ? 2 : 3; }
 
 template <typename XT, int F, int D>
 struct Query {
     static constexpr int NK = D / 32;
-    bf16x8 w[NK][Parts<XT>::q];
+    bf16x8 w[NK][query_parts<XT>()];
     float factor;                                          // of a score
     float sum[F == KVTC_CACHE_INT4 ? NK : 1];              // 4 bits: of the query over a group
 };
@@ -437,11 +439,11 @@ __device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is,
                 out.sum[s] = __builtin_amdgcn_ldexpf(sum_over_quarters(sum), kCodeUnit);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = v[s][(i & 4) + (i & 1) * 2 + (i >> 1 & 1)] * (i & 2 ? 0.0625f : 1.0f);
-                split<Parts<XT>::q, Signs::kAny>(o, out.w[s]);
+                split<query_parts<XT>(), Signs::kAny>(o, out.w[s]);
             }
         } else {
 #pragma unroll
-            for (int s = 0; s < NK; ++s) split<Parts<XT>::q, F == KVTC_CACHE_BF16 ? Signs::kOne : Signs::kAny>(v[s], out.w[s]);
+            for (int s = 0; s < NK; ++s) split<query_parts<XT>(), F == KVTC_CACHE_BF16 ? Signs::kOne : Signs::kAny>(v[s], out.w[s]);
         }
     }
 }
@@ -457,7 +459,7 @@ __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) { return __builtin_
 // Scores (without the query's factor) of the lane's query head and 8 tokens of its set's piece.
 template <typename XT, int F, int D, int J>
 __device__ __forceinline__ void scores(const Query<XT, F, D>& q, const Keys<F, D, J>& k, float (&s)[8]) {
-    constexpr int NK = D / 32, QP = Parts<XT>::q;
+    constexpr int NK = D / 32, QP = query_parts<XT>();
     const int set = set_of<J>(threadIdx.x & 15);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -524,7 +526,7 @@ __device__ __forceinline__ int feature_of(int i, int r, int quarter) {
 
 template <typename XT, int F, int D, bool IN_PAGE, int J>
 __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, J>& v, float (&s)[8], const Where<IN_PAGE> (&at)[J], float factor, const Constants& known) {
-    constexpr int NO = D / 16, G = D / 32, P = Parts<XT>::p;
+    constexpr int NO = D / 16, G = D / 32, P = probability_parts<XT, F>();
     const int quarter = (threadIdx.x & 63) >> 4, set = set_of<J>(threadIdx.x & 15);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] *= factor;

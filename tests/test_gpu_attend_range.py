@@ -58,19 +58,19 @@ def cut_error(p):
     return rest - kp.bf16_value(kp.bf16_bits(rest.astype(np.float32))).astype(np.float64)
 
 
-@pytest.mark.parametrize("fmt", ["fp8", "int4"])
+@pytest.mark.parametrize("fmt", ["bf16", "fp8", "int4"])
 @pytest.mark.parametrize("d", [64, 128, 256])
-def test_probabilities_of_codes_have_18_bits(fmt, d):
-    """Values that cancel, with probabilities that two parts cut towards zero would miss by nearly 2^-16 each, in one direction.  A probability is off by 2^-18 (two parts to nearest) and 2^-21 (the
-    exponential, the score), sums of n tokens by (n + 4) 2^-24 of their magnitudes (4 bits: whole bytes are 17 codes, of which a 16th counts), the result by bf16's rounding."""
+def test_probabilities_keep_their_bits(fmt, d):
+    """Values that cancel, with probabilities that two parts cut towards zero would miss by nearly 2^-16 each, in one direction.  A probability is off by nothing (three parts) or 2^-18 (4 bits: two parts
+    to nearest) and 2^-21 (the exponential, the score), sums of n tokens by (n + 4) 2^-24 of their magnitudes (4 bits: whole bytes are 17 codes, of which a 16th counts), the result by bf16's rounding."""
     x = np.arange(0.55, 0.69, 2.0 ** -11).astype(np.float16).astype(np.float64)
     p = np.exp(-x)
     err = cut_error(p)
     down = np.argsort(-err)[:3]                                  # too small by the most
     n = 7
     q = np.zeros(d)
-    q[0] = 1.0
-    rows = Rows(fmt, d, n, q, kv.KVTC_BF16)
+    q[:3] = 1.0, 2.0 ** -8, 2.0 ** -16
+    rows = Rows(fmt, d, n, q if fmt == "bf16" else q * (q == 1.0), kv.KVTC_BF16)
     weight = np.ones(n)
     if fmt == "int4":
         assert (err[down] > 0.8 * 2.0 ** -17).all()
@@ -79,23 +79,32 @@ def test_probabilities_of_codes_have_18_bits(fmt, d):
             rows.codes(0, t, 0, 0.0, 0.0 if t == 0 else -x[i])
             rows.codes(1, t, *((0, 0.0) if t == 0 else (15, 1.0) if t % 2 else (0, 0.0, -15.0)))
             weight[t] = 1.0 if t == 0 else p[i]
-        size = 17.0 * weight[1::2].sum(), 32.0 * weight[1::2].sum()
+        off = 2.0 ** -18 * 17.0 * weight[1::2].sum()
+        size = 32.0 * weight[1::2].sum()
     else:
         fine = x[down][:, None] + np.arange(-400, 400) * 2.0 ** -20      # near each, one too small by about as much and one too large
         e = cut_error(np.exp(-fine))
+        assert (e.max(1) > 0.8 * 2.0 ** -17).all() and (e.min(1) < -0.8 * 2.0 ** -17).all()
         pairs = [(fine[k, e[k].argmax()], fine[k, e[k].argmin()]) for k in range(3)]
         for t in range(n):
-            if t:
-                at = pairs[(t - 1) // 2][(t - 1) % 2]
-                weight[t] = np.exp(-np.float64(np.float32(at)))
-            rows.codes(0, t, -1.0 if t else 0.0, np.float32(at) if t else 1.0)
-            rows.codes(1, t, 0.0 if t == 0 else 1.0 if t % 2 else -1.0, 1.0)
-        assert (e.max(1) > 0.8 * 2.0 ** -17).all() and (e.min(1) < -0.8 * 2.0 ** -17).all()
-        size = weight[1:].sum(), weight[1:].sum()
+            at, sign = (pairs[(t - 1) // 2][(t - 1) % 2], 1.0 if t % 2 else -1.0) if t else (0.0, 0.0)
+            weight[t] = np.exp(-at)
+            if fmt == "fp8":
+                rows.codes(0, t, -1.0 if t else 0.0, np.float32(at) if t else 1.0)
+                rows.codes(1, t, sign, 1.0)
+            else:                                                # a key of 20 bits by three features of 8
+                k = np.zeros(d)
+                for i in range(3):
+                    k[i] = np.trunc(-at * 2.0 ** (8 * i + 8)) / 256.0
+                    at += k[i] * 2.0 ** (-8 * i)
+                assert at == 0.0
+                rows.values(0, t, k)
+                rows.values(1, t, sign)
+        off, size = 0.0, weight[1:].sum()
     want, want_lse = kp.attend(rows.q, rows.held(0), rows.held(1), 1.0)
     np.testing.assert_allclose(want_lse, np.log(weight.sum()), rtol=1e-6)
     out, lse = rows.run()
-    tol = ((2.0 ** -18 + 2.0 ** -21) * size[0] + (n + 4) * 2.0 ** -24 * size[1]) / weight.sum() + 2.0 ** -9 * np.abs(want)
+    tol = (off + (2.0 ** -21 + (n + 4) * 2.0 ** -24) * size) / weight.sum() + 2.0 ** -9 * np.abs(want)
     assert (np.abs(out - want) <= tol).all(), (np.abs(out - want).max(), tol.min())
 
 
