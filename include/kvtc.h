@@ -506,6 +506,9 @@ kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, i
  *                 one of whose pages with seen tokens is not in the pool (those tokens are not seen)
  * Sums and softmax statistics are fp32, products of bf16 values and codes are exact in them; probabilities enter their
  * product with the values as three bf16 parts (24 bits; with bf16 outputs and 4-bit codes as two, 18 bits), fp32 queries as three.
+ * Sums run over codes before a row's scale is applied: with 8 bits, queries times 448 d_head, and with 4 bits, queries times
+ * scale times 2^14, must not pass fp32's range; fp32 queries over bf16 and 8-bit pages keep 24 bits from magnitudes of 2^-109 on.  A token whose weight
+ * e^(s_t) is below about 2^-126 of the largest has none: a finite value counts for nothing then, an infinite one makes NaN.
  * The result is rounded once to dtype.  A fixed split and order of summation: results are reproducible.
  * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 is a no-op.
  */

@@ -400,7 +400,8 @@ __device__ __forceinline__ void load_query(const XT* q, RawQuery<XT, D>& out) {
     }
 }
 // 4 bits: a code as it stands is the bf16 pattern of code * 2^-133, a number below the normal ones, which the matrix unit takes for what it is; so is the whole byte of two codes, of low + 16 high.
-// The query is multiplied by 2^up, its largest magnitude to 2^64 (which a score's factor makes good; the factor itself stays finite), and odd features by 1 / 16.
+// The query is multiplied by 2^up, its largest magnitude to 2^120, so that sums of a group stay finite, and odd features by 1 / 16.  The factor of a score makes that good, and has to stay finite itself:
+// 2^up is no less than it needs, which is too much only for queries whose product with the factor passes 2^114.
 constexpr int kCodeUnit = -133;
 constexpr float kUp = 0x1p60f;                             // of probabilities times scales
 template <typename XT, int F, int D>
@@ -428,7 +429,8 @@ __device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is,
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(v[s][i]));
             top = max_over_quarters(top);
-            const int up = max(9, 64 + 127 - (int)(__float_as_uint(top) >> 23));
+            auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23 & 255u) - 127; };
+            const int up = max(exponent(factor) + 6, 119 - exponent(top));
             out.factor = __builtin_amdgcn_ldexpf(factor, -kCodeUnit - up);
 #pragma unroll
             for (int s = 0; s < NK; ++s) {

@@ -179,3 +179,33 @@ def test_fp32_queries_of_any_magnitude(d, up):
     out, lse = rows.run()
     assert (np.abs(out - want) <= tol).all(), np.abs((out - want) / tol).max()
     assert (np.abs(lse - want_lse) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("up,scale_up", [(119, -119), (126, -110), (126, -40), (80, 0), (60, 6), (60, 20), (-60, 60), (-126, 120)])
+def test_four_bit_queries_of_any_magnitude(dtype, d, up, scale_up):
+    """A feature of 2^up, where all keys are zero, and others whose scores are as ever, with scales of 2^scale_up: the first one, up to 2^86 times the others, takes no bits of theirs."""
+    rng = np.random.default_rng(d + up + 200)
+    n = 77
+    q = rng.standard_normal((4, d)) * 2.0 ** -scale_up
+    q[:, 0] = 2.0 ** up
+    rows = Rows("int4", d, n, q, dtype, scale=d ** -0.5 * 2.0 ** scale_up)
+    for t in range(n):
+        for side in range(2):
+            k = rng.standard_normal(d) * 4
+            if side == 0:
+                k[:32] = 1.0                                     # (the first group's range begins at zero)
+                k[0] = 0.0
+            bytes_, scales = kp.quantise(k.astype(np.float32), "int4")
+            r, s = rows.pool.at(t, 0)
+            rows.pool.bytes[side][r:r + len(bytes_)], rows.pool.scales[side][s:s + len(scales)] = bytes_, scales
+    (kr, ks), (vr, vs) = rows.pool.rows(0, range(n), 0), rows.pool.rows(1, range(n), 0)
+    k, v = rows.held(0), rows.held(1)
+    assert (k[:, 0] == 0.0).all()
+    sizes = kp.sizes(kr, ks, "int4", d)
+    sizes[:, 0] = 0.0
+    want, want_lse = kp.attend(rows.q, k, v, rows.scale)
+    tol, tol_lse = kp.attend_bound(rows.q, k, v, sizes, kp.sizes(vr, vs, "int4", d), rows.scale, 17 if dtype == kv.KVTC_BF16 else 22, 8 if dtype == kv.KVTC_BF16 else 22)
+    out, lse = rows.run()
+    assert (np.abs(out - want) <= tol).all() and (np.abs(lse - want_lse) <= tol_lse).all()
