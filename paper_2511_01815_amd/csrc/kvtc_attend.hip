@@ -1102,7 +1102,7 @@ static void launch_kernel(const AttendPlan& p, const Shares& s, hipStream_t stre
 }
 template <typename XT, int F, int D, bool IN_PAGE, int J>
 static void launch_shares(const AttendPlan& p, const Shares& s, hipStream_t stream) {
-    constexpr int most = heads_to_a_line(F, D, IN_PAGE);
+    constexpr int most = J == 1 && two_pieces(F, sizeof(XT) == 2, D, IN_PAGE) ? 1 : heads_to_a_line(F, D, IN_PAGE);
     if constexpr (most >= 4) { if (s.next == 4) return launch_kernel<XT, F, D, IN_PAGE, J, 4>(p, s, stream); }
     if constexpr (most >= 2) { if (s.next == 2) return launch_kernel<XT, F, D, IN_PAGE, J, 2>(p, s, stream); }
     launch_kernel<XT, F, D, IN_PAGE, J, 1>(p, s, stream);
@@ -1176,7 +1176,8 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     const int64_t items = rows / s.next;
     // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 9.5 and 12.5, of 4096
     // 12.6 and 11.3; 16 of 32768 178 and 153)
-    s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && pieces * rows >= 2 * places ? 2 : 1;
+    // (several KV heads to an item, of a large call, always have: for these there is no kernel of one)
+    s.pieces = !s.rows && two_pieces(c.format, bf16, c.d_head, c.page_tokens % 16 == 0) && cols <= kAttendCols / 2 && (s.next > 1 || pieces * rows >= 2 * places) ? 2 : 1;
     const int64_t tile = 4 / s.next * s.pieces, tiles = (pieces + tile - 1) / tile, most = places < kAttendMaxShares ? places : kAttendMaxShares;
     const __int128 all = (__int128)tiles * items;
     s.n = (int)(s.rows ? rows : all < most ? (int64_t)all : most);

@@ -43,3 +43,18 @@ def test_refusals_of_the_route():
     f, got = kv.lib().kvtc_host_attend_route, (C.c_int32 * 5)()
     assert f(C.byref(c), 2, 1, 8, 100, 0, 0, got) == 1 and f(C.byref(c), 0, 1, 6, 100, 0, 0, got) == 1 and f(C.byref(c), 0, 1, 8, 100, -1, 0, got) == 1 and f(C.byref(c), 0, 1, 8, 100, 0, 0, None) == 1
     assert f(C.byref(c), 0, 65536, 8, 1 << 23, 0, 0, got) == 2 and f(None, 0, 1, 8, 100, 0, 0, got) == 1
+
+
+def test_several_heads_to_a_workgroup_take_two_pieces_where_any_do():
+    """Of 4 bits with bf16 queries there is no kernel of several heads and one piece to a step; the others have one piece only."""
+    seen = set()
+    for fmt, dtype in (("int4", kv.KVTC_BF16), ("int4", kv.KVTC_F32), ("fp8", kv.KVTC_BF16)):
+        for d in (64, 128):
+            for heads, group in ((2, 1), (2, 8), (4, 3), (8, 2), (16, 1), (64, 5), (1024, 1)):
+                for n_seqs in (1, 3, 24, 48, 256, 4096, 65536):
+                    for max_tokens in (1, 33, 700, 2048, 4097, 16384, 33000):
+                        for sinks, window in ((0, 0), (4, 128), (1000, 3000)):
+                            r = route(cache_of(fmt, heads, d, 16), dtype, n_seqs, heads * group, max_tokens, sinks, window)
+                            assert r["next"] == 1 or not r["rows"] and r["pieces"] == (2 if (fmt, dtype) == ("int4", kv.KVTC_BF16) else 1), (fmt, dtype, d, heads, group, n_seqs, max_tokens, r)
+                            seen.add((fmt, dtype, d, r["next"], r["pieces"]))
+    assert {(f, t, d, n) for f, t, d, n, _ in seen if n > 1} == {("int4", t, d, n) for t in (kv.KVTC_BF16, kv.KVTC_F32) for d, n in ((64, 2), (64, 4), (128, 2))} | {("fp8", kv.KVTC_BF16, 64, 2)}
