@@ -403,6 +403,9 @@ __device__ __forceinline__ void load_query(const XT* q, RawQuery<XT, D>& out) {
 // The query is multiplied by 2^up, its largest magnitude to 2^120, so that sums of a group stay finite, and odd features by 1 / 16.  The factor of a score makes that good, and has to stay finite itself:
 // 2^up is no less than it needs, which is too much only for queries whose product with the factor passes 2^114.
 constexpr int kCodeUnit = -133;
+// Low codes as operands of the values' products: where they stand, or, for fp32 outputs, 16 of them.  (The matrix unit aligns products by their exponents as they are written, and cuts below; a number that begins
+// lower down in its pattern has fewer bits.  16 rows of 32768 tokens, fp32: 2.0e-6 off, relative, and 1.2e-6, 208 us and 212; of bf16 outputs that is far below the rounding.)
+template <typename XT> constexpr float low_code_up() { return sizeof(XT) == 2 ? 1.0f : 16.0f; }
 constexpr float kUp = 0x1p60f;                             // of probabilities times scales
 template <typename XT, int F, int D>
 __device__ __forceinline__ void to_operands(const RawQuery<XT, D>& raw, bool is, float factor, Query<XT, F, D>& out) {
@@ -526,6 +529,10 @@ __device__ __forceinline__ int feature_of(int i, int r, int quarter) {
     return F == KVTC_CACHE_INT4 ? i / 2 * 32 + 2 * c + i % 2 : c * (D / 16) + i;
 }
 
+// What a step's products begin with.  They are added to the running sums by the vector unit, which rounds to nearest: the matrix unit cuts, product by product, what lies below the last bit of the largest it adds, so
+// that sums over many steps that grow in there come out too small.  (Relative, fp32, 16 rows of 32768 tokens: 4 bits 2.4e-5 so, 1.9e-6 with sums of its own for every step; positive values in bf16 and 8 bits 1.1e-6
+// and 0.7e-7.  64 ragged rows in bf16 207.4 us both, 16 of 32768 tokens in 8 bits 210.5 and 209.5, in 4 bits 153.6 and 154.3, fp32 201 and 208.)
+constexpr f32x4 kNothing = {0.0f, 0.0f, 0.0f, 0.0f};
 template <typename XT, int F, int D, bool IN_PAGE, int J>
 __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, J>& v, float (&s)[8], const Where<IN_PAGE> (&at)[J], float factor, const Constants& known) {
     constexpr int NO = D / 16, G = D / 32, P = probability_parts<XT, F>();
@@ -576,22 +583,25 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             __builtin_amdgcn_sched_barrier(0);             // (one group after the other: all at once, the unpacked codes do not fit the registers, 330 us for 153)
-            float ps[8];
+            float ps[8], shifts = known.zero;                // (of the step: one rounding less for the running sums in eight.  fp32, as above, 1.2e-6 off, and 0.8e-6)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t header = v.scale[i][g];
                 ps[i] = __builtin_fmaf(half_of(header, 1), up[i], known.zero);
-                run.low[g] = __builtin_fmaf(half_of(header, 0), p[i], run.low[g]);
+                shifts = __builtin_fmaf(half_of(header, 0), p[i], shifts);
             }
+            run.low[g] += shifts;
             bf16x8 b[P];
             split<P, Signs::kAny>(ps, b);
+            constexpr float kLowUp = low_code_up<XT>();
+            f32x4 low_now = kNothing, both_now = kNothing;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 uint32_t low[4], both[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     both[i] = bytes_of(v.w[j][2 * i][g / 4], v.w[j][2 * i + 1][g / 4], g % 4, g % 4);
-                    low[i] = both[i] & 0x000f000fu;
+                    low[i] = kLowUp == 16.0f ? both[i] << 4 & 0x00f000f0u : both[i] & 0x000f000fu;
                 }
 #pragma unroll
                 for (int i = P - 1; i >= 0; --i) {
@@ -600,10 +610,12 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
 #pragma unroll
                         for (int k = 0; k < 4; ++k) own[k] = set == j ? own[k] : 0u;
                     }
-                    run.o[2 * g] = mfma(operand(low[0], low[1], low[2], low[3]), __builtin_bit_cast(bf16x8, own), run.o[2 * g]);
-                    run.o[2 * g + 1] = mfma(operand(both[0], both[1], both[2], both[3]), __builtin_bit_cast(bf16x8, own), run.o[2 * g + 1]);
+                    low_now = mfma(operand(low[0], low[1], low[2], low[3]), __builtin_bit_cast(bf16x8, own), low_now);
+                    both_now = mfma(operand(both[0], both[1], both[2], both[3]), __builtin_bit_cast(bf16x8, own), both_now);
                 }
             }
+            run.o[2 * g] += low_now;
+            run.o[2 * g + 1] += both_now;
         }
     } else {
         if constexpr (F == KVTC_CACHE_FP8) {
@@ -618,8 +630,10 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
                 uint32_t w[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[k] = i % 2 ? high_halves(v.w[0][2 * k][i / 2], v.w[0][2 * k + 1][i / 2]) : low_halves(v.w[0][2 * k][i / 2], v.w[0][2 * k + 1][i / 2]);
+                f32x4 now = kNothing;
 #pragma unroll
-                for (int k = P - 1; k >= 0; --k) run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
+                for (int k = P - 1; k >= 0; --k) now = mfma(operand(w[0], w[1], w[2], w[3]), b[k], now);
+                run.o[i] += now;
             }
         } else {
 #pragma unroll
@@ -631,11 +645,14 @@ __device__ __forceinline__ void add_tokens(Running<XT, F, D>& run, Values<F, D, 
                     w[k] = e4m3_to_bf16<false>(u);
                     x[k] = e4m3_to_bf16<true>(u);
                 }
+                f32x4 now = kNothing, next = kNothing;
 #pragma unroll
                 for (int k = P - 1; k >= 0; --k) {
-                    run.o[i] = mfma(operand(w[0], w[1], w[2], w[3]), b[k], run.o[i]);
-                    run.o[i + 1] = mfma(operand(x[0], x[1], x[2], x[3]), b[k], run.o[i + 1]);
+                    now = mfma(operand(w[0], w[1], w[2], w[3]), b[k], now);
+                    next = mfma(operand(x[0], x[1], x[2], x[3]), b[k], next);
                 }
+                run.o[i] += now;
+                run.o[i + 1] += next;
             }
         }
     }
@@ -653,7 +670,7 @@ __device__ __forceinline__ void settle(Running<XT, F, D>& run) {
             const float shift = sum_over_quarters(run.low[g]);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float low = run.o[2 * g][r], high = (run.o[2 * g + 1][r] - low) * 0.0625f;
+                const float low = run.o[2 * g][r] * (1.0f / low_code_up<XT>()), high = (run.o[2 * g + 1][r] - low) * 0.0625f;
                 run.o[2 * g][r] = __builtin_fmaf(low, kUnit, shift);
                 run.o[2 * g + 1][r] = __builtin_fmaf(high, kUnit, shift);
             }

@@ -209,3 +209,41 @@ def test_four_bit_queries_of_any_magnitude(dtype, d, up, scale_up):
     tol, tol_lse = kp.attend_bound(rows.q, k, v, sizes, kp.sizes(vr, vs, "int4", d), rows.scale, 17 if dtype == kv.KVTC_BF16 else 22, 8 if dtype == kv.KVTC_BF16 else 22)
     out, lse = rows.run()
     assert (np.abs(out - want) <= tol).all() and (np.abs(lse - want_lse) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("fmt,d", [("bf16", 64), ("bf16", 128), ("fp8", 128), ("fp8", 256), ("int4", 64), ("int4", 128), ("int4", 256)])
+def test_sums_over_long_rows_are_not_cut(fmt, d):
+    """1024 sequences over the same 131072 tokens, positive values: a wave adds up a thousand pieces of 32 tokens.  A piece's sums, in the matrix unit, are off by 128 2^-24 of themselves at most, and
+    adding t of them, each rounded to nearest, by t 2^-24, outputs and weights alike; of 4 bits, codes and shifts apart.  Such roundings average out: of t with an error spread evenly over an ulp (2^-24.8 at most),
+    of sums that grow evenly, in four waves, sqrt(t / 3) / 2 are left, and five times that is the bound of the features' mean.  (A matrix unit that adds to sums as large cuts off what does not reach their last bit.)"""
+    n, n_seqs, page = 131072, 1024, 64
+    rng = np.random.default_rng(d)
+    pool = Pool(fmt, n // page, page, 1, d)
+    for side in range(2):
+        x = rng.standard_normal((n, d)).astype(np.float32)
+        rows, scales = kp.quantise(np.abs(x) + np.float32(0.25) if side else x, fmt)
+        pool.bytes[side][:] = rows.reshape(-1)
+        if pool.scale:
+            pool.scales[side][:] = scales.reshape(-1)
+    cache = pool.upload()
+    q = rng.standard_normal((n_seqs, d)).astype(np.float32)
+    qd = torch.from_numpy(q).to(DEV)
+    pages = torch.from_numpy(np.tile(rng.permutation(n // page).astype(np.int32), (n_seqs, 1))).to(DEV)
+    work = Work.get(kv.kvtc_attend_work_bytes(cache, n_seqs, 1, n))
+    out, lse = torch.empty_like(qd), torch.empty((n_seqs, 1), device=DEV)
+    kv.kvtc_attend(cache, qd, kv.KVTC_F32, n_seqs, 1, d, d, pages, pages.shape[1], torch.full((n_seqs,), n, dtype=torch.int32, device=DEV), n, d ** -0.5, 0, 0, out, lse, work, work.numel())
+    torch.cuda.synchronize()
+    (kr, ks), (vr, vs) = [pool.rows(side, range(n), 0) for side in range(2)]
+    k, v = kp.values(kr, ks, fmt, d), kp.values(vr, vs, fmt, d)
+    sizes, t = np.abs(v), n // 32 // 4
+    if fmt == "int4":                                            # codes and shifts apart
+        shift = np.repeat(np.ascontiguousarray(vs).view(np.float16).astype(np.float64).reshape(n, -1, 2)[..., 0], kp.GROUP, axis=-1)
+        sizes = np.abs(shift) + (v - shift)
+    off = 2 * (t + 128) * 2.0 ** -24 + 2.0 ** -19                # (2^-19: scores and exponentials)
+    for b in (0, 1, 500, 1023):
+        want, want_lse = kp.attend(q[b:b + 1], k, v, d ** -0.5)
+        size = kp.attend(q[b:b + 1], k, sizes, d ** -0.5)[0]
+        err = (out[b].double().cpu().numpy() - want[0]) / size[0]
+        assert np.abs(err).max() <= off
+        assert abs(err.mean()) <= 5 * np.sqrt(t / 3) / 2 * 2.0 ** -24.8, err.mean()
+        assert abs(lse[b, 0].item() - want_lse[0]) <= off + 2.0 ** -21 * abs(want_lse[0])
