@@ -918,7 +918,7 @@ __device__ __forceinline__ void attend_tiles(const AttendPlan& p, int b, const H
 
 // Workgroups go to the eight XCDs in turn.  Each XCD takes neighbouring shares of n, the heads of a sequence one after another, so that where several heads' rows or scales are in one cache line its
 // L2 has it for all of them (24 rows of 12 heads of 64 features, 8 bits, token-major, 15.6 us, with the shares in turn 16.9; 64 ragged rows in bf16 206.6 and 208.7).  Of few long items the shares that read
-// the same tokens lie far apart; there they go in turn, which has them meet in an L2 where an item's shares are a multiple of eight.
+// the same tokens lie far apart; where an item's shares are a multiple of eight, they go in turn, which has them meet in an L2.
 __device__ __forceinline__ uint32_t neighbours_to_an_xcd(uint32_t block, uint32_t n) { return (block & 7u) * (n / 8) + min(block & 7u, n % 8) + block / 8; }
 
 // Long rows: shares of equal numbers of tiles, four waves to each.
@@ -1187,9 +1187,6 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     if (!s.rows && large)
         for (int n = to_a_line; n > 1 && s.next == 1; n /= 2)
             if (c.n_heads % n == 0 && n * cols <= kAttendCols && rows / n >= places / 8 && counted(n)) s.next = n;
-    // (one row of 131072 tokens, neighbours to an XCD and in turn: 4 bits of 8 heads of 128 61.6 and 54.4, 8 bits of 12 heads of 64 63.5 and 52.5; four rows of 32768 of 4 heads of 64 in 4 bits 23.0 and 21.3,
-    // five of 20000 23.5 and 26.8)
-    s.in_turn = s.next == 1 && to_a_line > 1 && rows <= 16;
     const int64_t items = rows / s.next;
     // two pieces to a step: two sets of the heads have to fit the columns, and a wave should have as much to do (us, one and two pieces: one row of 700 tokens of 8 heads 9.5 and 12.5, of 4096
     // 12.6 and 11.3; 16 of 32768 178 and 153)
@@ -1198,6 +1195,10 @@ static Shares shares_at_once(const kvtc_cache& c, bool bf16, int n_seqs, int par
     const int64_t tile = 4 / s.next * s.pieces, tiles = (pieces + tile - 1) / tile, most = places < kAttendMaxShares ? places : kAttendMaxShares;
     const __int128 all = (__int128)tiles * items;
     s.n = (int)(s.rows ? rows : all < most ? (int64_t)all : most);
+    // Few items whose rows share cache lines, each of a multiple of eight shares: in turn, the shares that read the same tokens are an XCD's.  (One row of 131072 tokens, us, neighbours to an XCD and in turn.  4 bits,
+    // heads of 128, two workgroups to a compute unit: 8 heads 62.3 and 55.8, 16 101 and 87, 2 45.8 and 46.5; 5, 10 and 12, no such multiples, 50.1 and 50.7, 73 and 75, 84 and 85.  8 bits, heads of 64, three: 3 heads 35.9 and
+    // 33.4, 8 55 and 42, 12 66 and 55, 16 84 and 67; 5, 7 and 10 43.1 and 43.1, 50.1 and 50.8, 61.3 and 61.8.  3 rows of 32768 of 4 heads 25.0 and 20.7; 3 of 20000 of 5 21.4 and 24.2, 5 of 30000 of 2 23.1 and 24.7.)
+    s.in_turn = s.next == 1 && to_a_line > 1 && rows <= 16 && s.n % (8 * rows) == 0;
     return s;
 }
 

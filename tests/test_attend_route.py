@@ -58,3 +58,18 @@ def test_several_heads_to_a_workgroup_take_two_pieces_where_any_do():
                             assert r["next"] == 1 or not r["rows"] and r["pieces"] == (2 if (fmt, dtype) == ("int4", kv.KVTC_BF16) else 1), (fmt, dtype, d, heads, group, n_seqs, max_tokens, r)
                             seen.add((fmt, dtype, d, r["next"], r["pieces"]))
     assert {(f, t, d, n) for f, t, d, n, _ in seen if n > 1} == {("int4", t, d, n) for t in (kv.KVTC_BF16, kv.KVTC_F32) for d, n in ((64, 2), (64, 4), (128, 2))} | {("fp8", kv.KVTC_BF16, 64, 2)}
+
+
+def test_shares_in_turn_only_where_the_same_tokens_fall_to_one_xcd():
+    """In turn, share i is XCD i % 8's: the shares of different heads that read the same tokens meet there where every item has a multiple of eight."""
+    seen = set()
+    for fmt, d, dtype in (("int4", 128, kv.KVTC_BF16), ("int4", 64, kv.KVTC_F32), ("fp8", 64, kv.KVTC_BF16)):
+        for heads in (1, 2, 3, 4, 5, 7, 8, 10, 12, 16, 24):
+            for n_seqs in (1, 2, 3, 5, 16):
+                for max_tokens in (700, 4096, 131072):
+                    r = route(cache_of(fmt, heads, d, 64), dtype, n_seqs, heads * 4, max_tokens)
+                    even = r["workgroups"] % (8 * heads * n_seqs) == 0
+                    assert not r["in_turn"] or even and r["next"] == 1 and heads * n_seqs <= 16, (fmt, d, heads, n_seqs, max_tokens, r)
+                    seen.add((r["in_turn"], even))
+                    assert not route(cache_of(fmt, heads, d, 64, "heads"), dtype, n_seqs, heads * 4, max_tokens)["in_turn"] or heads == 1
+    assert (1, True) in seen

@@ -70,3 +70,10 @@ def test_rows_of_a_thousand_tokens_by_single_waves(fmt, dtype, d, heads, group, 
     lengths[::12] = [513, 544, 545, 800, 841, 960, 991, 992, 993, 1023, 1024]
     case = Case(np.random.default_rng(d + group), fmt, d, heads, group, page, order, lengths, dtype, sinks, window)
     check(case, 1024, dict(rows=1, workgroups=len(lengths) * heads), only=list(range(0, 132, 12)) + [1, 2, 3])
+
+
+@pytest.mark.parametrize("fmt,dtype,d,heads,lengths", [("int4", BF16, 128, 8, [20000]), ("fp8", BF16, 64, 4, [9001, 0, 4097]), ("int4", F32, 64, 2, [0, 24601])])
+def test_shares_in_turn(fmt, dtype, d, heads, lengths):
+    """Few items of a multiple of eight shares, whose rows share cache lines."""
+    case = Case(np.random.default_rng(d + heads), fmt, d, heads, 2, 64, "tokens", lengths, dtype)
+    check(case, max(lengths), dict(rows=0, next=1, in_turn=1))
