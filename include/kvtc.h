@@ -444,9 +444,10 @@ kvtc_status kvtc_offsets_append(const kvtc_batch* batch, const kvtc_job* jobs_de
  *   KVTC_CACHE_FP8    d_head bytes of OCP E4M3 and an fp32 scale per row: scale = a * (1 / 448) for the row's largest
  *                     finite magnitude a (0 where that is below 2^-126; all codes are then 0 or NaN), code =
  *                     E4M3(x * (1 / scale)), to nearest even; infinities give +-448 and NaN stays NaN.  Value = code * scale.
- *   KVTC_CACHE_INT4   4-bit codes, and for every 32 features the coder's own header: fp16 shift (low half), fp16
+ *   KVTC_CACHE_INT4   4-bit codes, and for every 32 features a header like a record's: fp16 shift (low half), fp16
  *                     scale (high half), both and the codes decided as in a record's group of 4 bits (see above), but
- *                     the range is multiplied by fp32 1 / 15 where that divides it by 15; NaN gives an unspecified
+ *                     that the range is multiplied by fp32 1 / 15 where that divides it by 15, which leaves some scales (of bf16
+ *                     features one in twenty) the next fp16 number above a record's; NaN gives an unspecified
  *                     code.  Feature f's code is in byte (f % 32) / 2 * (d_head / 32) + f / 32 of the
  *                     row, the low four bits for even f.  Value = shift + code * scale.
  * Scales and headers are arrays of their own, [n_pages][n_heads][page_tokens] entries of kvtc_cache_scale_bytes.
@@ -496,7 +497,8 @@ kvtc_status kvtc_cache_read(const kvtc_cache* cache, const int64_t* slots_dev, i
  *                 n_q_heads a multiple of the cache's n_heads, at most 1024; n_seqs at most 65536
  *   pages_dev     page number of token t of sequence b: pages_dev[b * pages_stride + t / page_tokens] (device, int32);
  *                 entries beyond a sequence's last token, or of pages without a seen token, are not looked at
- *   lengths_dev   tokens per sequence (device, int32), at most max_tokens, the host's bound for sizing the launch;
+ *   lengths_dev   tokens per sequence (device, int32), at most max_tokens, the host's bound for sizing the launch and choosing the
+ *                 kernel (results do not depend on how close it is but for roundings; the time does, where rows are many and short);
  *                 pages_stride >= ceil(max_tokens / page_tokens), n_seqs * ceil(max_tokens / 128) below 2^31 (KVTC_E_UNSUPPORTED beyond)
  *   out_dev       [n_seqs][n_q_heads][d_head] of `dtype`, contiguous, 16-byte aligned; lse_dev [n_seqs][n_q_heads] fp32, or null
  *   work_dev      kvtc_attend_work_bytes(...) bytes of device memory, 256-byte aligned (work_bytes less: KVTC_E_SMALL), all zero

@@ -3,7 +3,7 @@
 // One pass over keys and values with the running maximum m and sum l of a softmax: for the scores s of some more tokens,
 //     m' = max(m, s),  l' = l e^(m - m') + sum e^(s - m'),  o' = o e^(m - m') + sum e^(s - m') v.
 // Bytes bound it: every key and value is used for the few query heads of its group only.  (64 ragged rows of 512 to 16384 tokens, 8 heads of 128 features, bf16:
-// 206 us for 1146 MB, 5.55 TB/s, the rate at which this card reads at all.  One row of 131072 tokens in 8 bits: 60.5 us, 4.6 TB/s.  4 bits: 16 rows of 32768 tokens 153 us, 4.2 TB/s, where the
+// 207 us for 1146 MB, 5.5 TB/s, the rate at which this card reads at all.  One row of 131072 tokens in 8 bits: 61.5 us, 4.5 TB/s.  4 bits: 16 rows of 32768 tokens 154 us, 4.2 TB/s, where the
 // vector unit's unpacking and scaling is in the way as well.)
 //
 // Work.  An item is (sequence, KV head, up to 16 of its query heads); its tokens come in tiles of four pieces of 32, one to a wave.  The tiles of all

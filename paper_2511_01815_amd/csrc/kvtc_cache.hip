@@ -7,8 +7,8 @@
 //          clamp(rne((x - shift) * (1/scale)), 0, 15); byte pair * (d/32) + group of the row has the codes of features 2 pair, 2 pair + 1 of the
 //          group, so that d/32 neighbouring bytes are of one pair (what the attention's matrix products take in one piece)
 // Streaming kernels, bound by memory: a lane has 8 neighbouring features (16 bytes of bf16) of ROWS rows, whose loads are on their way together; a row's d/8 lanes
-// find its extremes by lane exchanges.  32768 tokens of 8 heads of 128 bf16 features, 192 MB in all: into 8 bits 45 us, 4.5 TB/s (a copy of as much 43), out of 4 bits 40; one token 1.9, a
-// launch's time.
+// find its extremes by lane exchanges.  32768 tokens of 8 heads of 128 bf16 features, 192 MB in all: into 8 bits 45 us, 4.5 TB/s (a copy of as much 43), out of 4 bits 39.5; one token of each
+// of 64 caches 2.2, a launch's time (replayed from a graph; 5.4 a call where each is launched by itself).
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_numeric.h"
