@@ -445,7 +445,7 @@ def run(s):
     if op == "place":
         kv.kvtc_cache_place(s["seqs"], s["had"], s["new"], s["page"], s["table"], s["table"].shape[1], s["free"], s["n_free"], s["rows"], s["starts"], s["lengths"], s["left"], s["slots"],
                             s["positions"], s["status"])
-        return {"starts": s["starts"], "lengths": s["lengths"], "left": s["left"][0], "slots": s["slots"], "positions": s["positions"], "table": s["table"], "status": s["status"]}
+        return {"starts": s["starts"], "lengths": s["lengths"], "left": s["left"], "slots": s["slots"], "positions": s["positions"], "table": s["table"], "status": s["status"]}
     if op == "rope":
         wide = (s["heads"] + s["beside"]) * s["d"]
         kv.kvtc_rope_scaled(s["x"], s["out"], s["type"], s["tokens"], s["heads"], s["d"], wide, s["d"], s["heads"] * s["d"], s["d"], s["at"], s["first"], s["form"], s["inverse"])
