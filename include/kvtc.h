@@ -521,6 +521,92 @@ kvtc_status kvtc_attend(const kvtc_cache* cache, const void* q_dev, kvtc_dtype d
                         void* out_dev, float* lse_dev, void* work_dev, size_t work_bytes, uint32_t* status_dev,
                         kvtc_stream stream);
 
+/*
+ * ---- Many new tokens: places, positions, attention, joined parts ----------------------------
+ * What stands between a request and the live cache.  A batch holds the new tokens of several sequences one after another
+ * (prompts, parts of prompts, drafted tokens, single tokens, in any mixture): sequence b's are rows starts[b] .. starts[b + 1] - 1 of the batch.
+ *
+ * kvtc_cache_place works out on the GPU where they go.  Sequence b has lengths_dev[b] tokens, in the first ceil(lengths / page_tokens) pages of its
+ * row of the page table, and gets new_dev[b] more, at the positions that follow.  Pages beyond those that it has are taken from the end of the free
+ * list, sequence after sequence, each one's in the order of its tokens, and written into the table.
+ *   pages_dev       [n_seqs][pages_stride] int32: read where a sequence's last page has room, written where pages are added
+ *   free_dev        n_free_dev[0] page numbers (device, int32); the list itself is not changed
+ *   starts_dev      [n_seqs + 1] int32 out: running sums of new_dev, n_tokens at most
+ *   lengths_out_dev [n_seqs] out: lengths with the new tokens (may be lengths_dev);  n_free_out_dev [1] out: how many of the list are left (may be n_free_dev)
+ *   slots_dev       [n_tokens] int64 out, as kvtc_cache_write takes them (page * page_tokens + token in the page); positions_dev [n_tokens] int32 out, or null.
+ *                   Rows behind the last sequence (a padded batch) get slot -1 and position 0.
+ * A sequence that has no place -- a negative length or number, rows beyond n_tokens, more tokens than its row of the table holds, or
+ * pages than the list has left after the sequences before it -- keeps its length and takes no page, its rows get slot -1 and position 0, and *status_dev (device, may
+ * be null; the caller zeroes it) becomes 1 + the lowest such sequence.  Once the list does not do, no later sequence gets a page either; sequences that need none keep their places.
+ * Slots of pages that the table or the list gives as negative are -1.  n_seqs at most 65536.  One launch, or two; nothing else of the table is written.
+ */
+kvtc_status kvtc_cache_place(int n_seqs, const int32_t* lengths_dev, const int32_t* new_dev, int page_tokens, int32_t* pages_dev, int64_t pages_stride,
+                             const int32_t* free_dev, const int32_t* n_free_dev, int64_t n_tokens, int32_t* starts_dev, int32_t* lengths_out_dev,
+                             int32_t* n_free_out_dev, int64_t* slots_dev, int32_t* positions_dev, uint32_t* status_dev, kvtc_stream stream);
+
+/*
+ * Rotary positions of part of every head, with frequencies scaled for contexts longer than those that a model was trained on.  A form holds
+ * theta_j for the pairs j of the first n_rotated features of a head (which of these are pair j: as kvtc_rope, with n_rotated in place of d_head), from
+ * theta_j = base^(-2 j / n_rotated) by
+ *   KVTC_ROPE_SCALE_LINEAR  theta / factor (positions interpolated)
+ *   KVTC_ROPE_SCALE_BASE    base * factor^(n_rotated / (n_rotated - 2)) in place of base
+ *   KVTC_ROPE_SCALE_BANDS   by the turns t = original * theta / 2 pi over the original length: theta where t >= high, theta / factor where t <= low, between
+ *                           them (1 - s) theta / factor + s theta with s = (t - low) / (high - low)
+ *   KVTC_ROPE_SCALE_RAMP    by the pair's index: (1 - r) theta + r theta / factor, r = (j - first) / (last - first) within 0..1, where first and last are
+ *                           the pairs of `high` and of `low` turns over the original length, n ln(original / (2 pi turns)) / (2 ln base), rounded down and
+ *                           up and cut to 0 and n_rotated - 1
+ * factor is not looked at by KVTC_ROPE_SCALE_NONE, original, low and high only by the last two.  magnitude multiplies what is rotated (a factor of attention that goes with some
+ * scalings; 1 for none); undoing it divides.  kvtc_rope_form_init is host code; a form serves any number of calls.
+ *
+ * kvtc_rope_scaled turns x into out.  Element (token t, head h, feature f) is at x_dev[t * token_stride + h * head_stride + f], out_dev with strides of its own;
+ * heads and tokens must not overlap, in either order, as kvtc_rope.  Features beyond n_rotated are copied.  out_dev == x_dev with the same strides is in
+ * place; anything else must not overlap.  positions, dtype and inverse as kvtc_rope; d_head even, at most 256, n_heads at most 1024.  Angles, sines and cosines are
+ * double precision and rounded to fp32, the rotation is fp32 and rounded to dtype (nearest even).  Ordered on `stream`, allocates nothing, does not synchronise; n_tokens == 0 is a no-op.
+ */
+typedef enum { KVTC_ROPE_SCALE_NONE = 0, KVTC_ROPE_SCALE_LINEAR = 1, KVTC_ROPE_SCALE_BASE = 2, KVTC_ROPE_SCALE_BANDS = 3, KVTC_ROPE_SCALE_RAMP = 4 } kvtc_rope_scaling;
+typedef struct { int32_t n_rotated, pairing; double magnitude; double theta[128]; } kvtc_rope_form;
+kvtc_status kvtc_rope_form_init(kvtc_rope_form* out, int n_rotated, kvtc_rope_pairing pairing, double base, kvtc_rope_scaling scaling, double factor,
+                                double original, double low, double high, double magnitude);
+kvtc_status kvtc_rope_scaled(const void* x_dev, void* out_dev, kvtc_dtype dtype, int64_t n_tokens, int n_heads, int d_head, int64_t token_stride,
+                             int64_t head_stride, int64_t out_token_stride, int64_t out_head_stride, const int32_t* positions_dev, int64_t position0,
+                             const kvtc_rope_form* form, int inverse, kvtc_stream stream);
+
+/*
+ * Attention of the new tokens of every sequence over its pages (their own keys and values are in the cache already): kvtc_attend for any number of rows
+ * to a sequence.  Row i of sequence b, of its n = starts[b + 1] - starts[b], is at position lengths[b] - n + i.  If causal is 1 it sees the tokens up to its own, or, with a
+ * window, those t of them that are sinks (t < sinks) or among the last `window` (t > position - window); if 0 it sees all lengths[b] tokens (keys and values of
+ * another length: of an encoder, of a prefix that several sequences share, joined by kvtc_attend_join), and window must be 0.  A row that sees no token, or
+ * only scores of minus infinity, gives out = 0 and lse = minus infinity.  What lies in tokens that a row does not see is never part of its result, whatever it holds.
+ *   q_dev         [n_tokens][n_q_heads][d_head] of `dtype` with strides in elements (base and strides 16-byte aligned); n_q_heads a multiple of the cache's n_heads, at most 1024
+ *   starts_dev    [n_seqs + 1] int32, ascending, in 0..n_tokens (device).  Rows before the first sequence's and behind the last one's are left as they are.
+ *   pages_dev, pages_stride, lengths_dev, max_tokens, scale, sinks, window   as kvtc_attend
+ *   out_dev       [n_tokens][n_q_heads][d_head] of `dtype`, contiguous, 16-byte aligned; lse_dev [n_tokens][n_q_heads] fp32, or null
+ *   work_dev      kvtc_attend_many_work_bytes(...) bytes, 256-byte aligned (work_bytes less: KVTC_E_SMALL), all zero before its first use and left ready for the next: calls on one stream may
+ *                 share it, of any sizes that it is large enough for; calls that may overlap need one each
+ *   status_dev    (device, may be null; the caller zeroes it) 1 + the lowest sequence whose starts are not ascending or not in 0..n_tokens (its rows are left as they are), whose length is negative
+ *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen)
+ * n_tokens * n_q_heads at most 2^30 (KVTC_E_UNSUPPORTED beyond).
+ * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 or n_tokens == 0 is a no-op.
+ */
+size_t kvtc_attend_many_work_bytes(const kvtc_cache* cache, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens);     /* 0 for what kvtc_attend_many refuses */
+kvtc_status kvtc_attend_many(const kvtc_cache* cache, const void* q_dev, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t q_token_stride,
+                             int64_t q_head_stride, const int32_t* starts_dev, const int32_t* pages_dev, int64_t pages_stride, const int32_t* lengths_dev,
+                             int64_t max_tokens, float scale, int causal, int64_t sinks, int64_t window, void* out_dev, float* lse_dev, void* work_dev,
+                             size_t work_bytes, uint32_t* status_dev, kvtc_stream stream);
+
+/*
+ * Attention over several sets of tokens, each worked out by a call of its own (kvtc_attend, kvtc_attend_many), joined to attention over all of them:
+ *     out = sum_p e^(lse_p) out_p / sum_p e^(lse_p),   lse = log sum_p e^(lse_p)
+ *   part_outs    host array of n_parts (1..16) device pointers: [n_rows][n_heads][d_head] of part_dtype, contiguous, 16-byte aligned
+ *   part_lses    host array of n_parts device pointers: [n_rows][n_heads] fp32.  Where it is minus infinity, that row of the part is not part of the result, whatever it holds; rows with no
+ *                part give out = 0 and lse = minus infinity.
+ *   out_dev      [n_rows][n_heads][d_head] of out_dtype, 16-byte aligned; may be one of the parts, if the types are the same; lse_dev [n_rows][n_heads] fp32, or null; may be one of the parts'
+ *   d_head       64, 128 or 256 (KVTC_E_UNSUPPORTED otherwise)
+ * Weights and sums are fp32.  Ordered on `stream`, allocates nothing, does not synchronise; n_rows == 0 is a no-op.
+ */
+kvtc_status kvtc_attend_join(int n_parts, const void* const* part_outs, const float* const* part_lses, kvtc_dtype part_dtype, int64_t n_rows, int n_heads,
+                             int d_head, void* out_dev, kvtc_dtype out_dtype, float* lse_dev, kvtc_stream stream);
+
 /* Thread-local text for the last non-OK status returned on this thread (static storage). */
 const char* kvtc_last_error(void);
 

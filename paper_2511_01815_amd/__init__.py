@@ -20,6 +20,8 @@ from .binding import (  # noqa: F401
     kvtc_calib_block_errors, kvtc_calib_moments,
     KVTC_CACHE_BF16, KVTC_CACHE_FP8, KVTC_CACHE_INT4, KvtcCache, cache, kvtc_cache_row_bytes, kvtc_cache_scale_bytes,
     kvtc_cache_write, kvtc_cache_read, kvtc_attend_work_bytes, kvtc_attend,
+    kvtc_cache_place, KvtcRopeForm, rope_form, kvtc_rope_scaled, ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP,
+    kvtc_attend_many_work_bytes, kvtc_attend_many, kvtc_attend_join,
     KvtcLayout, layout, kvtc_encode_blocked, kvtc_decode_blocked, kvtc_encode_batch_blocked, kvtc_decode_batch_blocked,
 )
 from . import bundles  # noqa: F401

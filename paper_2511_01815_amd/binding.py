@@ -39,6 +39,10 @@ class KvtcCache(C.Structure):
                 ("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("k_scales_dev", C.c_void_p), ("v_scales_dev", C.c_void_p)]
 
 
+class KvtcRopeForm(C.Structure):
+    _fields_ = [("n_rotated", C.c_int32), ("pairing", C.c_int32), ("magnitude", C.c_double), ("theta", C.c_double * 128)]
+
+
 def lib_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), "libkvtc.so")
 
@@ -134,7 +138,15 @@ def lib() -> C.CDLL:
         L.kvtc_attend_work_bytes.argtypes = [cp, C.c_int, C.c_int, i64]
         L.kvtc_attend_work_bytes.restype = sz
         L.kvtc_attend.argtypes = [cp, vp, C.c_int, C.c_int, C.c_int, i64, i64, vp, i64, vp, i64, C.c_float, i64, i64, vp, vp, vp, sz, vp, vp]
-        for f in (L.kvtc_cache_write, L.kvtc_cache_read, L.kvtc_attend):
+        L.kvtc_cache_place.argtypes = [C.c_int, vp, vp, C.c_int, vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp]
+        fp = C.POINTER(KvtcRopeForm)
+        L.kvtc_rope_form_init.argtypes = [fp, C.c_int, C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double]
+        L.kvtc_rope_scaled.argtypes = [vp, vp, C.c_int, i64, C.c_int, C.c_int, i64, i64, i64, i64, vp, i64, fp, C.c_int, vp]
+        L.kvtc_attend_many_work_bytes.argtypes = [cp, C.c_int, i64, C.c_int, i64]
+        L.kvtc_attend_many_work_bytes.restype = sz
+        L.kvtc_attend_many.argtypes = [cp, vp, C.c_int, C.c_int, i64, C.c_int, i64, i64, vp, vp, i64, vp, i64, C.c_float, C.c_int, i64, i64, vp, vp, vp, sz, vp, vp]
+        L.kvtc_attend_join.argtypes = [C.c_int, vp, vp, C.c_int, i64, C.c_int, C.c_int, vp, C.c_int, vp, vp]
+        for f in (L.kvtc_cache_write, L.kvtc_cache_read, L.kvtc_attend, L.kvtc_cache_place, L.kvtc_rope_form_init, L.kvtc_rope_scaled, L.kvtc_attend_many, L.kvtc_attend_join):
             f.restype = C.c_int
         L.kvtc_last_error.argtypes = []
         L.kvtc_last_error.restype = C.c_char_p
@@ -390,6 +402,50 @@ def kvtc_attend(cache, q_dev, dtype: int, n_seqs: int, n_q_heads: int, q_seq_str
     _check(lib().kvtc_attend(C.byref(cache), _ptr(q_dev), dtype, n_seqs, n_q_heads, q_seq_stride, q_head_stride, _ptr(pages_dev),
                              pages_stride, _ptr(lengths_dev), max_tokens, scale, sinks, window, _ptr(out_dev), _ptr(lse_dev),
                              _ptr(work_dev), work_bytes, _ptr(status_dev), _stream(stream)))
+
+
+def kvtc_cache_place(n_seqs: int, lengths_dev, new_dev, page_tokens: int, pages_dev, pages_stride: int, free_dev, n_free_dev, n_tokens: int, starts_dev,
+                     lengths_out_dev, n_free_out_dev, slots_dev, positions_dev=None, status_dev=None, stream=None) -> None:
+    _check(lib().kvtc_cache_place(n_seqs, _ptr(lengths_dev), _ptr(new_dev), page_tokens, _ptr(pages_dev), pages_stride, _ptr(free_dev), _ptr(n_free_dev), n_tokens,
+                                  _ptr(starts_dev), _ptr(lengths_out_dev), _ptr(n_free_out_dev), _ptr(slots_dev), _ptr(positions_dev), _ptr(status_dev), _stream(stream)))
+
+
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDS, ROPE_SCALE_RAMP = range(5)
+
+
+def rope_form(n_rotated: int, pairing: int, base: float, scaling: int = ROPE_SCALE_NONE, factor: float = 1.0, original: float = 0.0, low: float = 0.0,
+              high: float = 0.0, magnitude: float = 1.0) -> "KvtcRopeForm":
+    """A kvtc_rope_form (kvtc_rope_form_init): the frequencies of a head's rotated features."""
+    form = KvtcRopeForm()
+    _check(lib().kvtc_rope_form_init(C.byref(form), n_rotated, pairing, base, scaling, factor, original, low, high, magnitude))
+    return form
+
+
+def kvtc_rope_scaled(x_dev, out_dev, dtype: int, n_tokens: int, n_heads: int, d_head: int, token_stride: int, head_stride: int, out_token_stride: int,
+                     out_head_stride: int, positions_dev, position0: int, form, inverse: bool = False, stream=None) -> None:
+    _check(lib().kvtc_rope_scaled(_ptr(x_dev), _ptr(out_dev), dtype, n_tokens, n_heads, d_head, token_stride, head_stride, out_token_stride, out_head_stride,
+                                  _ptr(positions_dev), position0, C.byref(form), 1 if inverse else 0, _stream(stream)))
+
+
+def kvtc_attend_many_work_bytes(cache, n_seqs: int, n_tokens: int, n_q_heads: int, max_tokens: int) -> int:
+    return lib().kvtc_attend_many_work_bytes(C.byref(cache), n_seqs, n_tokens, n_q_heads, max_tokens)
+
+
+def kvtc_attend_many(cache, q_dev, dtype: int, n_seqs: int, n_tokens: int, n_q_heads: int, q_token_stride: int, q_head_stride: int, starts_dev, pages_dev,
+                     pages_stride: int, lengths_dev, max_tokens: int, scale: float, causal: bool, sinks: int, window: int, out_dev, lse_dev, work_dev,
+                     work_bytes: int, status_dev=None, stream=None) -> None:
+    _check(lib().kvtc_attend_many(C.byref(cache), _ptr(q_dev), dtype, n_seqs, n_tokens, n_q_heads, q_token_stride, q_head_stride, _ptr(starts_dev), _ptr(pages_dev),
+                                  pages_stride, _ptr(lengths_dev), max_tokens, scale, 1 if causal else 0, sinks, window, _ptr(out_dev), _ptr(lse_dev), _ptr(work_dev),
+                                  work_bytes, _ptr(status_dev), _stream(stream)))
+
+
+def kvtc_attend_join(part_outs: Sequence, part_lses: Sequence, part_dtype: int, n_rows: int, n_heads: int, d_head: int, out_dev, out_dtype: int, lse_dev=None,
+                     stream=None) -> None:
+    n = len(part_outs)
+    if len(part_lses) != n:
+        raise ValueError(f"{n} parts with {len(part_lses)} log-sums")
+    outs, lses = (C.c_void_p * n)(*[_ptr(t) for t in part_outs]), (C.c_void_p * n)(*[_ptr(t) for t in part_lses])
+    _check(lib().kvtc_attend_join(n, outs, lses, part_dtype, n_rows, n_heads, d_head, _ptr(out_dev), out_dtype, _ptr(lse_dev), _stream(stream)))
 
 
 def kvtc_probe_stream(mode: int, src_dev, dst_dev, nbytes: int, stream=None) -> None:

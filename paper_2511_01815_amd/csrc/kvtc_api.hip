@@ -1534,3 +1534,7 @@ kvtc_status kvtc_attend(const kvtc_cache* cache, const void* q_dev, kvtc_dtype d
 }
 
 }  // extern "C"
+
+namespace kvtc {
+kvtc_status cache_check(const char* who, const kvtc_cache* c) { return check_cache(who, c); }
+}  // namespace kvtc

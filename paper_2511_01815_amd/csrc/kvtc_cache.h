@@ -39,6 +39,9 @@ struct AttendArgs {
     uint32_t* status;
 };
 
+// The checks of a cache that every call makes; `who` is the call.
+kvtc_status cache_check(const char* who, const kvtc_cache* c);
+
 // *status = 1 + the lowest index reported, 0 as long as there is none.
 __device__ __forceinline__ void report_lowest(uint32_t* status, uint32_t index) {
     if (!status) return;
