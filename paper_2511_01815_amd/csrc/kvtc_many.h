@@ -26,6 +26,8 @@ struct ManyArgs {
     uint32_t* status;
 };
 
+// Kinds of kernel: all in fp32; blocks of 128, of 64 and of 32 rows in 16 bits.
+enum ManyKind { kManyPlain = 0, kManyWide = 1, kManyTwo = 2, kManyOne = 3 };
 // How a call runs: rows (token, query head of the group) of an item and tokens of a tile by the kernel's kind, items that there can be, parts that an item's tiles are cut into, tiles of a part.
 struct ManyRoute { int kind, rows, tile, items, parts; uint32_t part_tiles; };
 

@@ -1,4 +1,4 @@
-// Attention of many new tokens of every sequence over the pages of a live cache, for gfx950: launches, the kernel in fp32, and the join of parts.
+// Attention of many new tokens of every sequence over the pages of a live cache, for gfx950: launches, the kernel for fp32 queries, and the join of parts.  (bf16 queries: kvtc_many_mfma.hip.)
 //
 // For a row (a new token's query head) at position i of its sequence, over the tokens that it sees,
 //     s_t = scale q . k_t,   out = sum_t e^(s_t) v_t / sum_t e^(s_t),   lse = log sum_t e^(s_t),
@@ -104,7 +104,7 @@ __device__ __forceinline__ float sum_over_quarters(float v) {
 __device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // Four waves of 16 rows; a row's scores over lanes 16 apart, four neighbouring tokens of every 16 to each.
-template <int F, int D, typename XT>
+template <int F, int D>
 __global__ void __launch_bounds__(256) many_plain_kernel(const ManyPlan p) {
     constexpr int LD = D + 4, NS = D / 4, NO = D / 16;     // (rows 4 banks apart)
     __shared__ float keys[kPlainTile][LD], values[kPlainTile][LD];
@@ -132,12 +132,9 @@ __global__ void __launch_bounds__(256) many_plain_kernel(const ManyPlan p) {
     const float factor = p.a.scale * kLog2e;
     float q[NS];                                           // features quarter * NS and on
     {
-        const XT* from = static_cast<const XT*>(p.a.q) + (int64_t)(it.first + token) * p.a.q_token_stride + (int64_t)q_head * p.a.q_head_stride + quarter * NS;
+        const float* from = static_cast<const float*>(p.a.q) + (int64_t)(it.first + token) * p.a.q_token_stride + (int64_t)q_head * p.a.q_head_stride + quarter * NS;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            if constexpr (sizeof(XT) == 2) q[i] = is_row ? __uint_as_float((uint32_t)from[i] << 16) : 0.0f;
-            else q[i] = is_row ? from[i] : 0.0f;
-        }
+        for (int i = 0; i < NS; ++i) q[i] = is_row ? from[i] : 0.0f;
     }
     f32x4 o[NO];
 #pragma unroll
@@ -277,15 +274,11 @@ __global__ void __launch_bounds__(256) many_plain_kernel(const ManyPlan p) {
     }
     const bool none = m == kNoScore && l == 0.0f;
     const float inverse = none ? 0.0f : 1.0f / l;
-    XT* out = static_cast<XT*>(p.a.out) + place * D;
+    float* out = static_cast<float*>(p.a.out) + place * D;
 #pragma unroll
     for (int c = 0; c < NO; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float x = none ? 0.0f : o[c][i] * inverse;
-            if constexpr (sizeof(XT) == 2) out[16 * c + 4 * quarter + i] = f32_bf16(x);
-            else out[16 * c + 4 * quarter + i] = x;
-        }
+        for (int i = 0; i < 4; ++i) out[16 * c + 4 * quarter + i] = none ? 0.0f : o[c][i] * inverse;
     if (p.a.lse && quarter == 0) p.a.lse[place] = none ? kNoScore : (m + __builtin_log2f(l)) * kLn2;
 }
 
@@ -333,10 +326,11 @@ __global__ void __launch_bounds__(256) many_join_kernel(const ManyPlan p) {
 
 ManyRoute many_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window) {
     ManyRoute r;
-    r.kind = 0;
-    r.rows = kPlainRows;
-    r.tile = kPlainTile;
-    const int64_t group = n_q_heads / c.n_heads;
+    const int64_t group = n_q_heads / c.n_heads, mean = n_tokens * group / n_seqs;
+    r.kind = dtype == KVTC_F32 ? kManyPlain : mean > 64 ? kManyWide : mean > 32 ? kManyTwo : kManyOne;
+    const int rows[4] = {kPlainRows, 128, 64, 32}, tile[4] = {kPlainTile, 64, 64, c.d_head == 256 ? 64 : 128};
+    r.rows = rows[r.kind];
+    r.tile = tile[r.kind];
     r.items = (int)(n_tokens * group / r.rows + n_seqs);
     int64_t tiles = (max_tokens + r.tile - 1) / r.tile;
     if (window) {
@@ -363,21 +357,30 @@ size_t many_work_bytes(const kvtc_cache& c, int n_seqs, int64_t n_tokens, int n_
     return most + 256;
 }
 
-template <int F, int D, typename XT>
+hipError_t launch_many_mfma_0(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_1(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_2(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_3(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_4(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_5(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_6(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_7(const ManyPlan& p, hipStream_t stream);
+hipError_t launch_many_mfma_8(const ManyPlan& p, hipStream_t stream);
+
+template <int F, int D>
 static void launch_plain(const ManyPlan& p, hipStream_t stream) {
-    hipLaunchKernelGGL((many_plain_kernel<F, D, XT>), dim3(p.r.items, p.a.c.n_heads, p.r.parts), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((many_plain_kernel<F, D>), dim3(p.r.items, p.a.c.n_heads, p.r.parts), dim3(256), 0, stream, p);
 }
-template <int F, typename XT>
+template <int F>
 static void launch_plain_width(const ManyPlan& p, hipStream_t stream) {
-    if (p.a.c.d_head == 64) launch_plain<F, 64, XT>(p, stream);
-    else if (p.a.c.d_head == 128) launch_plain<F, 128, XT>(p, stream);
-    else launch_plain<F, 256, XT>(p, stream);
+    if (p.a.c.d_head == 64) launch_plain<F, 64>(p, stream);
+    else if (p.a.c.d_head == 128) launch_plain<F, 128>(p, stream);
+    else launch_plain<F, 256>(p, stream);
 }
-template <typename XT>
 static void launch_plain_format(const ManyPlan& p, hipStream_t stream) {
-    if (p.a.c.format == KVTC_CACHE_BF16) launch_plain_width<KVTC_CACHE_BF16, XT>(p, stream);
-    else if (p.a.c.format == KVTC_CACHE_FP8) launch_plain_width<KVTC_CACHE_FP8, XT>(p, stream);
-    else launch_plain_width<KVTC_CACHE_INT4, XT>(p, stream);
+    if (p.a.c.format == KVTC_CACHE_BF16) launch_plain_width<KVTC_CACHE_BF16>(p, stream);
+    else if (p.a.c.format == KVTC_CACHE_FP8) launch_plain_width<KVTC_CACHE_FP8>(p, stream);
+    else launch_plain_width<KVTC_CACHE_INT4>(p, stream);
 }
 
 hipError_t launch_many(const ManyArgs& a, kvtc_dtype dtype, hipStream_t stream) {
@@ -396,9 +399,15 @@ hipError_t launch_many(const ManyArgs& a, kvtc_dtype dtype, hipStream_t stream) 
     const int64_t rows = (int64_t)a.n_tokens * a.n_q_heads;
     p.part_out = static_cast<float*>(a.work);
     p.part_sums = reinterpret_cast<float2*>(p.part_out + (p.r.parts > 1 ? p.r.parts * rows * a.c.d_head : 0));
-    if (dtype == KVTC_BF16) launch_plain_format<uint16_t>(p, stream);
-    else launch_plain_format<float>(p, stream);
-    hipError_t e = hipGetLastError();
+    hipError_t e;
+    if (p.r.kind == kManyPlain) {
+        launch_plain_format(p, stream);
+        e = hipGetLastError();
+    } else {
+        static hipError_t (*const launch[9])(const ManyPlan&, hipStream_t) = {launch_many_mfma_0, launch_many_mfma_1, launch_many_mfma_2, launch_many_mfma_3, launch_many_mfma_4,
+                                                                              launch_many_mfma_5, launch_many_mfma_6, launch_many_mfma_7, launch_many_mfma_8};
+        e = launch[3 * a.c.format + (a.c.d_head == 64 ? 0 : a.c.d_head == 128 ? 1 : 2)](p, stream);
+    }
     if (e != hipSuccess || p.r.parts == 1) return e;
     const dim3 grid(p.r.items, a.c.n_heads, 4);
     if (dtype == KVTC_BF16) hipLaunchKernelGGL((many_join_kernel<uint16_t>), grid, dim3(256), 0, stream, p);
