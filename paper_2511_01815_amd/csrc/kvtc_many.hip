@@ -328,7 +328,7 @@ ManyRoute many_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t 
     ManyRoute r;
     const int64_t group = n_q_heads / c.n_heads, mean = n_tokens * group / n_seqs;
     r.kind = dtype == KVTC_F32 ? kManyPlain : mean > 64 ? kManyWide : mean > 32 ? kManyTwo : kManyOne;
-    const int rows[4] = {kPlainRows, 128, 64, 32}, tile[4] = {kPlainTile, 64, 64, c.d_head == 256 ? 64 : 128};
+    const int rows[4] = {kPlainRows, 128, 64, 32}, tile[4] = {kPlainTile, 64, 64, c.d_head == 256 && c.format == KVTC_CACHE_BF16 ? 64 : 128};
     r.rows = rows[r.kind];
     r.tile = tile[r.kind];
     r.items = (int)(n_tokens * group / r.rows + n_seqs);

@@ -4,8 +4,9 @@
 // (64, or 32 to a wave), whose results are joined through the LDS in the end.
 //
 // Operands.  bf16 pages: keys, values and queries as they are, probabilities rounded to bf16 (off by 2^-8 of themselves at most, as much as the rounding of the output; sums of probabilities are of those before it).
-// 8 and 4 bits: fp16.  A key or value is what the cache stands for, times a power of two, rounded once to fp16 (2^-11): 16 tokens have an exponent in common, chosen so that the largest among them is below 2^15,
-// which goes into the scores' factor and, of the values, into the probabilities' exponential; queries likewise by rows; probabilities are rounded to fp16.  What is more than 2^28 below the largest value near it loses bits.
+// 8 and 4 bits: fp16.  Queries times a power of two, a row's largest below 2^15; 8 bits: codes as they are, and a token's scales go into its scores and probabilities; 4 bits: shift + code * scale, rounded once to fp16 (2^-11; a
+// number of the format below 2^-14 is one of fp16; 16 tokens of which one passes 2^15 are all divided by a power of two); probabilities, of 8 bits times the values' scale, are rounded to fp16.  The scales of 16 tokens' values
+// have an exponent in common, which goes into the probabilities' exponential.  What is more than 2^28 below the largest value so far loses bits.
 //
 // Products.  32 x 32 x 16 instructions, S^T = K Q^T and O^T = V^T P^T.  A lane has the scores of one row, of tokens 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..15, of every 32.  The second product sums over
 // tokens in that order: its operand of probabilities is what the lane has, and that of values comes out of the LDS by transposing loads of four tokens of a feature.  Maxima and sums need one exchange of halves.
@@ -17,7 +18,6 @@
 // Tiles of which some row does not see all (or that have no page) are masked, row by row, as 32 bits to 32 tokens.  Their values that are not finite are zeros in the LDS, lest a probability of zero make NaN of them, and are added
 // afterwards to the rows that see them.
 #include <hip/hip_runtime.h>
-#include <type_traits>
 #include "kvtc_dev.h"
 #include "kvtc_many.h"
 
@@ -44,7 +44,7 @@ template <int F> constexpr bool is_bf16() { return F == KVTC_CACHE_BF16; }
 // By how much, in powers of two, scores may pass the maximum that is taken off; fp16: and the values' exponents theirs, with probabilities times 2^kBias: below 2^15 together.
 template <int F> constexpr float slack() { return is_bf16<F>() ? 8.0f : 4.0f; }
 constexpr int kProducts = 0x8, kLdsReads = 0x100;           // of instructions whose order is asked for
-constexpr int kBias = 7, kExponentSlack = 4, kLeastExponent = -100;
+constexpr int kBias = 6, kExponentSlack = 4, kLeastExponent = -100;
 
 template <int F> __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
     if constexpr (is_bf16<F>()) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -77,7 +77,6 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 }
 __device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
-__device__ __forceinline__ int64_t lane_value64(int64_t v, int lane) { return (int64_t)((uint64_t)lane_value((uint32_t)((uint64_t)v >> 32), lane) << 32 | lane_value((uint32_t)v, lane)); }
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
@@ -101,7 +100,12 @@ struct Shape {
     static constexpr int ROW = 2 * D;                      // bytes of a token in the LDS
     static constexpr int BUFFER = TILE * ROW;
     static constexpr int NS = D / 16, NF = D / 32, NB = NT / 32, NG = RPW / 16;
-    static constexpr int kExponents = 4 * BUFFER, kWild = kExponents + 2 * 2 * (TILE / 16) * 4, kLds = kWild + 2 * NW * 4;
+    // Where a wave's tokens are those that it brings in, it waits for no other, and numbers that it makes itself need one buffer.
+    static constexpr bool ALONE = RW == 1;
+    static constexpr int BUFFERS = ALONE && !is_bf16<F>() ? 1 : 2;
+    // behind the buffers of keys and values: exponents of 16 tokens' keys and values; 8 bits: every token's scales; tokens with values that are not finite, by waves
+    static constexpr int kExponents = 2 * BUFFERS * BUFFER, kScales = kExponents + BUFFERS * 2 * (TILE / 16) * 4, kWild = kScales + (F == KVTC_CACHE_FP8 ? BUFFERS * 2 * TILE * 4 : 0),
+                         kLds = kWild + BUFFERS * NW * 4;
     static_assert(RPW % 16 == 0, "");
 };
 
@@ -144,10 +148,10 @@ struct Quarter {
 #pragma unroll
         for (int i = 0; i < kScales; ++i) scale[i] = reinterpret_cast<const KVTC_GLOBAL uint32_t*>(scales)[i];
     }
-    // a bound of the finite magnitudes of the row, or zero
+    // 8 bits: the scale, 4 bits: a bound of the magnitudes of the row; zero if it is not finite
     __device__ __forceinline__ float most() const {
         if constexpr (F == KVTC_CACHE_FP8) {
-            const float s = __builtin_fabsf(__uint_as_float(scale[0])) * 448.0f;
+            const float s = __builtin_fabsf(__uint_as_float(scale[0]));
             return not_finite(s) ? 0.0f : s;
         } else {
             float m = 0.0f;
@@ -160,21 +164,17 @@ struct Quarter {
             return m;
         }
     }
-    // f(piece, eight values) for the quarter's pieces of eight features
+    // f(piece, its eight features in fp16) for the quarter's pieces.  8 bits: the codes; 4 bits: values times 2^-e.
     template <typename FN>
-    __device__ __forceinline__ void each(int quarter, FN f) const {
-        float v[8];
+    __device__ __forceinline__ void each(int quarter, int e, FN f) const {
+        u32x4 v;
         if constexpr (F == KVTC_CACHE_FP8) {
-            const float s = __uint_as_float(scale[0]);
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const auto low = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[2 * i + j], false), high = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[2 * i + j], true);
-                    v[4 * j] = low[0] * s;
-                    v[4 * j + 1] = low[1] * s;
-                    v[4 * j + 2] = high[0] * s;
-                    v[4 * j + 3] = high[1] * s;
+                    v[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + j], 1.0f, false));
+                    v[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[2 * i + j], 1.0f, true));
                 }
                 f(quarter * (D / 32) + i, v);
             }
@@ -182,13 +182,19 @@ struct Quarter {
             constexpr int G = D / 32;                      // pairs 4 quarter .. + 3 of every group: byte pair * G + group
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const float shift = (float)__builtin_bit_cast(_Float16, (uint16_t)scale[g]), s = (float)__builtin_bit_cast(_Float16, (uint16_t)(scale[g] >> 16));
+                uint32_t header = scale[g];
+                if (e != 0) {                              // (the same for 16 rows)
+                    const f16x2 h = __builtin_bit_cast(f16x2, header);
+                    header = round_pair<F>(__builtin_amdgcn_ldexpf((float)h[0], -e), __builtin_amdgcn_ldexpf((float)h[1], -e));
+                }
+                const f16x2 shift = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(header, header, 0x01000100u)), size = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(header, header, 0x03020302u));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    // a byte's low code, behind 1024, and its high one, behind 64, where they stand
                     const int byte = j * G + g;
-                    const uint32_t codes = w[byte / 4] >> (8 * (byte % 4));
-                    v[2 * j] = __builtin_fmaf((float)(codes & 15u), s, shift);
-                    v[2 * j + 1] = __builtin_fmaf((float)(codes >> 4 & 15u), s, shift);
+                    const uint32_t twice = __builtin_amdgcn_perm(w[byte / 4], w[byte / 4], 0x0c000c00u | (uint32_t)(byte % 4) | (uint32_t)(byte % 4) << 16);
+                    const f16x2 codes = __builtin_bit_cast(f16x2, (twice & 0x00f0000fu) | 0x54006400u) - f16x2{(_Float16)1024.0f, (_Float16)64.0f};
+                    v[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(codes, size, shift));
                 }
                 f(4 * g + quarter, v);
             }
@@ -278,7 +284,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
 
     // Page numbers of a tile, on their way: of 16 tokens to a lane, or of one.
     int32_t pages[UNITS];
-    uint32_t page_t[UNITS];
+    uint32_t page_t[UNITS];                                // (the tokens that they are of)
     auto look = [&](uint32_t n) {
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
@@ -289,27 +295,40 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         }
     };
     // Where they are: bytes from the pools' (and the scales') bases; tokens that are there, a bit each.
-    int64_t rows_at[UNITS], scales_at[UNITS];
+    int64_t rows_at[IN_PAGE ? NG : UNITS], scales_at[IN_PAGE ? NG : UNITS];   // IN_PAGE: of the wave's own 16 tokens, the same in all lanes
     uint64_t have[(TILE + 63) / 64];
     auto place = [&](uint32_t n) {
-        uint64_t valid[UNITS];
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            const bool is = (uint32_t)pages[u] < (uint64_t)p.a.c.n_pages;
-            const uint32_t in = page_t[u] - many_page(p, page_t[u]) * (uint32_t)p.a.c.page_tokens;
-            rows_at[u] = is ? (int64_t)pages[u] * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
-            if constexpr (!BF) scales_at[u] = is ? (int64_t)pages[u] * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
-            valid[u] = __ballot(is);
-        }
         const uint32_t t0 = many_tile(it, n) * TILE;
+        if constexpr (IN_PAGE) {                           // (by the scalar unit: the wave's own 16 tokens only)
+            const uint64_t valid = __ballot((uint32_t)pages[0] < (uint64_t)p.a.c.n_pages) & ((1ull << (TILE / 16)) - 1ull);
 #pragma unroll
-        for (int w = 0; w < (TILE + 63) / 64; ++w) {
-            const bool is = TILE >= 64 || lane < TILE;
-            const uint32_t t = t0 + 64 * w + lane;
-            const bool wanted = is && there(t), page = IN_PAGE ? (valid[0] >> ((64 * w + lane) / 16) & 1u) != 0 : (valid[IN_PAGE ? 0 : w] >> lane & 1u) != 0;
-            have[w] = __ballot(wanted && page);
-            if (__ballot(wanted && !page)) {
-                if (lane == 0) report_lowest(p.a.status, (uint32_t)it.b);
+            for (int g = 0; g < NG; ++g) {
+                const uint32_t t = t0 + (wave * NG + g) * 16, page = lane_value((uint32_t)pages[0], wave * NG + g), in = t - many_page(p, t) * (uint32_t)p.a.c.page_tokens;
+                const bool is = (valid >> (wave * NG + g) & 1u) != 0;
+                rows_at[g] = is ? (int64_t)page * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
+                if constexpr (!BF) scales_at[g] = is ? (int64_t)page * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
+            }
+            if (valid == (1ull << (TILE / 16)) - 1ull && t0 + TILE <= (uint32_t)it.end && (p.window == 0u || t0 + TILE <= p.sinks || (int)t0 >= gap)) {
+#pragma unroll
+                for (int w = 0; w < (TILE + 63) / 64; ++w) have[w] = ~0ull;
+                return;
+            }
+#pragma unroll
+            for (int w = 0; w < (TILE + 63) / 64; ++w) {
+                const bool wanted = there(t0 + 64 * w + lane), page = (valid >> ((64 * w + lane) / 16) & 1u) != 0;
+                have[w] = __ballot(wanted && page);
+                if (__ballot(wanted && !page) && lane == 0) report_lowest(p.a.status, (uint32_t)it.b);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const bool is = (uint32_t)pages[u] < (uint64_t)p.a.c.n_pages;
+                const uint32_t in = page_t[u] - many_page(p, page_t[u]) * (uint32_t)p.a.c.page_tokens;
+                rows_at[u] = is ? (int64_t)pages[u] * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
+                if constexpr (!BF) scales_at[u] = is ? (int64_t)pages[u] * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
+                const bool wanted = there(t0 + 64 * u + lane);
+                have[u] = __ballot(wanted && is);
+                if (__ballot(wanted && !is) && lane == 0) report_lowest(p.a.status, (uint32_t)it.b);
             }
         }
     };
@@ -341,7 +360,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             if constexpr (IN_PAGE) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const int64_t off = lane_value64(rows_at[0], wave * NG + g);
+                    const int64_t off = rows_at[g];
                     constexpr int each = NJ / NG;
 #pragma unroll
                     for (int j = 0; j < each; ++j) {
@@ -364,8 +383,8 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 const int in_group = lane >> 2, quarter = lane & 3;
                 int64_t off, scale_off;
                 if constexpr (IN_PAGE) {
-                    off = lane_value64(rows_at[0], wave * NG + g) + (uint32_t)(in_group * ts);
-                    scale_off = lane_value64(scales_at[0], wave * NG + g) + in_group * cache_scale_bytes(F, D);
+                    off = rows_at[g] + (uint32_t)(in_group * ts);
+                    scale_off = scales_at[g] + in_group * cache_scale_bytes(F, D);
                 } else {
                     const int t = wave * RPW + 16 * g + in_group;
                     off = shfl64(rows_at[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
@@ -377,6 +396,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         }
     };
     float* exponents = reinterpret_cast<float*>(lds + S::kExponents);        // [buffer][keys, values][16 tokens]
+    float* scales = reinterpret_cast<float*>(lds + S::kScales);              // [buffer][keys, values][token]: 8 bits, values' without the 16 tokens' exponent
     uint32_t* wild = reinterpret_cast<uint32_t*>(lds + S::kWild);            // [buffer][wave]: of its tokens, a bit each, those with values that are not finite
     // 8 and 4 bits: into the LDS, as numbers.
     auto settle = [&](int buffer, bool masked) {
@@ -389,38 +409,44 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 auto over_rows = [&](float v) {
 #pragma unroll
                     for (int d = 4; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-                    return v;
+                    return __uint_as_float(same(__float_as_uint(v)));
                 };
-                const float k_most = over_rows(is ? kq[g].most() : 0.0f), v_most = over_rows(is ? vq[g].most() : 0.0f);
-                // (the largest below 2^15)
-                const int ke = k_most == 0.0f ? kLeastExponent : max(kLeastExponent, exponent_of(k_most) - 14), ve = v_most == 0.0f ? kLeastExponent : max(kLeastExponent, exponent_of(v_most) - 14);
+                int ke = 0, ve;
+                float value_scale = 0.0f;
+                bool odd = false;
+                const float v_most = over_rows(is ? vq[g].most() : 0.0f);
+                if constexpr (F == KVTC_CACHE_FP8) {
+                    ve = v_most == 0.0f ? kLeastExponent : max(kLeastExponent, exponent_of(v_most));
+                    value_scale = __uint_as_float(vq[g].scale[0]);
+                    if (masked) {
+                        odd = not_finite(value_scale);
+                        value_scale = odd || !is ? 0.0f : value_scale;
+                    }
+                    if (quarter == 0) {
+                        scales[(buffer * 2 + 0) * TILE + t] = __uint_as_float(kq[g].scale[0]);
+                        scales[(buffer * 2 + 1) * TILE + t] = __builtin_amdgcn_ldexpf(value_scale, -ve);
+                    }
+                } else {
+                    const float k_most = over_rows(is ? kq[g].most() : 0.0f);
+                    ke = max(0, exponent_of(k_most) - 14);
+                    ve = max(0, exponent_of(v_most) - 14);
+                }
                 if (lane == 0) {
                     exponents[(buffer * 2 + 0) * (TILE / 16) + wave * NG + g] = (float)ke;
                     exponents[(buffer * 2 + 1) * (TILE / 16) + wave * NG + g] = (float)ve;
                 }
                 uint8_t* to_k = lds + buffer * 2 * S::BUFFER + t * S::ROW;
                 uint8_t* to_v = to_k + S::BUFFER;
-                kq[g].each(quarter, [&](int piece, const float (&v)[8]) {
-                    u32x4 w;
+                kq[g].each(quarter, ke, [&](int piece, u32x4 w) { *reinterpret_cast<u32x4*>(to_k + ((piece ^ key_turn<D>(t)) << 4)) = w; });
+                vq[g].each(quarter, F == KVTC_CACHE_FP8 ? 0 : ve, [&](int piece, u32x4 w) {
+                    if (masked) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = round_pair<F>(__builtin_amdgcn_ldexpf(v[2 * i], -ke), __builtin_amdgcn_ldexpf(v[2 * i + 1], -ke));
-                    *reinterpret_cast<u32x4*>(to_k + ((piece ^ key_turn<D>(t)) << 4)) = w;
-                });
-                bool odd = false;
-                vq[g].each(quarter, [&](int piece, const float (&v)[8]) {
-                    u32x4 w;
-                    float x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        x[i] = v[i];
-                        if (masked) {
-                            const bool bad = not_finite(x[i]);
-                            odd |= bad;
-                            x[i] = bad || !is ? 0.0f : x[i];
+                        for (int i = 0; i < 4; ++i) {
+                            const bool high = (w[i] & 0x7c000000u) == 0x7c000000u, low = (w[i] & 0x7c00u) == 0x7c00u;
+                            odd |= high || low;
+                            w[i] &= is ? (high ? 0x0000ffffu : 0xffffffffu) & (low ? 0xffff0000u : 0xffffffffu) : 0u;
                         }
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = round_pair<F>(__builtin_amdgcn_ldexpf(x[2 * i], -ve), __builtin_amdgcn_ldexpf(x[2 * i + 1], -ve));
                     *reinterpret_cast<u32x4*>(to_v + ((((piece >> 1) ^ value_turn<D>(t)) << 5) | (piece & 1) << 4)) = w;
                 });
                 if (masked) {
@@ -471,8 +497,8 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         for (int f = 0; f < (NF > 4 ? 4 : NF); ++f)
             v_at[f] = lds0 + S::BUFFER + (slice + t) * S::ROW + (((2 * f + (group & 1)) ^ value_turn<D>(t)) << 5) + (in & 3) * 8;
     }
-    auto tile = [&](auto masked_tag, uint32_t n, int buffer, const uint64_t (&mine)[(TILE + 63) / 64]) {
-        constexpr bool MASKED = decltype(masked_tag)::value;
+    // (masked tiles by the same code, with a step more where it is needed: with code of their own for them outputs were moved from registers to registers)
+    auto tile = [&](bool masked, uint32_t n, int buffer, const uint64_t (&mine)[(TILE + 63) / 64]) {
         const uint32_t shift = buffer * 2 * S::BUFFER;
         const int t0 = (int)(many_tile(it, n) * TILE + tw * NT);
         f32x16 s[NB];
@@ -494,7 +520,17 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
         }
-        if constexpr (MASKED) {
+        if constexpr (F == KVTC_CACHE_FP8) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(scales + (buffer * 2 + 0) * TILE + tw * NT + 32 * b + 2 * i + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[b][i + j] *= w[j];
+                }
+        }
+        if (masked) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const int t = t0 + 32 * b, in_tile = tw * NT + 32 * b;
@@ -509,7 +545,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             }
         }
         // the scores' factors and the values' exponents, of every 16 tokens
-        float c[2 * NB], up[2 * NB];
+        float c[2 * NB];
         int ve[2 * NB], ve_most = kLeastExponent;
         if constexpr (BF) {
 #pragma unroll
@@ -518,7 +554,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
 #pragma unroll
             for (int g = 0; g < 2 * NB; ++g) {
                 const float* e = exponents + buffer * 2 * (TILE / 16) + tw * (NT / 16) + g;
-                c[g] = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(factor, (int)e[0]), kLeastFactor, kMostFactor);
+                c[g] = F == KVTC_CACHE_FP8 ? factor : __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(factor, (int)e[0]), kLeastFactor, kMostFactor);
                 ve[g] = (int)same((uint32_t)(int)e[TILE / 16]);
                 ve_most = max(ve_most, ve[g]);
             }
@@ -532,10 +568,10 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 g0 = fmaxf(g0, s[b][i]);
                 g1 = fmaxf(g1, s[b][8 + i]);
             }
-            if constexpr (BF) top = fmaxf(top, fmaxf(g0, g1));
+            if constexpr (F != KVTC_CACHE_INT4) top = fmaxf(top, fmaxf(g0, g1));
             else top = fmaxf(top, fmaxf(g0 * c[2 * b], g1 * c[2 * b + 1]));
         }
-        if constexpr (BF) top *= factor;
+        if constexpr (F != KVTC_CACHE_INT4) top *= factor;
         top = max_of_halves(top);
         if (__any(top > m + slack<F>()) || (!BF && ve_most > exponent + kExponentSlack)) {
             const float now = fmaxf(m, top);
@@ -566,6 +602,14 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 sum += e[i];
             }
             l += BF ? sum : __builtin_amdgcn_ldexpf(sum, -dv);
+            if constexpr (F == KVTC_CACHE_FP8) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(scales + (buffer * 2 + 1) * TILE + tw * NT + 16 * g + 2 * i + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) e[i + j] *= w[j];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) pr[g][i] = round_pair<F>(e[2 * i], e[2 * i + 1]);
         }
@@ -584,8 +628,8 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 2, 1);
         }
-        if constexpr (MASKED) {
-            for (int w = 0; w < NW; ++w) {                 // values that are not finite, to the rows that see them
+        if (masked) {
+            for (int w = S::ALONE ? wave : 0; w < (S::ALONE ? wave + 1 : NW); ++w) {      // values that are not finite, to the rows that see them
                 uint32_t bits = same(wild[buffer * NW + w]);
                 while (bits) {
                     const int in_tile = w * RPW + __builtin_ctz(bits), t = (int)(many_tile(it, n) * TILE) + in_tile;
@@ -607,8 +651,6 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             }
         }
     };
-    constexpr std::true_type kMasked{};
-    constexpr std::false_type kFull{};
 
     look(n0);
     place(n0);
@@ -620,14 +662,15 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
     look(n0 + 1);
     settle(0, !now_full);
     for (uint32_t n = n0; n < n1; ++n) {
-        const int buffer = (int)(n - n0) & 1;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __syncthreads();
+        const int buffer = S::BUFFERS == 1 ? 0 : (int)(n - n0) & 1, next = S::BUFFERS - 1 - buffer;
+        if constexpr (BF || !S::ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if constexpr (S::ALONE) asm volatile("" ::: "memory");       // (a wave's accesses to the LDS are done in their order, which the compiler is to keep)
+        else __syncthreads();
         bool next_full = true;
         if (n + 1 < n1) {
             place(n + 1);
             next_full = is_full(n + 1);
-            bring(n + 1, buffer ^ 1);
+            bring(n + 1, next);
             look(n + 2);
         }
         if (!now_full && BF) {
@@ -638,7 +681,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
 #pragma unroll
             for (int w = 0; w < (TILE + 63) / 64; ++w) have[w] = next_have[w];
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();                  // (the next tile's loads stay on their way)
+            if constexpr (!S::ALONE) __builtin_amdgcn_s_barrier();           // (the next tile's loads stay on their way)
             asm volatile("" ::: "memory");
         }
         const uint32_t t0 = many_tile(it, n) * TILE + tw * NT;
@@ -649,13 +692,13 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 const uint64_t bits = now_have[tw * NT / 64] >> (tw * NT % 64);
                 full = full && (NT == 64 ? bits == ~0ull : (uint32_t)bits == 0xffffffffu);
                 uint32_t strange = 0;
-                for (int w = 0; w < NW; ++w) strange |= wild[buffer * NW + w];
+                for (int w = S::ALONE ? wave : 0; w < (S::ALONE ? wave + 1 : NW); ++w) strange |= wild[buffer * NW + w];
                 full = full && same(strange) == 0u;
             }
-            if (full) tile(kFull, n, buffer, now_have);
-            else tile(kMasked, n, buffer, now_have);
+            tile(!full, n, buffer, now_have);
         }
-        if (n + 1 < n1) settle(buffer ^ 1, !next_full);
+        if constexpr (S::ALONE) asm volatile("" ::: "memory");
+        if (n + 1 < n1) settle(next, !next_full);
         now_full = next_full;
 #pragma unroll
         for (int w = 0; w < (TILE + 63) / 64; ++w) now_have[w] = have[w];
@@ -744,7 +787,7 @@ template <int F, int D>
 static hipError_t launch_kind(const ManyPlan& p, hipStream_t stream) {
     if (p.r.kind == kManyWide) return launch_shape<F, D, 4, 1>(p, stream);
     if (p.r.kind == kManyTwo) return launch_shape<F, D, 2, 2>(p, stream);
-    return launch_shape<F, D, 1, D == 256 ? 2 : 4>(p, stream);
+    return launch_shape<F, D, 1, D == 256 && F == KVTC_CACHE_BF16 ? 2 : 4>(p, stream);
 }
 
 #define KVTC_MANY_NAME2(n) launch_many_mfma_##n
