@@ -284,42 +284,92 @@ __global__ void __launch_bounds__(256) many_plain_kernel(const ManyPlan p) {
 
 // ---- parts of an item's tiles, joined ------------------------------------------------------------------------------------------
 
-// 64 work-items to a row; an item's rows in turn.
-template <typename XT>
+// WAVES waves to a row, among which its parts are shared; eight parts' loads of a wave together.  (24 rows of 64 parts, heads of 128: one after another 121 us.)
+template <typename XT, int D, int WAVES>
 __global__ void __launch_bounds__(256) many_join_kernel(const ManyPlan p) {
+    constexpr int N = D / 64, ROWS = 4 / WAVES;
+    typedef float Features __attribute__((ext_vector_type(N == 1 ? 2 : N)));
+    __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
     ManyItem it;
     if (!many_item(p, blockIdx.x, it) || it.tiles <= p.r.part_tiles) return;
-    const int head = blockIdx.y, lane = threadIdx.x & 63, d = p.a.c.d_head;
+    const int head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = wave % WAVES;
     const int parts = (int)((it.tiles + p.r.part_tiles - 1) / p.r.part_tiles);
     const int64_t all = (int64_t)p.a.n_tokens * p.a.n_q_heads;
-    for (int row = blockIdx.z * 4 + (threadIdx.x >> 6); row < it.rows; row += gridDim.z * 4) {
-        const int r = it.row0 + row, token = r / p.group, q_head = head * p.group + r - token * p.group;
+    for (int row0 = blockIdx.z * ROWS; row0 < it.rows; row0 += gridDim.z * ROWS) {
+        const int row = row0 + wave / WAVES, r = it.row0 + (row < it.rows ? row : it.rows - 1), token = r / p.group, q_head = head * p.group + r - token * p.group;
         const int64_t place = (int64_t)(it.first + token) * p.a.n_q_heads + q_head;
-        float m = kNoScore;
-        for (int i = 0; i < parts; ++i) m = fmaxf(m, p.part_sums[i * all + place].x);
+        float m = kNoScore, l = 0.0f;
+        for (int i = lane; i < parts; i += 64) m = fmaxf(m, p.part_sums[i * all + place].x);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         const float base = m == kNoScore ? 0.0f : m;
-        float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = 0; i < parts; ++i) {
-            const float2 s = p.part_sums[i * all + place];
-            if (s.x == kNoScore && s.y == 0.0f) continue;  // (a part without a token that the row sees)
-            const float share = exp2_fast(s.x - base);
-            l += s.y * share;
-            const float* from = p.part_out + (i * all + place) * d;
+        float o[N];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (lane + 64 * j < d) o[j] += from[lane + 64 * j] * share;
-        }
-        const bool none = m == kNoScore && l == 0.0f;
-        XT* out = static_cast<XT*>(p.a.out) + place * d;
+        for (int j = 0; j < N; ++j) o[j] = 0.0f;
+        for (int i0 = mine; i0 < parts; i0 += 8 * WAVES) {
+            float x[8][N];
+            float2 s[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < d) {
-                const float x = none ? 0.0f : o[j] / l;
-                if constexpr (sizeof(XT) == 2) out[lane + 64 * j] = f32_bf16(x);
-                else out[lane + 64 * j] = x;
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * WAVES < parts ? i0 + k * WAVES : mine;
+                s[k] = p.part_sums[i * all + place];
+                const float* from = p.part_out + (i * all + place) * D + lane * N;
+                if constexpr (N == 1) {
+                    x[k][0] = from[0];
+                } else {
+                    const Features v = *reinterpret_cast<const Features*>(from);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) x[k][j] = v[j];
+                }
             }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k * WAVES < parts) {
+                    const float share = exp2_fast(s[k].x - base);
+                    l += s[k].y * share;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) o[j] += x[k][j] * share;
+                }
+        }
+        if constexpr (WAVES > 1) {
+            __shared__ float of_waves[WAVES];
+            __syncthreads();
+            if (lane == 0) of_waves[mine] = l;
+#pragma unroll
+            for (int j = 0; j < N; ++j) sums[mine][lane * N + j] = o[j];
+            __syncthreads();
+            if (mine > 0) continue;
+            for (int w = 1; w < WAVES; ++w) {
+                l += of_waves[w];
+#pragma unroll
+                for (int j = 0; j < N; ++j) o[j] += sums[w][lane * N + j];
+            }
+        }
+        if (row >= it.rows) continue;
+        const bool none = m == kNoScore && l == 0.0f;
+        XT* out = static_cast<XT*>(p.a.out) + place * D + lane * N;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float v = none ? 0.0f : o[j] / l;
+            if constexpr (sizeof(XT) == 2) out[j] = f32_bf16(v);
+            else out[j] = v;
+        }
         if (p.a.lse && lane == 0) p.a.lse[place] = none ? kNoScore : (m + __builtin_log2f(l)) * kLn2;
     }
+}
+template <typename XT, int D>
+static void launch_join_width(const ManyPlan& p, hipStream_t stream) {
+    const uint32_t each = p.r.parts > 8 ? 1 : 8;           // rows of a workgroup
+    const dim3 grid(p.r.items, p.a.c.n_heads, (p.r.rows + each - 1) / each);
+    if (p.r.parts > 8) hipLaunchKernelGGL((many_join_kernel<XT, D, 4>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((many_join_kernel<XT, D, 1>), grid, dim3(256), 0, stream, p);
+}
+template <typename XT>
+static hipError_t launch_join(const ManyPlan& p, hipStream_t stream) {
+    if (p.a.c.d_head == 64) launch_join_width<XT, 64>(p, stream);
+    else if (p.a.c.d_head == 128) launch_join_width<XT, 128>(p, stream);
+    else launch_join_width<XT, 256>(p, stream);
+    return hipGetLastError();
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------------
@@ -409,10 +459,7 @@ hipError_t launch_many(const ManyArgs& a, kvtc_dtype dtype, hipStream_t stream) 
         e = launch[3 * a.c.format + (a.c.d_head == 64 ? 0 : a.c.d_head == 128 ? 1 : 2)](p, stream);
     }
     if (e != hipSuccess || p.r.parts == 1) return e;
-    const dim3 grid(p.r.items, a.c.n_heads, 4);
-    if (dtype == KVTC_BF16) hipLaunchKernelGGL((many_join_kernel<uint16_t>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((many_join_kernel<float>), grid, dim3(256), 0, stream, p);
-    return hipGetLastError();
+    return dtype == KVTC_BF16 ? launch_join<uint16_t>(p, stream) : launch_join<float>(p, stream);
 }
 
 }  // namespace kvtc
