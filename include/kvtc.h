@@ -585,7 +585,7 @@ kvtc_status kvtc_rope_scaled(const void* x_dev, void* out_dev, kvtc_dtype dtype,
  *                 share it, of any sizes that it is large enough for; calls that may overlap need one each
  *   status_dev    (device, may be null; the caller zeroes it) 1 + the lowest sequence whose starts are not ascending or not in 0..n_tokens (its rows are left as they are), whose length is negative
  *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen)
- * n_tokens * n_q_heads at most 2^30 (KVTC_E_UNSUPPORTED beyond).
+ * n_tokens * n_q_heads at most 2^29 (KVTC_E_UNSUPPORTED beyond).
  * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 or n_tokens == 0 is a no-op.
  */
 size_t kvtc_attend_many_work_bytes(const kvtc_cache* cache, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens);     /* 0 for what kvtc_attend_many refuses */

@@ -36,6 +36,10 @@ uint64_t kvtc_host_decode_pass_bytes(int tiles, kvtc_dtype dtype, uint64_t bases
  * shares go to the XCDs in turn; pieces of 32 tokens to a wave's step; KV heads to a workgroup; workgroups.  Returns what kvtc_attend's checks of these do. */
 kvtc_status kvtc_host_attend_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route);
 
+/* How a kvtc_attend_many of these sizes runs, in route[0..5]: the kernel (0 for fp32 queries, 1 .. 3 for bf16 ones); rows of an item; tokens of a tile; items to a
+ * KV head; parts that an item's tiles are cut into; tiles of a part (0: all).  Returns what kvtc_attend_many's checks of these do. */
+kvtc_status kvtc_host_attend_many_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route);
+
 /* Tokens of 1 .. 1024 heads of 64, 128 or 256 features that kvtc_cache_write and kvtc_cache_read move in one launch, at most. */
 int64_t kvtc_host_cache_launch_tokens(int n_heads, int d_head);
 

@@ -166,6 +166,8 @@ def lib() -> C.CDLL:
         L.kvtc_host_decode_pass_bytes.restype = C.c_uint64
         L.kvtc_host_attend_route.argtypes = [cp, C.c_int, C.c_int, C.c_int, i64, i64, i64, C.POINTER(C.c_int32)]
         L.kvtc_host_attend_route.restype = C.c_int
+        L.kvtc_host_attend_many_route.argtypes = [cp, C.c_int, C.c_int, i64, C.c_int, i64, i64, i64, C.POINTER(C.c_int32)]
+        L.kvtc_host_attend_many_route.restype = C.c_int
         L.kvtc_host_cache_launch_tokens.argtypes = [C.c_int, C.c_int]
         L.kvtc_host_cache_launch_tokens.restype = i64
         L.kvtc_test_cache_tokens.argtypes = [C.c_int, cp, vp, vp, C.c_int, i64, i64, i64, vp, vp, i64, vp]

@@ -6,7 +6,7 @@
 
 namespace kvtc {
 
-constexpr int64_t kManyMaxRows = 1LL << 30;                // tokens times query heads of a call
+constexpr int64_t kManyMaxRows = 1LL << 29;                // tokens times query heads of a call: items of 64 rows and 256 threads are fewer than 2^32 threads
 
 struct ManyArgs {
     kvtc_cache c;

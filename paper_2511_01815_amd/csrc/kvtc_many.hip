@@ -9,9 +9,11 @@
 // Products: S^T = K Q^T, O^T = V^T P^T with tokens in the rows of the first and in the sum of the second, so that a lane has scores of one row only, and of those tokens that its operand of the second
 // product needs: probabilities never leave their registers.
 #include <hip/hip_runtime.h>
+#include <algorithm>
 #include <cmath>
 #include "kvtc_dev.h"
 #include "kvtc_many.h"
+#include "../../include/kvtc_test_hooks.h"
 
 namespace kvtc {
 kvtc_status set_error(kvtc_status st, const char* fmt, ...);
@@ -359,9 +361,10 @@ __global__ void __launch_bounds__(256) many_join_kernel(const ManyPlan p) {
 }
 template <typename XT, int D>
 static void launch_join_width(const ManyPlan& p, hipStream_t stream) {
-    const uint32_t each = p.r.parts > 8 ? 1 : 8;           // rows of a workgroup
+    const bool few = (int64_t)p.a.n_tokens * p.a.n_q_heads <= 8 * compute_units();
+    const uint32_t each = few ? 1 : 16;                    // rows of a workgroup
     const dim3 grid(p.r.items, p.a.c.n_heads, (p.r.rows + each - 1) / each);
-    if (p.r.parts > 8) hipLaunchKernelGGL((many_join_kernel<XT, D, 4>), grid, dim3(256), 0, stream, p);
+    if (few) hipLaunchKernelGGL((many_join_kernel<XT, D, 4>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((many_join_kernel<XT, D, 1>), grid, dim3(256), 0, stream, p);
 }
 template <typename XT>
@@ -374,25 +377,79 @@ static hipError_t launch_join(const ManyPlan& p, hipStream_t stream) {
 
 // ---- host ----------------------------------------------------------------------------------------------------------------------
 
-ManyRoute many_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window) {
-    ManyRoute r;
-    const int64_t group = n_q_heads / c.n_heads, mean = n_tokens * group / n_seqs;
-    r.kind = dtype == KVTC_F32 ? kManyPlain : mean > 64 ? kManyWide : mean > 32 ? kManyTwo : kManyOne;
-    const int rows[4] = {kPlainRows, 128, 64, 32}, tile[4] = {kPlainTile, 64, 64, c.d_head == 256 && c.format == KVTC_CACHE_BF16 ? 64 : 128};
-    r.rows = rows[r.kind];
-    r.tile = tile[r.kind];
-    r.items = (int)(n_tokens * group / r.rows + n_seqs);
-    int64_t tiles = (max_tokens + r.tile - 1) / r.tile;
-    if (window) {
-        const int64_t some = (sinks < max_tokens ? sinks : max_tokens) / r.tile + (window < max_tokens ? window : max_tokens) / r.tile + (r.rows + r.tile - 1) / r.tile + 3;
-        tiles = some < tiles ? some : tiles;
+// A kernel's rows, tokens of a tile and workgroups to a compute unit, and the time of a tile (us) where a compute unit has one workgroup and where it has all of them.
+struct ManyCost { int rows, tile, each; float alone, among; };
+// (Measured: heads of 128 features; one sequence of 8000 tokens with 64 new ones, and of 32768 with 2048, 32 query heads to 8; those of 64 and of 256 by their share of the work.)
+static ManyCost many_cost(int kind, int format, int d) {
+    static constexpr ManyCost of_128[3][4] = {
+        {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 1.36f, 2.15f}, {64, 64, 2, 1.0f, 1.33f}, {32, 128, 1, 1.2f, 1.55f}},
+        {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 2.06f, 2.75f}, {64, 64, 2, 1.83f, 2.4f}, {32, 128, 2, 2.24f, 2.8f}},
+        {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 2.3f, 3.4f}, {64, 64, 2, 2.0f, 2.9f}, {32, 128, 2, 2.6f, 3.9f}}};
+    ManyCost c = of_128[format][kind];
+    if (d == 64) {
+        c.alone *= 0.6f;
+        c.among *= kind == kManyPlain ? 0.5f : 0.6f;
+        if (kind == kManyOne) c.each = 2;
+    } else if (d == 256) {
+        c.alone *= 2.0f;
+        c.among *= kind == kManyPlain ? 2.0f : 1.2f;       // (one workgroup where there were two)
+        c.each = kind == kManyPlain ? 2 : 1;
+        if (kind == kManyOne && format == KVTC_CACHE_BF16) c.tile = 64;
     }
-    // parts where there are not items enough for all compute units, of four tiles at least
-    const int64_t workgroups = (int64_t)r.items * c.n_heads, places = 2 * (int64_t)compute_units();
-    int64_t parts = workgroups < places ? (places + workgroups - 1) / workgroups : 1;
-    if (parts > (tiles + 3) / 4) parts = (tiles + 3) / 4;
-    r.part_tiles = (uint32_t)((tiles + parts - 1) / parts);
-    r.parts = (int)((tiles + r.part_tiles - 1) / r.part_tiles);
+    return c;
+}
+
+// The kernel, and into how many parts an item's tiles are cut, by an estimate of the call's time: the tiles of the longest item one after another, those of all items by all compute units, and their bytes; and what parts have to
+// write and join.  The lengths stand on the device: a lone sequence's is max_tokens, of more of them the mean is taken for a third of it, and for more of what a window leaves.
+static ManyRoute many_estimate(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window) {
+    const int64_t group = n_q_heads / c.n_heads, mean = n_tokens * group / n_seqs, cus = compute_units();
+    const bool lone = n_seqs == 1;
+    if (sinks > max_tokens) sinks = max_tokens;
+    if (window > max_tokens) window = max_tokens;
+    const int64_t seen = window && sinks + window < max_tokens ? sinks + window : max_tokens;      // tokens that a row sees, at most
+    const float length = lone ? (float)seen - 0.5f * (float)(n_tokens < seen ? n_tokens : seen) : (window ? 0.7f : 0.35f) * (float)seen;
+    const float bytes = (float)n_seqs * (float)c.n_heads * length * 2.0f * (float)(cache_row_bytes(c.format, c.d_head) + cache_scale_bytes(c.format, c.d_head)) / 5.0e6f;
+    ManyRoute best{};
+    float least = 0.0f;
+    for (int kind = dtype == KVTC_F32 ? kManyPlain : kManyWide; kind <= (dtype == KVTC_F32 ? kManyPlain : kManyOne); ++kind) {
+        if (kind == kManyOne && !lone && mean > 32) continue;
+        const ManyCost k = many_cost(kind, c.format, c.d_head);
+        const int64_t items = n_tokens * group / k.rows + n_seqs, blocks = ((mean > 0 ? mean : 1) + k.rows - 1) / k.rows * n_seqs * c.n_heads;
+        int64_t tiles = (max_tokens + k.tile - 1) / k.tile;    // of an item, at most
+        if (window) {
+            const int64_t some = sinks / k.tile + window / k.tile + (k.rows + k.tile - 1) / k.tile + 3;
+            tiles = some < tiles ? some : tiles;
+        }
+        const float among = kind == kManyWide && mean < k.rows ? k.alone + (k.among - k.alone) * (float)mean / (float)k.rows : k.among;      // (its waves without rows leave the others their time)
+        for (int64_t parts = 1; parts <= tiles && parts <= 512; parts += parts < 4 ? 1 : parts < 8 ? 2 : parts / 2) {
+            if (parts > 1 && blocks * parts > 32 * cus * k.each) break;
+            const int64_t part_tiles = (tiles + parts - 1) / parts, rounds = (blocks * parts + cus * k.each - 1) / (cus * k.each);
+            const float path = (float)part_tiles * (blocks * parts <= cus ? k.alone : among);
+            float all = (float)blocks * length / (float)k.tile * among / (float)(cus * k.each);
+            if (lone && rounds < 3 && blocks * parts > cus && all < (float)rounds * (float)part_tiles * among) all = (float)rounds * (float)part_tiles * among;
+            if (all < bytes) all = bytes;
+            float time = 8.0f + (lone ? (path > all ? path : all) : sqrtf(path * path + all * all)) + (kind == kManyOne ? 2.0f : 0.0f);
+            if (parts > 1) time = 1.02f * time + (lone ? 6.0f : 16.0f) + (float)n_tokens * (float)n_q_heads * (float)parts * (float)c.d_head * 8.0f / 6.0e6f;
+            if (kind == kManyTwo && parts > 1) time *= 1.08f;
+            if (best.parts == 0 || time < least) {
+                least = time;
+                best = {kind, k.rows, k.tile, (int)items, (int)((tiles + part_tiles - 1) / part_tiles), (uint32_t)part_tiles};
+            }
+        }
+    }
+    return best;
+}
+
+ManyRoute many_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window) {
+    ManyRoute r = many_estimate(c, dtype, n_seqs, n_tokens, n_q_heads, max_tokens, sinks, window);
+    if (window) {                                          // no more parts than the workspace has room for, which is sized without one
+        const int most = many_estimate(c, dtype, n_seqs, n_tokens, n_q_heads, max_tokens, 0, 0).parts;
+        if (r.parts > most) {
+            const uint32_t tiles = r.part_tiles * (uint32_t)r.parts;
+            r.part_tiles = (tiles + most - 1) / most;
+            r.parts = most;
+        }
+    }
     if (r.parts == 1) r.part_tiles = 0xffffffffu;
     return r;
 }
@@ -400,8 +457,8 @@ ManyRoute many_route(const kvtc_cache& c, kvtc_dtype dtype, int n_seqs, int64_t 
 size_t many_work_bytes(const kvtc_cache& c, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens) {
     size_t most = 0;
     for (int type = 0; type < 2; ++type) {
-        const ManyRoute r = many_route(c, (kvtc_dtype)type, n_seqs < 1 ? 1 : n_seqs, n_tokens < 1 ? 1 : n_tokens, n_q_heads, max_tokens, 0, 0);
-        const size_t need = r.parts > 1 ? (size_t)r.parts * (size_t)n_tokens * n_q_heads * (c.d_head + 2) * sizeof(float) : 0;
+        const int parts = many_route(c, (kvtc_dtype)type, n_seqs < 1 ? 1 : n_seqs, n_tokens < 1 ? 1 : n_tokens, n_q_heads, max_tokens, 0, 0).parts;
+        const size_t need = parts > 1 ? (size_t)parts * (size_t)n_tokens * n_q_heads * (c.d_head + 2) * sizeof(float) : 0;
         most = need > most ? need : most;
     }
     return most + 256;
@@ -475,7 +532,18 @@ static kvtc_status check_many(const char* who, const kvtc_cache* c, int n_seqs, 
         return set_error(KVTC_E_ARG, "%s: n_q_heads=%d must be a multiple of the cache's %d heads, at most %d", who, n_q_heads, c->n_heads, kCacheMaxHeads);
     if (max_tokens < 1 || max_tokens > 0x7fffffffLL) return set_error(KVTC_E_ARG, "%s: max_tokens=%lld outside 1..2^31-1", who, (long long)max_tokens);
     if (n_tokens < 0 || n_tokens > 0x7fffffffLL) return set_error(KVTC_E_ARG, "%s: n_tokens=%lld", who, (long long)n_tokens);
-    if (n_tokens * n_q_heads > kManyMaxRows) return set_error(KVTC_E_UNSUPPORTED, "%s: %lld tokens of %d query heads are more than 2^30 rows", who, (long long)n_tokens, n_q_heads);
+    if (n_tokens * n_q_heads > kManyMaxRows) return set_error(KVTC_E_UNSUPPORTED, "%s: %lld tokens of %d query heads are more than 2^29 rows", who, (long long)n_tokens, n_q_heads);
+    return KVTC_OK;
+}
+
+kvtc_status kvtc_host_attend_many_route(const kvtc_cache* cache, kvtc_dtype dtype, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens, int64_t sinks, int64_t window, int32_t* route) {
+    using namespace kvtc;
+    const kvtc_status st = check_many("kvtc_host_attend_many_route", cache, n_seqs, n_tokens, n_q_heads, max_tokens);
+    if (st != KVTC_OK) return st;
+    if ((dtype != KVTC_BF16 && dtype != KVTC_F32) || n_seqs < 1 || n_tokens < 1 || sinks < 0 || window < 0 || !route) return set_error(KVTC_E_ARG, "kvtc_host_attend_many_route: bad argument");
+    const ManyRoute r = many_route(*cache, dtype, n_seqs, n_tokens, n_q_heads, max_tokens, sinks, window);
+    const int32_t all[6] = {r.kind, r.rows, r.tile, r.items, r.parts, r.parts == 1 ? 0 : (int32_t)r.part_tiles};
+    std::copy(all, all + 6, route);
     return KVTC_OK;
 }
 

@@ -10,7 +10,7 @@
 //
 // Products.  32 x 32 x 16 instructions, S^T = K Q^T and O^T = V^T P^T.  A lane has the scores of one row, of tokens 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..15, of every 32.  The second product sums over
 // tokens in that order: its operand of probabilities is what the lane has, and that of values comes out of the LDS by transposing loads of four tokens of a feature.  Maxima and sums need one exchange of halves.
-// The maximum that is taken off the scores follows the true one when that has grown by more than 2^kSlack: outputs are rarely rescaled.
+// The maximum that is taken off the scores follows the true one when that has grown by more than slack(): outputs are rarely rescaled.
 //
 // Tiles.  Two buffers in the LDS: while one is used, the next tile is on its way, bf16 rows directly from memory to the LDS, others by registers, where they become numbers.  16-byte pieces of a row lie in an order that differs
 // from row to row, so that neither the loads of keys (32 rows at a column) nor those of values (8 rows at two columns) meet in a bank.
@@ -34,7 +34,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define KVTC_GLOBAL __attribute__((address_space(1)))
 #define KVTC_LDS __attribute__((address_space(3)))
-typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoScore = -__builtin_huge_valf();
@@ -77,6 +76,7 @@ __device__ __forceinline__ float sum_of_halves(float v) {
 }
 __device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ int64_t lane_value64(int64_t v, int lane) { return (int64_t)((uint64_t)lane_value((uint32_t)((uint64_t)v >> 32), lane) << 32 | lane_value((uint32_t)v, lane)); }
 __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
     const int lo = __shfl((int)(uint32_t)v, from, 64), hi = __shfl((int)(v >> 32), from, 64);
     return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
@@ -91,10 +91,10 @@ __device__ __forceinline__ void to_lds(const void* at, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(at) : "memory");
 }
 
-template <int F, int D, int RW, int TW>
+template <int F, int D, int RW, int TW, int TOKENS>
 struct Shape {
     static constexpr int NW = RW * TW;
-    static constexpr int NT = TW == 1 ? 64 : 32;           // tokens of a wave
+    static constexpr int NT = TOKENS;                      // of a wave, to a tile
     static constexpr int TILE = NT * TW, ROWS = 32 * RW;
     static constexpr int RPW = TILE / NW;                  // tokens that a wave brings in
     static constexpr int ROW = 2 * D;                      // bytes of a token in the LDS
@@ -202,12 +202,12 @@ struct Quarter {
     }
 };
 
-template <int F, int D, int RW, int TW, bool IN_PAGE>
+template <int F, int D, int RW, int TW, int TOKENS, bool IN_PAGE>
 __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kernel(const ManyPlan p) {
-    using S = Shape<F, D, RW, TW>;
+    using S = Shape<F, D, RW, TW, TOKENS>;
     constexpr bool BF = is_bf16<F>();
     constexpr int NW = S::NW, NT = S::NT, TILE = S::TILE, RPW = S::RPW, NS = S::NS, NF = S::NF, NB = S::NB, NG = S::NG;
-    constexpr int UNITS = IN_PAGE ? 1 : (TILE + 63) / 64;  // tokens (16 of them if in a page) that a lane looks up
+    constexpr int UNITS = IN_PAGE ? 1 : (TILE + 63) / 64;  // what a lane looks up: 16 tokens in a page, or tokens of a tile
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = (int)same(tid >> 6), rw = wave / TW, tw = wave % TW, col = lane & 31, half = lane >> 5;
     const int head = blockIdx.x, part = blockIdx.z;
@@ -282,53 +282,66 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
     const int gap = p.window == 0u ? 0 : (int)max((int64_t)0, (int64_t)it.at0 - (int64_t)p.window + 1);      // tokens from p.sinks to before it are seen by no row
     auto there = [&](uint32_t t) { return t < (uint32_t)it.end && (p.window == 0u || t < p.sinks || (int)t >= gap); };
 
-    // Page numbers of a tile, on their way: of 16 tokens to a lane, or of one.
+    // Where tokens are: bytes from the pools' (and the scales') bases.  IN_PAGE: of every 16 tokens, a lane each, for PER tiles at a time, the next ones' page numbers on their way; what a tile needs of that is read out of
+    // the lanes.  Else of the next tile, a token to a lane.  (Worked out for every tile, by the scalar unit, this was up to 0.4 us a tile where a wave is alone; page numbers through the scalar cache make every wait for the
+    // LDS one for them, and a load of the vector unit for every tile one for all keys and values before it: loads come back in their order.)
+    constexpr int GROUPS = TILE / 16, PER = 64 / GROUPS;
     int32_t pages[UNITS];
-    uint32_t page_t[UNITS];                                // (the tokens that they are of)
-    auto look = [&](uint32_t n) {
+    int64_t rows_of[UNITS], scales_of[BF ? 1 : UNITS];
+    uint64_t valid[UNITS];
+    auto look = [&](uint32_t n) {                          // page numbers from tile n on
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            const uint32_t t = many_tile(it, n) * TILE + (IN_PAGE ? (lane & (TILE / 16 - 1)) * 16 : lane + 64 * u);
-            page_t[u] = t;
+            const uint32_t t = IN_PAGE ? many_tile(it, n + lane / GROUPS) * TILE + (lane % GROUPS) * 16 : many_tile(it, n) * TILE + lane + 64 * u;
             pages[u] = -1;
-            if (n < n1 && t < (uint32_t)it.end && (IN_PAGE ? t + 15 < p.sinks || p.window == 0u || (int)t + 15 >= gap || t < p.sinks : there(t))) pages[u] = table[many_page(p, t)];
+            if (IN_PAGE ? n + lane / GROUPS < n1 && t < (uint32_t)it.end : n < n1 && there(t)) pages[u] = table[many_page(p, t)];
         }
     };
-    // Where they are: bytes from the pools' (and the scales') bases; tokens that are there, a bit each.
-    int64_t rows_at[IN_PAGE ? NG : UNITS], scales_at[IN_PAGE ? NG : UNITS];   // IN_PAGE: of the wave's own 16 tokens, the same in all lanes
-    uint64_t have[(TILE + 63) / 64];
+    auto find = [&](uint32_t n) {                          // ... and places
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const uint32_t t = IN_PAGE ? many_tile(it, n + lane / GROUPS) * TILE + (lane % GROUPS) * 16 : many_tile(it, n) * TILE + lane + 64 * u;
+            const bool is = (uint32_t)pages[u] < (uint64_t)p.a.c.n_pages;
+            const uint32_t in = t - many_page(p, t) * (uint32_t)p.a.c.page_tokens;
+            rows_of[u] = is ? (int64_t)pages[u] * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
+            if constexpr (!BF) scales_of[u] = is ? (int64_t)pages[u] * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
+            valid[u] = __ballot(is);
+        }
+    };
+    int64_t rows_at[IN_PAGE ? NG : 1], scales_at[IN_PAGE ? NG : 1];          // IN_PAGE: of the wave's own 16 tokens, the same in all lanes
+    uint64_t have[(TILE + 63) / 64];                       // tokens that are there, a bit each
     auto place = [&](uint32_t n) {
         const uint32_t t0 = many_tile(it, n) * TILE;
-        if constexpr (IN_PAGE) {                           // (by the scalar unit: the wave's own 16 tokens only)
-            const uint64_t valid = __ballot((uint32_t)pages[0] < (uint64_t)p.a.c.n_pages) & ((1ull << (TILE / 16)) - 1ull);
+        if constexpr (IN_PAGE) {
+            const int first = (int)((n - n0) % PER) * GROUPS;
+            if (first == 0) {
+                find(n);
+                look(n + PER);
+            }
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                const uint32_t t = t0 + (wave * NG + g) * 16, page = lane_value((uint32_t)pages[0], wave * NG + g), in = t - many_page(p, t) * (uint32_t)p.a.c.page_tokens;
-                const bool is = (valid >> (wave * NG + g) & 1u) != 0;
-                rows_at[g] = is ? (int64_t)page * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
-                if constexpr (!BF) scales_at[g] = is ? (int64_t)page * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
+                rows_at[g] = lane_value64(rows_of[0], first + wave * NG + g);
+                if constexpr (!BF) scales_at[g] = lane_value64(scales_of[0], first + wave * NG + g);
             }
-            if (valid == (1ull << (TILE / 16)) - 1ull && t0 + TILE <= (uint32_t)it.end && (p.window == 0u || t0 + TILE <= p.sinks || (int)t0 >= gap)) {
+            const uint32_t is = (uint32_t)(valid[0] >> first) & ((1u << GROUPS) - 1u);
+            if (is == (1u << GROUPS) - 1u && t0 + TILE <= (uint32_t)it.end && (p.window == 0u || t0 + TILE <= p.sinks || (int)t0 >= gap)) {
 #pragma unroll
                 for (int w = 0; w < (TILE + 63) / 64; ++w) have[w] = ~0ull;
                 return;
             }
 #pragma unroll
             for (int w = 0; w < (TILE + 63) / 64; ++w) {
-                const bool wanted = there(t0 + 64 * w + lane), page = (valid >> ((64 * w + lane) / 16) & 1u) != 0;
+                const bool wanted = there(t0 + 64 * w + lane), page = (is >> ((64 * w + lane) / 16) & 1u) != 0;
                 have[w] = __ballot(wanted && page);
                 if (__ballot(wanted && !page) && lane == 0) report_lowest(p.a.status, (uint32_t)it.b);
             }
         } else {
+            find(n);
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                const bool is = (uint32_t)pages[u] < (uint64_t)p.a.c.n_pages;
-                const uint32_t in = page_t[u] - many_page(p, page_t[u]) * (uint32_t)p.a.c.page_tokens;
-                rows_at[u] = is ? (int64_t)pages[u] * p.a.c.page_stride + (int64_t)((uint64_t)in * ts) : 0;
-                if constexpr (!BF) scales_at[u] = is ? (int64_t)pages[u] * p.scale_stride + (int64_t)in * cache_scale_bytes(F, D) : 0;
-                const bool wanted = there(t0 + 64 * u + lane);
-                have[u] = __ballot(wanted && is);
-                if (__ballot(wanted && !is) && lane == 0) report_lowest(p.a.status, (uint32_t)it.b);
+                const bool wanted = there(t0 + lane + 64 * u);
+                have[u] = __ballot(wanted) & valid[u];
+                if (have[u] != __ballot(wanted) && wanted && !(valid[u] >> lane & 1u)) report_lowest(p.a.status, (uint32_t)it.b);
             }
         }
     };
@@ -354,9 +367,12 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         }
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(KVTC_LDS uint8_t*)lds;
-    auto bring = [&](uint32_t n, int buffer) {
+    // bf16: keys (side 0) or values (1) of the tile that was placed last, NJ loads
+    auto bring_side = [&](int side, int buffer) {
         if constexpr (BF) {
-            const uint32_t to = lds0 + buffer * 2 * S::BUFFER + wave * RPW * S::ROW;
+            const uint32_t to = lds0 + (buffer * 2 + side) * S::BUFFER + wave * RPW * S::ROW;
+            const ManyBytes from = side ? v0 : k0;
+            const uint32_t* off_of = side ? v_off : k_off;
             if constexpr (IN_PAGE) {
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
@@ -364,20 +380,22 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                     constexpr int each = NJ / NG;
 #pragma unroll
                     for (int j = 0; j < each; ++j) {
-                        to_lds((const void*)(uintptr_t)(k0 + off), k_off[g * each + j], to + (g * each + j) * 1024);
-                        to_lds((const void*)(uintptr_t)(v0 + off), v_off[g * each + j], to + S::BUFFER + (g * each + j) * 1024);
+                        to_lds((const void*)(uintptr_t)(from + off), off_of[g * each + j], to + (g * each + j) * 1024);
                     }
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) {
                     const uint32_t t = wave * RPW + (j * 1024 + lane * 16) / S::ROW;
-                    const int64_t off = shfl64(rows_at[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
-                    to_lds((const void*)(uintptr_t)(k0 + off + k_off[j]), to + j * 1024);
-                    to_lds((const void*)(uintptr_t)(v0 + off + v_off[j]), to + S::BUFFER + j * 1024);
+                    const int64_t off = shfl64(rows_of[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
+                    to_lds((const void*)(uintptr_t)(from + off + off_of[j]), to + j * 1024);
                 }
             }
-        } else {
+        }
+    };
+    // 8 and 4 bits: both, into registers
+    auto bring = [&]() {
+        if constexpr (!BF) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const int in_group = lane >> 2, quarter = lane & 3;
@@ -387,8 +405,8 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                     scale_off = scales_at[g] + in_group * cache_scale_bytes(F, D);
                 } else {
                     const int t = wave * RPW + 16 * g + in_group;
-                    off = shfl64(rows_at[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
-                    scale_off = shfl64(scales_at[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
+                    off = shfl64(rows_of[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
+                    scale_off = shfl64(scales_of[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
                 }
                 kq[g].load(k0 + off + quarter * Quarter<F, D>::kBytes, ks0 + scale_off);
                 vq[g].load(v0 + off + quarter * Quarter<F, D>::kBytes, vs0 + scale_off);
@@ -459,14 +477,14 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         }
     };
     // bf16, a masked tile: the wave's own tokens' values, in the LDS.
-    auto clean = [&](int buffer) {
+    auto clean = [&](int buffer, const uint64_t (&there_bits)[(TILE + 63) / 64]) {
         if constexpr (BF) {
             uint32_t strange = 0;
             constexpr int in_piece = 1024 / S::ROW, lanes = S::ROW / 16;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 const int in_wave = (j * 1024 + lane * 16) / S::ROW, t = wave * RPW + in_wave;
-                const bool is = (have[TILE > 64 ? (wave * RPW) / 64 : 0] >> (t & 63) & 1u) != 0;
+                const bool is = (there_bits[TILE > 64 ? (wave * RPW) / 64 : 0] >> (t & 63) & 1u) != 0;
                 u32x4* at_lds = reinterpret_cast<u32x4*>(lds + (buffer * 2 + 1) * S::BUFFER + wave * RPW * S::ROW + j * 1024 + lane * 16);
                 u32x4 w = *at_lds;
                 bool odd = false;
@@ -498,7 +516,8 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             v_at[f] = lds0 + S::BUFFER + (slice + t) * S::ROW + (((2 * f + (group & 1)) ^ value_turn<D>(t)) << 5) + (in & 3) * 8;
     }
     // (masked tiles by the same code, with a step more where it is needed: with code of their own for them outputs were moved from registers to registers)
-    auto tile = [&](bool masked, uint32_t n, int buffer, const uint64_t (&mine)[(TILE + 63) / 64]) {
+    u32x4 pr[2 * NB];                                      // probabilities
+    auto scores = [&](bool masked, uint32_t n, int buffer, const uint64_t (&mine)[(TILE + 63) / 64]) {
         const uint32_t shift = buffer * 2 * S::BUFFER;
         const int t0 = (int)(many_tile(it, n) * TILE + tw * NT);
         f32x16 s[NB];
@@ -514,7 +533,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 s[b] = mfma<F>(a, q[k], s[b]);
             }
         // (a few loads ahead of the products, no more: the compiler left to itself puts them all first, and what they load does not fit the registers)
-        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, F == KVTC_CACHE_INT4 ? 4 : 8, 0);
 #pragma unroll
         for (int k = 0; k < NS * NB; ++k) {
             __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
@@ -589,7 +608,6 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[f][i] *= keep;
         }
-        u32x4 pr[2 * NB];
 #pragma unroll
         for (int g = 0; g < 2 * NB; ++g) {
             int dv = 0;
@@ -613,6 +631,9 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
 #pragma unroll
             for (int i = 0; i < 4; ++i) pr[g][i] = round_pair<F>(e[2 * i], e[2 * i + 1]);
         }
+    };
+    auto sums = [&](bool masked, uint32_t n, int buffer) {
+        const uint32_t shift = buffer * 2 * S::BUFFER;
 #pragma unroll
         for (int g = 0; g < 2 * NB; ++g)
 #pragma unroll
@@ -622,7 +643,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((KVTC_LDS s16x4*)(uintptr_t)(place_v + 8 * S::ROW)));
                 o[f] = mfma<F>(u32x4{a[0], a[1], b[0], b[1]}, pr[g], o[f]);
             }
-        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, F == KVTC_CACHE_INT4 ? 4 : 12, 1);
 #pragma unroll
         for (int k = 0; k < 2 * NB * NF; ++k) {
             __builtin_amdgcn_sched_group_barrier(kProducts, 1, 1);
@@ -652,56 +673,101 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
         }
     };
 
-    look(n0);
-    place(n0);
-    bring(n0, 0);
-    uint64_t now_have[(TILE + 63) / 64];
-    bool now_full = is_full(n0);
-#pragma unroll
-    for (int w = 0; w < (TILE + 63) / 64; ++w) now_have[w] = have[w];
-    look(n0 + 1);
-    settle(0, !now_full);
-    for (uint32_t n = n0; n < n1; ++n) {
-        const int buffer = S::BUFFERS == 1 ? 0 : (int)(n - n0) & 1, next = S::BUFFERS - 1 - buffer;
-        if constexpr (BF || !S::ALONE) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        if constexpr (S::ALONE) asm volatile("" ::: "memory");       // (a wave's accesses to the LDS are done in their order, which the compiler is to keep)
-        else __syncthreads();
-        bool next_full = true;
-        if (n + 1 < n1) {
-            place(n + 1);
-            next_full = is_full(n + 1);
-            bring(n + 1, next);
-            look(n + 2);
-        }
-        if (!now_full && BF) {
-            uint64_t next_have[(TILE + 63) / 64];
-#pragma unroll
-            for (int w = 0; w < (TILE + 63) / 64; ++w) { next_have[w] = have[w]; have[w] = now_have[w]; }
-            clean(buffer);
-#pragma unroll
-            for (int w = 0; w < (TILE + 63) / 64; ++w) have[w] = next_have[w];
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if constexpr (!S::ALONE) __builtin_amdgcn_s_barrier();           // (the next tile's loads stay on their way)
-            asm volatile("" ::: "memory");
-        }
+    // Whether the wave has rows that see anything of tile n, and whether it has to mask them.
+    auto is_seen = [&](uint32_t n, bool full) { return any_row && (full || !p.a.causal || (int)(many_tile(it, n) * TILE + tw * NT) <= last_at); };
+    auto is_masked = [&](uint32_t n, bool full, const uint64_t (&mine)[(TILE + 63) / 64]) {
+        if (full) return false;
         const uint32_t t0 = many_tile(it, n) * TILE + tw * NT;
-        if (any_row && (now_full || !p.a.causal || (int)t0 <= last_at)) {
-            bool full = now_full;
-            if (!full) {                                   // a wave's rows may see all of its tokens
-                full = (!p.a.causal || (int)(t0 + NT - 1) <= first_at) && (p.window == 0u || t0 + NT - 1 < p.sinks || (int)t0 >= last_from);
-                const uint64_t bits = now_have[tw * NT / 64] >> (tw * NT % 64);
-                full = full && (NT == 64 ? bits == ~0ull : (uint32_t)bits == 0xffffffffu);
-                uint32_t strange = 0;
-                for (int w = S::ALONE ? wave : 0; w < (S::ALONE ? wave + 1 : NW); ++w) strange |= wild[buffer * NW + w];
-                full = full && same(strange) == 0u;
-            }
-            tile(!full, n, buffer, now_have);
-        }
-        if constexpr (S::ALONE) asm volatile("" ::: "memory");
-        if (n + 1 < n1) settle(next, !next_full);
-        now_full = next_full;
+        const uint64_t bits = mine[tw * NT / 64] >> (tw * NT % 64);
+        return !((!p.a.causal || (int)(t0 + NT - 1) <= first_at) && (p.window == 0u || t0 + NT - 1 < p.sinks || (int)t0 >= last_from) && (NT == 64 ? bits == ~0ull : (uint32_t)bits == 0xffffffffu));
+    };
+    constexpr int WORDS = (TILE + 63) / 64;
+    uint64_t now_have[WORDS], next_have[WORDS];
+    bool now_full, next_full = true;
+    if (n0 == n1) {                                        // (rows that see nothing)
+    } else if constexpr (BF) {
+        // A tile's keys are asked for when the scores of the tile two before it are done, its values a barrier later; each has a tile and a half to arrive.  Loads come back in their order: what may be on its way
+        // still, when keys or values are waited for, is what was asked for after them.  What a wave reads out of the LDS it has before others write there.
+        auto arrive = [&](bool two, bool keys) {           // two: the next tile's keys and values are on their way as well
+            if (two) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * NJ) : "memory");
+            else if (keys) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NJ) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if constexpr (!S::ALONE) asm volatile("s_barrier" ::: "memory");
+        };
+        look(n0);
+        place(n0);
+        now_full = is_full(n0);
 #pragma unroll
-        for (int w = 0; w < (TILE + 63) / 64; ++w) now_have[w] = have[w];
+        for (int w = 0; w < WORDS; ++w) now_have[w] = have[w];
+        bring_side(0, 0);
+        bring_side(1, 0);
+        if constexpr (!IN_PAGE) look(n0 + 1);
+        if (n0 + 1 < n1) {
+            place(n0 + 1);
+            next_full = is_full(n0 + 1);
+            bring_side(0, 1);
+            if constexpr (!IN_PAGE) look(n0 + 2);
+        }
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) next_have[w] = have[w];
+        for (uint32_t n = n0; n < n1; ++n) {
+            const int buffer = (int)(n - n0) & 1;
+            arrive(n + 1 < n1, true);
+            if (n + 1 < n1) bring_side(1, buffer ^ 1);     // (all waves are through with the values before)
+            const bool seen = is_seen(n, now_full), masked = is_masked(n, now_full, now_have);
+            if (seen) scores(masked, n, buffer, now_have);
+            arrive(n + 1 < n1, false);
+            bool then_full = true;
+            if (n + 2 < n1) {                              // (all waves are through with the keys)
+                place(n + 2);
+                then_full = is_full(n + 2);
+                bring_side(0, buffer);
+                if constexpr (!IN_PAGE) look(n + 3);
+            }
+            if (!now_full) {
+                clean(buffer, now_have);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if constexpr (!S::ALONE) asm volatile("s_barrier" ::: "memory");
+            }
+            if (seen) sums(!now_full, n, buffer);
+            now_full = next_full;
+            next_full = then_full;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                now_have[w] = next_have[w];
+                next_have[w] = have[w];
+            }
+        }
+    } else {
+        look(n0);
+        place(n0);
+        bring();
+        now_full = is_full(n0);
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) now_have[w] = have[w];
+        if constexpr (!IN_PAGE) look(n0 + 1);
+        settle(0, !now_full);
+        for (uint32_t n = n0; n < n1; ++n) {
+            const int buffer = S::BUFFERS == 1 ? 0 : (int)(n - n0) & 1, next = S::BUFFERS - 1 - buffer;
+            if constexpr (S::ALONE) asm volatile("" ::: "memory");   // (a wave's accesses to the LDS are done in their order, which the compiler is to keep)
+            else __syncthreads();
+            next_full = true;
+            if (n + 1 < n1) {
+                place(n + 1);
+                next_full = is_full(n + 1);
+                bring();
+                if constexpr (!IN_PAGE) look(n + 2);
+            }
+            if (is_seen(n, now_full)) {
+                scores(is_masked(n, now_full, now_have), n, buffer, now_have);
+                sums(!now_full, n, buffer);
+            }
+            if constexpr (S::ALONE) asm volatile("" ::: "memory");
+            if (n + 1 < n1) settle(next, !next_full);
+            now_full = next_full;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) now_have[w] = have[w];
+        }
     }
 
     // ---- results ----
@@ -767,27 +833,27 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
     if (p.a.lse && half == 0) p.a.lse[at_out] = none ? kNoScore : (m + __builtin_log2f(l)) * kLn2;
 }
 
-template <int F, int D, int RW, int TW>
+template <int F, int D, int RW, int TW, int TOKENS>
 static hipError_t launch_shape(const ManyPlan& p, hipStream_t stream) {
-    using S = Shape<F, D, RW, TW>;
+    using S = Shape<F, D, RW, TW, TOKENS>;
     const dim3 grid(p.a.c.n_heads, p.r.items, p.r.parts), block(64 * S::NW);
     constexpr int lds = S::kLds > (TW > 1 ? RW * (TW / 2) * (S::NF * 16 + 2) * 256 : 0) ? S::kLds : RW * (TW / 2) * (S::NF * 16 + 2) * 256;
     if (p.a.c.page_tokens % 16 == 0) {
-        const hipError_t e = allow_full_lds(reinterpret_cast<const void*>(&many_mfma_kernel<F, D, RW, TW, true>));
+        const hipError_t e = allow_full_lds(reinterpret_cast<const void*>(&many_mfma_kernel<F, D, RW, TW, TOKENS, true>));
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((many_mfma_kernel<F, D, RW, TW, true>), grid, block, lds, stream, p);
+        hipLaunchKernelGGL((many_mfma_kernel<F, D, RW, TW, TOKENS, true>), grid, block, lds, stream, p);
     } else {
-        const hipError_t e = allow_full_lds(reinterpret_cast<const void*>(&many_mfma_kernel<F, D, RW, TW, false>));
+        const hipError_t e = allow_full_lds(reinterpret_cast<const void*>(&many_mfma_kernel<F, D, RW, TW, TOKENS, false>));
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((many_mfma_kernel<F, D, RW, TW, false>), grid, block, lds, stream, p);
+        hipLaunchKernelGGL((many_mfma_kernel<F, D, RW, TW, TOKENS, false>), grid, block, lds, stream, p);
     }
     return hipGetLastError();
 }
 template <int F, int D>
 static hipError_t launch_kind(const ManyPlan& p, hipStream_t stream) {
-    if (p.r.kind == kManyWide) return launch_shape<F, D, 4, 1>(p, stream);
-    if (p.r.kind == kManyTwo) return launch_shape<F, D, 2, 2>(p, stream);
-    return launch_shape<F, D, 1, D == 256 && F == KVTC_CACHE_BF16 ? 2 : 4>(p, stream);
+    if (p.r.kind == kManyWide) return launch_shape<F, D, 4, 1, 64>(p, stream);
+    if (p.r.kind == kManyTwo) return launch_shape<F, D, 2, 2, 32>(p, stream);
+    return launch_shape<F, D, 1, D == 256 && F == KVTC_CACHE_BF16 ? 2 : 4, 32>(p, stream);
 }
 
 #define KVTC_MANY_NAME2(n) launch_many_mfma_##n
