@@ -6,7 +6,8 @@
 //
 // A workgroup works both sums out for itself, a thread to a sequence, a block of sequences after another, finds the sequence of each of its rows among those in the LDS by halving, and writes the
 // rows' slots; whoever has a page's first token writes the page into the table.  One workgroup, where that has rows few enough, writes the sequences' results as well: one launch, of which latencies in a row
-// are the time (64 sequences of one token each: loads, six steps of a sum, a search, stores).  Else a second launch does, after all workgroups have read what it may write over.
+// are the time (64 sequences of one token each, 5.1 us a call: loads, six steps of a sum, a search, stores).  Of more rows a workgroup of its own does (27578 rows of 256 sequences: 5.7 us a call), or, where the
+// results may be written over what other workgroups read, a second launch (13.8 us, then with 4096 rows to a workgroup).
 #include <hip/hip_runtime.h>
 #include "kvtc_cache.h"
 #include "kvtc_dev.h"
@@ -33,16 +34,16 @@ __device__ __forceinline__ uint32_t sum_to_end(uint32_t a, uint32_t b) {
     return s < kSumsEnd ? (uint32_t)s : kSumsEnd;
 }
 
-// ROWS: slots and positions are written; SEQS: the sequences' results.
+// ROWS: slots and positions of workgroup `group` of those that have rows are written; SEQS: the sequences' results.
 template <int THREADS, bool ROWS, bool SEQS>
-__global__ void __launch_bounds__(THREADS) place_kernel(const PlaceArgs a) {
+__device__ __forceinline__ void place_group(const PlaceArgs& a, uint32_t group) {
     constexpr int WAVES = THREADS / 64;
     __shared__ uint32_t end_of[THREADS], dealt_of[THREADS], sums[2][WAVES];
     __shared__ int32_t had_of[THREADS], start_of[THREADS];
     __shared__ uint32_t most_dealt;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t n_free = a.n_free[0];
-    const uint32_t row0 = ROWS ? blockIdx.x * (uint32_t)a.rows_each : 0u, row1 = ROWS ? min((uint32_t)a.n_tokens, row0 + (uint32_t)a.rows_each) : 0u;
+    const uint32_t row0 = ROWS ? group * (uint32_t)a.rows_each : 0u, row1 = ROWS ? min((uint32_t)a.n_tokens, row0 + (uint32_t)a.rows_each) : 0u;
     auto pages_of = [&](uint32_t n) { return n == 0u ? 0u : (uint32_t)(((uint64_t)(n - 1u) * a.page_mul) >> a.page_shift) + 1u; };
     if (tid == 0) most_dealt = 0u;
     uint32_t rows_before = 0, dealt_before = 0;
@@ -142,13 +143,41 @@ __global__ void __launch_bounds__(THREADS) place_kernel(const PlaceArgs a) {
     }
 }
 
-constexpr int kPlaceRows = 4096;                           // rows of a workgroup
+template <int THREADS, bool ROWS, bool SEQS>
+__global__ void __launch_bounds__(THREADS) place_kernel(const PlaceArgs a) {
+    place_group<THREADS, ROWS, SEQS>(a, blockIdx.x);
+}
+// The first workgroup writes the sequences' results.
+__global__ void __launch_bounds__(1024) place_all_kernel(const PlaceArgs a) {
+    if (blockIdx.x == 0) place_group<1024, false, true>(a, 0u);
+    else place_group<1024, true, false>(a, blockIdx.x - 1u);
+}
 
-hipError_t launch_place(const PlaceArgs& a, hipStream_t stream) {
-    const int groups = (int)(((int64_t)a.n_tokens + kPlaceRows - 1) / kPlaceRows);
-    if (groups <= 1) {
+constexpr int kPlaceRows = 4096, kPlaceRowsEach = 1024;    // rows of a workgroup that is alone, and of one among others
+
+// Whether nothing that a workgroup reads is written by another: results in buffers of their own.
+static bool place_apart(const PlaceArgs& a) {
+    struct Range { uintptr_t at, bytes; };
+    const size_t seqs = (size_t)a.n_seqs * 4;
+    const Range in[3] = {{reinterpret_cast<uintptr_t>(a.had), seqs}, {reinterpret_cast<uintptr_t>(a.fresh), seqs}, {reinterpret_cast<uintptr_t>(a.n_free), 4}};
+    const Range out[3] = {{reinterpret_cast<uintptr_t>(a.lengths), seqs}, {reinterpret_cast<uintptr_t>(a.starts), seqs + 4}, {reinterpret_cast<uintptr_t>(a.left), 4}};
+    for (const Range& i : in)
+        for (const Range& o : out)
+            if (i.at < o.at + o.bytes && o.at < i.at + i.bytes) return false;
+    return true;
+}
+
+hipError_t launch_place(PlaceArgs a, hipStream_t stream) {
+    if (a.n_tokens <= kPlaceRows) {
+        a.rows_each = kPlaceRows;
         if (a.n_seqs <= 256 && a.n_tokens <= 1024) hipLaunchKernelGGL((place_kernel<256, true, true>), dim3(1), dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((place_kernel<1024, true, true>), dim3(1), dim3(1024), 0, stream, a);
+        return hipGetLastError();
+    }
+    a.rows_each = kPlaceRowsEach;
+    const int groups = (int)(((int64_t)a.n_tokens + kPlaceRowsEach - 1) / kPlaceRowsEach);
+    if (place_apart(a)) {
+        hipLaunchKernelGGL(place_all_kernel, dim3(groups + 1), dim3(1024), 0, stream, a);
         return hipGetLastError();
     }
     hipLaunchKernelGGL((place_kernel<1024, true, false>), dim3(groups), dim3(1024), 0, stream, a);
@@ -190,7 +219,6 @@ extern "C" kvtc_status kvtc_cache_place(int n_seqs, const int32_t* lengths_dev, 
     a.n_seqs = n_seqs;
     a.n_tokens = (int32_t)n_tokens;
     a.page_tokens = page_tokens;
-    a.rows_each = kPlaceRows;
     uint32_t s = 0;                                        // (n < 2^31: m = ceil(2^(31 + s) / d) is near enough)
     while ((1ull << s) < (uint64_t)page_tokens) ++s;
     a.page_mul = (uint32_t)(((1ull << (31 + s)) + page_tokens - 1) / page_tokens);
