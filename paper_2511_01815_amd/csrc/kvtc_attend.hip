@@ -45,7 +45,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttendCols = 16;                            // query heads of an item, at most
-constexpr int kAttendMaxShares = 1024;                     // shares of a launch, at most: a counter each in the workspace
 // Rows of at most so many pieces may be a wave's each, whole: no shares to find, nothing to join, and a workgroup takes the next row as it ends; but the last rows run alone, and in 4 bits
 // a step is of one piece.  (256 rows of 8 heads of 128 features, us, shares and so.  bf16: 40 tokens 20.4 and 13.5, 300 65.6 and 61.4, 100 to 1000 102 and 94, 200 to 2000 166 and 178; 8 bits: 300
 // 45.2 and 36.9, 100 to 1000 77.5 and 67.8, 200 to 2000 110 and 126; 4 bits: 300 49.6 and 38.8, 512 61.8 and 58.6, 1 to 600 41.9 and 53.9, 100 to 1000 76 and 92.)

@@ -8,6 +8,7 @@ namespace kvtc {
 
 constexpr int kCacheMaxHeads = 1024;
 constexpr int kAttendMaxSeqs = 65536;
+constexpr int kAttendMaxShares = 1024;                     // shares of a kvtc_attend, at most: a counter each at the workspace's begin, which calls leave zero and kvtc_attend_many keeps clear of
 constexpr int kCacheGroup = 32;                            // features that share a shift and a scale in the 4-bit format
 
 __host__ __device__ constexpr int cache_row_bytes(int format, int d) { return format == KVTC_CACHE_BF16 ? 2 * d : format == KVTC_CACHE_FP8 ? d : d / 2; }

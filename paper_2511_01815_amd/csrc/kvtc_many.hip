@@ -461,7 +461,7 @@ size_t many_work_bytes(const kvtc_cache& c, int n_seqs, int64_t n_tokens, int n_
         const size_t need = parts > 1 ? (size_t)parts * (size_t)n_tokens * n_q_heads * (c.d_head + 2) * sizeof(float) : 0;
         most = need > most ? need : most;
     }
-    return most + 256;
+    return most + kAttendMaxShares * 4;
 }
 
 hipError_t launch_many_mfma_0(const ManyPlan& p, hipStream_t stream);
@@ -504,7 +504,7 @@ hipError_t launch_many(const ManyArgs& a, kvtc_dtype dtype, hipStream_t stream) 
     p.page_mul = (uint32_t)(((1ull << (31 + s)) + a.c.page_tokens - 1) / a.c.page_tokens);
     p.page_shift = 31 + s;
     const int64_t rows = (int64_t)a.n_tokens * a.n_q_heads;
-    p.part_out = static_cast<float*>(a.work);
+    p.part_out = static_cast<float*>(a.work) + kAttendMaxShares;           // (behind kvtc_attend's counters)
     p.part_sums = reinterpret_cast<float2*>(p.part_out + (p.r.parts > 1 ? p.r.parts * rows * a.c.d_head : 0));
     hipError_t e;
     if (p.r.kind == kManyPlain) {

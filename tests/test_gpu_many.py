@@ -393,6 +393,51 @@ def test_calls_that_share_a_workspace():
             assert torch.equal(g[0], a[0]) and torch.equal(g[1], a[1])
 
 
+def test_a_workspace_shared_with_single_tokens():
+    """kvtc_attend counts on zeros that it left; calls of kvtc_attend_many in between, whatever else the workspace holds, do not change what either gives."""
+    rng = np.random.default_rng(23)
+    many = [Case(rng, "fp8", 128, 2, 4, 16, "heads", [5, 3], [6000, 300], kv.KVTC_BF16), Case(rng, "bf16", 64, 2, 1, 16, "heads", [4], [2500], kv.KVTC_F32)]
+    one = Case(rng, "bf16", 128, 2, 4, 16, "heads", [1] * 3, [9000, 40, 2000], kv.KVTC_BF16, before=0, behind=0)
+    hq, most = one.q.shape[1], max(one.lengths)
+    need = max([kv.kvtc_attend_many_work_bytes(c.cache, len(c.new), c.rows, c.q.shape[1], max(c.lengths)) for c in many] + [kv.kvtc_attend_work_bytes(one.cache, 3, hq, most)])
+    work = torch.zeros(need, dtype=torch.uint8, device=DEV)
+
+    def step():
+        out, lse = torch.empty_like(one.q_dev), torch.empty((3, hq), device=DEV)
+        kv.kvtc_attend(one.cache, one.q_dev, kv.KVTC_BF16, 3, hq, hq * one.d, one.d, one.table_dev, one.table.shape[1], one.lengths_dev, most, one.scale, 0, 0, out, lse, work, work.numel())
+        return out, lse
+
+    want_many, want = [c.run() for c in many], step()
+    for _ in range(3):
+        for c, w in zip(many, want_many):
+            got = c.run(work=work)
+            assert torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
+            again = step()
+            assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+    garbage = torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)      # of any contents, for kvtc_attend_many
+    for c, w in zip(many, want_many):
+        got = c.run(work=garbage)
+        assert torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
+    assert (garbage[:4096] == 0xFF).all()
+
+
+def test_calls_at_once_on_two_streams():
+    """Each with a workspace of its own."""
+    rng = np.random.default_rng(29)
+    cases = [Case(rng, "int4", 128, 2, 4, 16, "heads", [6, 3], [5000, 300], kv.KVTC_BF16), Case(rng, "bf16", 128, 2, 4, 20, "tokens", [40, 33], [1500, 64], kv.KVTC_BF16)]
+    alone = [c.run() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[] for _ in cases]
+    for _ in range(8):
+        for g, c, s in zip(got, cases, streams):
+            with torch.cuda.stream(s):
+                g.append(c.run(stream=s.cuda_stream))
+    torch.cuda.synchronize()
+    for g, a in zip(got, alone):
+        assert all(torch.equal(x[0], a[0]) and torch.equal(x[1], a[1]) and int(x[2].item()) == 0 for x in g)
+
+
 def test_places_positions_tokens_and_attention_under_capture():
     """A recorded step -- places, rotations of queries and keys, tokens written, attention over them and over a shared prefix, joined -- with new inputs in the same buffers, as eager calls, on every replay; and the
     eager calls against the oracle's values."""
