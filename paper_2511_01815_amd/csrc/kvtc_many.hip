@@ -20,6 +20,7 @@ kvtc_status set_error(kvtc_status st, const char* fmt, ...);
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #define KVTC_GLOBAL __attribute__((address_space(1)))
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -286,86 +287,135 @@ __global__ void __launch_bounds__(256) many_plain_kernel(const ManyPlan p) {
 
 // ---- parts of an item's tiles, joined ------------------------------------------------------------------------------------------
 
-// WAVES waves to a row, among which its parts are shared; eight parts' loads of a wave together.  (24 rows of 64 parts, heads of 128: one after another 121 us.)
-template <typename XT, int D, int WAVES>
-__global__ void __launch_bounds__(256) many_join_kernel(const ManyPlan p) {
-    constexpr int N = D / 64, ROWS = 4 / WAVES;
+// Few rows: a workgroup to a row, its four waves take parts in turn, eight parts' loads of a wave together.  (24 rows of 64 parts, heads of 128: one after another 121 us, so 5.9.)
+template <typename XT, int D>
+__global__ void __launch_bounds__(256) many_join_few_kernel(const ManyPlan p) {
+    constexpr int N = D / 64, WAVES = 4;
     typedef float Features __attribute__((ext_vector_type(N == 1 ? 2 : N)));
-    __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
+    __shared__ float sums[WAVES][D], of_waves[WAVES];
     ManyItem it;
-    if (!many_item(p, blockIdx.x, it) || it.tiles <= p.r.part_tiles) return;
-    const int head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = wave % WAVES;
+    if (!many_item(p, blockIdx.x, it) || it.tiles <= p.r.part_tiles || (int)blockIdx.z >= it.rows) return;
+    const int head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int parts = (int)((it.tiles + p.r.part_tiles - 1) / p.r.part_tiles);
     const int64_t all = (int64_t)p.a.n_tokens * p.a.n_q_heads;
-    for (int row0 = blockIdx.z * ROWS; row0 < it.rows; row0 += gridDim.z * ROWS) {
-        const int row = row0 + wave / WAVES, r = it.row0 + (row < it.rows ? row : it.rows - 1), token = r / p.group, q_head = head * p.group + r - token * p.group;
+    const int r = it.row0 + (int)blockIdx.z, token = r / p.group, q_head = head * p.group + r - token * p.group;
+    const int64_t place = (int64_t)(it.first + token) * p.a.n_q_heads + q_head;
+    float m = kNoScore, l = 0.0f;
+    for (int i = lane; i < parts; i += 64) m = fmaxf(m, p.part_sums[i * all + place].x);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    const float base = m == kNoScore ? 0.0f : m;
+    float o[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = 0.0f;
+    for (int i0 = wave; i0 < parts; i0 += 8 * WAVES) {
+        float x[8][N];
+        float2 s[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = i0 + k * WAVES < parts ? i0 + k * WAVES : wave;
+            s[k] = p.part_sums[i * all + place];
+            const float* from = p.part_out + (i * all + place) * D + lane * N;
+            if constexpr (N == 1) {
+                x[k][0] = from[0];
+            } else {
+                const Features v = *reinterpret_cast<const Features*>(from);
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[k][j] = v[j];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i0 + k * WAVES < parts) {
+                const float share = exp2_fast(s[k].x - base);
+                l += s[k].y * share;
+#pragma unroll
+                for (int j = 0; j < N; ++j) o[j] += x[k][j] * share;
+            }
+    }
+    if (lane == 0) of_waves[wave] = l;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sums[wave][lane * N + j] = o[j];
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < WAVES; ++w) {
+        l += of_waves[w];
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[j] += sums[w][lane * N + j];
+    }
+    const bool none = m == kNoScore && l == 0.0f;
+    XT* out = static_cast<XT*>(p.a.out) + place * D + lane * N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float v = none ? 0.0f : o[j] / l;
+        if constexpr (sizeof(XT) == 2) out[j] = f32_bf16(v);
+        else out[j] = v;
+    }
+    if (p.a.lse && lane == 0) p.a.lse[place] = none ? kNoScore : (m + __builtin_log2f(l)) * kLn2;
+}
+
+// Many rows: D / 4 lanes to each, several rows to a wave, four parts together, in one pass with a running maximum: what an item's workgroups wait for is its sequence and a part's loads once or twice.
+template <typename XT, int D>
+__global__ void __launch_bounds__(256) many_join_kernel(const ManyPlan p) {
+    constexpr int LANES = D / 4, AT_ONCE = 256 / LANES;
+    ManyItem it;
+    if (!many_item(p, blockIdx.x, it) || it.tiles <= p.r.part_tiles) return;
+    const int head = blockIdx.y, lane = threadIdx.x % LANES;
+    const int parts = (int)((it.tiles + p.r.part_tiles - 1) / p.r.part_tiles);
+    const int64_t all = (int64_t)p.a.n_tokens * p.a.n_q_heads;
+    for (int row = blockIdx.z * AT_ONCE + threadIdx.x / LANES; row < it.rows; row += gridDim.z * AT_ONCE) {
+        const int r = it.row0 + row, token = r / p.group, q_head = head * p.group + r - token * p.group;
         const int64_t place = (int64_t)(it.first + token) * p.a.n_q_heads + q_head;
         float m = kNoScore, l = 0.0f;
-        for (int i = lane; i < parts; i += 64) m = fmaxf(m, p.part_sums[i * all + place].x);
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i0 = 0; i0 < parts; i0 += 4) {
+            f32x4 x[4];
+            float2 s[4];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-        const float base = m == kNoScore ? 0.0f : m;
-        float o[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) o[j] = 0.0f;
-        for (int i0 = mine; i0 < parts; i0 += 8 * WAVES) {
-            float x[8][N];
-            float2 s[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int i = i0 + k * WAVES < parts ? i0 + k * WAVES : mine;
-                s[k] = p.part_sums[i * all + place];
-                const float* from = p.part_out + (i * all + place) * D + lane * N;
-                if constexpr (N == 1) {
-                    x[k][0] = from[0];
-                } else {
-                    const Features v = *reinterpret_cast<const Features*>(from);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) x[k][j] = v[j];
-                }
+            for (int k = 0; k < 4; ++k) {
+                const int64_t at = (i0 + k < parts ? i0 + k : i0) * all + place;
+                s[k] = p.part_sums[at];
+                x[k] = *reinterpret_cast<const f32x4*>(p.part_out + at * D + 4 * lane);
             }
+            float now = m;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i0 + k * WAVES < parts) {
+            for (int k = 0; k < 4; ++k) now = fmaxf(now, s[k].x);
+            const float base = now == kNoScore ? 0.0f : now, keep = exp2_fast(m - base);
+            m = now;
+            l *= keep;
+            o *= keep;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i0 + k < parts) {
                     const float share = exp2_fast(s[k].x - base);
                     l += s[k].y * share;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) o[j] += x[k][j] * share;
+                    o += x[k] * share;
                 }
         }
-        if constexpr (WAVES > 1) {
-            __shared__ float of_waves[WAVES];
-            __syncthreads();
-            if (lane == 0) of_waves[mine] = l;
-#pragma unroll
-            for (int j = 0; j < N; ++j) sums[mine][lane * N + j] = o[j];
-            __syncthreads();
-            if (mine > 0) continue;
-            for (int w = 1; w < WAVES; ++w) {
-                l += of_waves[w];
-#pragma unroll
-                for (int j = 0; j < N; ++j) o[j] += sums[w][lane * N + j];
-            }
-        }
-        if (row >= it.rows) continue;
         const bool none = m == kNoScore && l == 0.0f;
-        XT* out = static_cast<XT*>(p.a.out) + place * D + lane * N;
+        XT* out = static_cast<XT*>(p.a.out) + place * D + 4 * lane;
+        f32x4 v;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float v = none ? 0.0f : o[j] / l;
-            if constexpr (sizeof(XT) == 2) out[j] = f32_bf16(v);
-            else out[j] = v;
+        for (int j = 0; j < 4; ++j) v[j] = none ? 0.0f : o[j] / l;
+        if constexpr (sizeof(XT) == 2) {
+            u32x2 w;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) w[j] = (uint32_t)f32_bf16(v[2 * j]) | (uint32_t)f32_bf16(v[2 * j + 1]) << 16;
+            *reinterpret_cast<u32x2*>(out) = w;
+        } else {
+            *reinterpret_cast<f32x4*>(out) = v;
         }
         if (p.a.lse && lane == 0) p.a.lse[place] = none ? kNoScore : (m + __builtin_log2f(l)) * kLn2;
     }
 }
 template <typename XT, int D>
 static void launch_join_width(const ManyPlan& p, hipStream_t stream) {
-    const bool few = (int64_t)p.a.n_tokens * p.a.n_q_heads <= 8 * compute_units();
-    const uint32_t each = few ? 1 : 16;                    // rows of a workgroup
-    const dim3 grid(p.r.items, p.a.c.n_heads, (p.r.rows + each - 1) / each);
-    if (few) hipLaunchKernelGGL((many_join_kernel<XT, D, 4>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((many_join_kernel<XT, D, 1>), grid, dim3(256), 0, stream, p);
+    constexpr int each = 2 * 256 / (D / 4);                // rows of a workgroup
+    if ((int64_t)p.a.n_tokens * p.a.n_q_heads <= 8 * compute_units()) {
+        hipLaunchKernelGGL((many_join_few_kernel<XT, D>), dim3(p.r.items, p.a.c.n_heads, p.r.rows), dim3(256), 0, stream, p);
+    } else {
+        hipLaunchKernelGGL((many_join_kernel<XT, D>), dim3(p.r.items, p.a.c.n_heads, (p.r.rows + each - 1) / each), dim3(256), 0, stream, p);
+    }
 }
 template <typename XT>
 static hipError_t launch_join(const ManyPlan& p, hipStream_t stream) {
