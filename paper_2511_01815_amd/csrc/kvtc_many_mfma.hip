@@ -17,6 +17,10 @@
 //
 // Tiles of which some row does not see all (or that have no page) are masked, row by row, as 32 bits to 32 tokens.  Their values that are not finite are zeros in the LDS, lest a probability of zero make NaN of them, and are added
 // afterwards to the rows that see them.
+//
+// What bounds it.  Large calls: matrix products and, by the same waves in between, the softmax; two workgroups to a compute unit work at both at once.  A prompt of 8192 tokens, 32 query heads of 128 to 8: 550 us, 1000 TFLOP/s of
+// products that count, 81 % of what a large product alone reaches here (both at the clock that power leaves).  2048 tokens behind 30720: 1397 us in 8 bits, 1633 in 4: the vector unit, with scales, codes to numbers and the softmax.
+// Few items: a tile's chain of instructions, 1.0 to 2.3 us with one workgroup to a compute unit, hence parts; 6 tokens behind 131066 in 8 bits 65 us, 4.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <type_traits>
 #include "kvtc_dev.h"

@@ -16,7 +16,7 @@ CALLS = [(1, 1, [1], [0]), (2, 3, [1], [699]), (2, 1, [1, 1], [699, 20]), (1, 1,
          (8, 4, [33], [3967]), (4, 4, [9, 7], [7991, 300]), (32, 4, [150], [0]), (32, 6, [150], [0]), (32, 1, [1], [7999]), (1, 1, [1] * 5, [3999, 0, 64, 31, 700]), (1, 1, [17, 0] + [16] * 14, [7983] + [100] * 15),
          (2, 1, [1] * 64, [7999] + [33] * 63), (1, 1, [300] + [200] * 15, [3700] + [i for i in range(15)]), (4, 4, [33, 31], [7967, 700]),
          (32, 6, [33] * 64, [0] * 64), (1, 1, [300] * 16, [3700] + [9 * i for i in range(15)]), (4, 4, [7, 7], [7993, 300]), (4, 6, [33] * 64, [0] * 64), (8, 4, [33] * 64, [0] * 64),
-         (1, 1, [1] * 16, [3999] + [7 * i for i in range(15)])]
+         (32, 1, [1], [11999]), (4, 1, [1], [8999]), (1, 1, [1] * 16, [3999] + [7 * i for i in range(15)])]
 
 
 def reached(fmt, d):
