@@ -96,14 +96,16 @@ struct Eighth {
     }
 };
 
-__device__ __forceinline__ float max_over_quarters(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+// Of lanes 16, 32 and 48 apart.  (A swap with itself gives a lane its own and the other's, in either order.)
+template <typename FN>
+__device__ __forceinline__ float over_quarters(float v, FN both) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = both(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return both(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ float sum_over_quarters(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
-}
+__device__ __forceinline__ float max_over_quarters(float v) { return over_quarters(v, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float sum_over_quarters(float v) { return over_quarters(v, [](float x, float y) { return x + y; }); }
 __device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // Four waves of 16 rows; a row's scores over lanes 16 apart, four neighbouring tokens of every 16 to each.

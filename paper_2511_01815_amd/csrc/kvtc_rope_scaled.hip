@@ -6,7 +6,8 @@
 //
 // Angles, sines and cosines are double precision -- an angle reaches 10^6 radians -- and rounded to fp32, the rotation is one product and one fused product in fp32, rounded once more to bf16.
 // A workgroup has some tokens: first it works out their sines and cosines, one to a thread, into the LDS, for all heads; then threads take units of two pieces, the a's and the b's of
-// some neighbouring pairs, of up to 16 bytes each.
+// some neighbouring pairs, of up to 16 bytes each.  Large calls are bound by memory (20001 tokens of 12 heads of 64 in fp32, 123 MB: 30.5 us, 4.0 TB/s), small ones by the launch and the double precision
+// (64 tokens of 40 heads: 4.2 us in the kernel).
 #include <hip/hip_runtime.h>
 #include <cmath>
 #include <cstring>
