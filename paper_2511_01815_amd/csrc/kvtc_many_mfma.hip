@@ -116,8 +116,9 @@ struct Shape {
     // Where a wave's tokens are those that it brings in, it waits for no other, and numbers that it makes itself need one buffer.
     static constexpr bool ALONE = RW == 1;
     static constexpr int BUFFERS = ALONE && !is_bf16<F>() ? 1 : 2;
-    // behind the buffers of keys and values: exponents of 16 tokens' keys and values; 8 bits: every token's scales; tokens with values that are not finite, by waves
-    static constexpr int kExponents = 2 * BUFFERS * BUFFER, kScales = kExponents + BUFFERS * 2 * (TILE / 16) * 4, kWild = kScales + (F == KVTC_CACHE_FP8 ? BUFFERS * 2 * TILE * 4 : 0),
+    // behind the buffers of keys and values: exponents of 16 tokens' keys and values; 8 bits: every token's scales, 4 bits: its keys' scales and shifts; tokens with values that are not finite, by waves
+    static constexpr int G = F == KVTC_CACHE_INT4 ? D / 32 : 0;              // groups of a row with a header each
+    static constexpr int kExponents = 2 * BUFFERS * BUFFER, kScales = kExponents + BUFFERS * (TILE / 16) * 4, kWild = kScales + (F == KVTC_CACHE_FP8 ? BUFFERS * 2 * TILE * 4 : BUFFERS * TILE * G * 6),
                          kLds = kWild + BUFFERS * NW * 4;
     static_assert(RPW % 16 == 0, "");
 };
@@ -177,6 +178,22 @@ struct Quarter {
             return m;
         }
     }
+    // A byte's codes in fp16: the low one behind 1024, the high one behind 64, where they stand.
+    __device__ __forceinline__ f16x2 codes(int byte) const {
+        const uint32_t twice = __builtin_amdgcn_perm(w[byte / 4], w[byte / 4], 0x0c000c00u | (uint32_t)(byte % 4) | (uint32_t)(byte % 4) << 16);
+        return __builtin_bit_cast(f16x2, (twice & 0x00f0000fu) | 0x54006400u) - f16x2{(_Float16)1024.0f, (_Float16)64.0f};
+    }
+    // 4 bits: each(), of the codes.
+    template <typename FN>
+    __device__ __forceinline__ void each_code(int quarter, FN f) const {
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {
+            u32x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(uint32_t, codes(j * (D / 32) + g));
+            f(4 * g + quarter, v);
+        }
+    }
     // f(piece, its eight features in fp16) for the quarter's pieces.  8 bits: the codes; 4 bits: values times 2^-e.
     template <typename FN>
     __device__ __forceinline__ void each(int quarter, int e, FN f) const {
@@ -202,13 +219,7 @@ struct Quarter {
                 }
                 const f16x2 shift = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(header, header, 0x01000100u)), size = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(header, header, 0x03020302u));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // a byte's low code, behind 1024, and its high one, behind 64, where they stand
-                    const int byte = j * G + g;
-                    const uint32_t twice = __builtin_amdgcn_perm(w[byte / 4], w[byte / 4], 0x0c000c00u | (uint32_t)(byte % 4) | (uint32_t)(byte % 4) << 16);
-                    const f16x2 codes = __builtin_bit_cast(f16x2, (twice & 0x00f0000fu) | 0x54006400u) - f16x2{(_Float16)1024.0f, (_Float16)64.0f};
-                    v[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(codes, size, shift));
-                }
+                for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(codes(j * G + g), size, shift));
                 f(4 * g + quarter, v);
             }
         }
@@ -268,7 +279,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                     most = fmaxf(most, fmaxf(not_finite(a) ? 0.0f : a, not_finite(b) ? 0.0f : b));
                 }
             most = max_of_halves(most);
-            const int e = most == 0.0f ? 0 : exponent_of(most) - 14;
+            const int e = most == 0.0f ? 0 : exponent_of(most) - (F == KVTC_CACHE_INT4 ? 9 : 14);      // (4 bits: and sums of 32 below 2^15)
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -277,6 +288,42 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             factor = __builtin_amdgcn_ldexpf(factor, e);
         }
         factor = __builtin_amdgcn_fmed3f(factor, kLeastFactor, kMostFactor);
+    }
+    // 4 bits: a row's queries summed over each group, in three parts of fp16 (33 bits): part c of group g is number c * G + g of the operand that goes with the tokens' shifts
+    constexpr int G = S::G, NSHIFT = (3 * G + 15) / 16;
+    u32x4 q_sums[F == KVTC_CACHE_INT4 ? NSHIFT : 1];
+    if constexpr (F == KVTC_CACHE_INT4) {
+        float part[3][G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int s = 2 * g; s < 2 * g + 2; ++s)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f16x2 v = __builtin_bit_cast(f16x2, (uint32_t)q[s][j]);
+                    sum += (float)v[0] + (float)v[1];
+                }
+            sum = sum_of_halves(sum);
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+                part[c][g] = (float)(_Float16)sum;
+                sum -= part[c][g];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NSHIFT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int low = 16 * n + 2 * j + i, high = low + 8;
+                    const float of_low = low < 3 * G ? part[low / G % 3][low % G] : 0.0f, of_high = high < 3 * G ? part[high / G % 3][high % G] : 0.0f;
+                    v[i] = half ? of_high : of_low;
+                }
+                q_sums[n][j] = round_pair<F>(v[0], v[1]);
+            }
     }
     f32x16 o[NF];
 #pragma unroll
@@ -426,8 +473,9 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             }
         }
     };
-    float* exponents = reinterpret_cast<float*>(lds + S::kExponents);        // [buffer][keys, values][16 tokens]
-    float* scales = reinterpret_cast<float*>(lds + S::kScales);              // [buffer][keys, values][token]: 8 bits, values' without the 16 tokens' exponent
+    float* exponents = reinterpret_cast<float*>(lds + S::kExponents);        // [buffer][16 tokens]: of values
+    float* scales = reinterpret_cast<float*>(lds + S::kScales);              // 8 bits: [buffer][keys, values][token], values' without the 16 tokens' exponent; 4 bits: [buffer][group][token], of keys
+    uint16_t* shifts = reinterpret_cast<uint16_t*>(lds + S::kScales + S::BUFFERS * TILE * G * 4);      // 4 bits: [buffer][token][group], of keys
     uint32_t* wild = reinterpret_cast<uint32_t*>(lds + S::kWild);            // [buffer][wave]: of its tokens, a bit each, those with values that are not finite
     // 8 and 4 bits: into the LDS, as numbers.
     auto settle = [&](int buffer, bool masked) {
@@ -438,7 +486,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 const int in_group = lane >> 2, quarter = lane & 3, t = wave * RPW + 16 * g + in_group;
                 const bool is = (have[TILE > 64 ? (wave * RPW) / 64 : 0] >> (t & 63) & 1u) != 0;
                 auto over_rows = [&](float v) { return __uint_as_float(same(__float_as_uint(max_of_quarters(v)))); };
-                int ke = 0, ve;
+                int ve;
                 float value_scale = 0.0f;
                 bool odd = false;
                 const float v_most = over_rows(is ? vq[g].most() : 0.0f);
@@ -454,17 +502,21 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                         scales[(buffer * 2 + 1) * TILE + t] = __builtin_amdgcn_ldexpf(value_scale, -ve);
                     }
                 } else {
-                    const float k_most = over_rows(is ? kq[g].most() : 0.0f);
-                    ke = max(0, exponent_of(k_most) - 14);
                     ve = max(0, exponent_of(v_most) - 14);
+                    if (quarter == 0) {
+#pragma unroll
+                        for (int i = 0; i < G; ++i) {
+                            scales[(buffer * G + i) * TILE + t] = (float)__builtin_bit_cast(_Float16, (uint16_t)(kq[g].scale[i] >> 16));
+                            shifts[(buffer * TILE + t) * G + i] = (uint16_t)kq[g].scale[i];
+                        }
+                    }
                 }
-                if (lane == 0) {
-                    exponents[(buffer * 2 + 0) * (TILE / 16) + wave * NG + g] = (float)ke;
-                    exponents[(buffer * 2 + 1) * (TILE / 16) + wave * NG + g] = (float)ve;
-                }
+                if (lane == 0) exponents[buffer * (TILE / 16) + wave * NG + g] = (float)ve;
                 uint8_t* to_k = lds + buffer * 2 * S::BUFFER + t * S::ROW;
                 uint8_t* to_v = to_k + S::BUFFER;
-                kq[g].each(quarter, ke, [&](int piece, u32x4 w) { *reinterpret_cast<u32x4*>(to_k + ((piece ^ key_turn<D>(t)) << 4)) = w; });
+                auto put_key = [&](int piece, u32x4 w) { *reinterpret_cast<u32x4*>(to_k + ((piece ^ key_turn<D>(t)) << 4)) = w; };
+                if constexpr (F == KVTC_CACHE_FP8) kq[g].each(quarter, 0, put_key);
+                else kq[g].each_code(quarter, put_key);
                 vq[g].each(quarter, F == KVTC_CACHE_FP8 ? 0 : ve, [&](int piece, u32x4 w) {
                     if (masked) {
 #pragma unroll
@@ -527,26 +579,63 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
     // (masked tiles by the same code, with a step more where it is needed: with code of their own for them outputs were moved from registers to registers)
     u32x4 pr[2 * NB];                                      // probabilities
     auto scores = [&](bool masked, uint32_t n, int buffer, const uint64_t (&mine)[(TILE + 63) / 64]) {
-        const uint32_t shift = buffer * 2 * S::BUFFER;
+        const uint32_t shift_of_buffer = buffer * 2 * S::BUFFER;
         const int t0 = (int)(many_tile(it, n) * TILE + tw * NT);
         f32x16 s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < NS; ++k)
+        if constexpr (F == KVTC_CACHE_INT4) {
+            // sum over groups of scale * (codes . queries) + shift * (sum of queries)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const u32x4 a = *reinterpret_cast<const KVTC_LDS u32x4*>((uintptr_t)(k_at[k & 7] + shift + b * 32 * S::ROW + (k >> 3) * 256));
-                s[b] = mfma<F>(a, q[k], s[b]);
-            }
-        // (a few loads ahead of the products, no more: the compiler left to itself puts them all first, and what they load does not fit the registers)
-        __builtin_amdgcn_sched_group_barrier(kLdsReads, F == KVTC_CACHE_INT4 ? 4 : 8, 0);
+                const int t = tw * NT + 32 * b;
+                u32x4 shift;
+                if constexpr (G == 2) {
+                    const uint32_t w = *reinterpret_cast<const uint32_t*>(shifts + (buffer * TILE + t + col) * G);
+                    shift = u32x4{w, w, w, w};
+                } else if constexpr (G == 4) {
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(shifts + (buffer * TILE + t + col) * G);
+                    shift = u32x4{w[0], w[1], w[0], w[1]};
+                } else {
+                    shift = *reinterpret_cast<const u32x4*>(shifts + (buffer * TILE + t + col) * G);
+                }
 #pragma unroll
-        for (int k = 0; k < NS * NB; ++k) {
-            __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+                for (int n = 0; n < NSHIFT; ++n) s[b] = mfma<F>(shift, q_sums[n], s[b]);
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    f32x16 dot;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dot[i] = 0.0f;
+#pragma unroll
+                    for (int k = 2 * g; k < 2 * g + 2; ++k) {
+                        const u32x4 a = *reinterpret_cast<const KVTC_LDS u32x4*>((uintptr_t)(k_at[k & 7] + shift_of_buffer + b * 32 * S::ROW + (k >> 3) * 256));
+                        dot = mfma<F>(a, q[k], dot);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const f32x4 w = *reinterpret_cast<const f32x4*>(scales + (buffer * G + g) * TILE + t + 2 * i + 4 * half);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[b][i + j] = __builtin_fmaf(dot[i + j], w[j], s[b][i + j]);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const u32x4 a = *reinterpret_cast<const KVTC_LDS u32x4*>((uintptr_t)(k_at[k & 7] + shift_of_buffer + b * 32 * S::ROW + (k >> 3) * 256));
+                    s[b] = mfma<F>(a, q[k], s[b]);
+                }
+            // (a few loads ahead of the products, no more: the compiler left to itself puts them all first, and what they load does not fit the registers)
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 8, 0);
+#pragma unroll
+            for (int k = 0; k < NS * NB; ++k) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+            }
         }
         if constexpr (F == KVTC_CACHE_FP8) {
 #pragma unroll
@@ -572,18 +661,12 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 for (int i = 0; i < 16; ++i) s[b][i] = seen >> (8 * (i / 4) + i % 4) & 1u ? s[b][i] : kNoScore;
             }
         }
-        // the scores' factors and the values' exponents, of every 16 tokens
-        float c[2 * NB];
+        // the values' exponents, of every 16 tokens
         int ve[2 * NB], ve_most = kLeastExponent;
-        if constexpr (BF) {
-#pragma unroll
-            for (int g = 0; g < 2 * NB; ++g) c[g] = factor;
-        } else {
+        if constexpr (!BF) {
 #pragma unroll
             for (int g = 0; g < 2 * NB; ++g) {
-                const float* e = exponents + buffer * 2 * (TILE / 16) + tw * (NT / 16) + g;
-                c[g] = F == KVTC_CACHE_FP8 ? factor : __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(factor, (int)e[0]), kLeastFactor, kMostFactor);
-                ve[g] = (int)same((uint32_t)(int)e[TILE / 16]);
+                ve[g] = (int)same((uint32_t)(int)exponents[buffer * (TILE / 16) + tw * (NT / 16) + g]);
                 ve_most = max(ve_most, ve[g]);
             }
         }
@@ -596,11 +679,9 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 g0 = fmaxf(g0, s[b][i]);
                 g1 = fmaxf(g1, s[b][8 + i]);
             }
-            if constexpr (F != KVTC_CACHE_INT4) top = fmaxf(top, fmaxf(g0, g1));
-            else top = fmaxf(top, fmaxf(g0 * c[2 * b], g1 * c[2 * b + 1]));
+            top = fmaxf(top, fmaxf(g0, g1));
         }
-        if constexpr (F != KVTC_CACHE_INT4) top *= factor;
-        top = max_of_halves(top);
+        top = max_of_halves(top * factor);
         if (__any(top > m + slack<F>()) || (!BF && ve_most > exponent + kExponentSlack)) {
             const float now = fmaxf(m, top);
             base = now == kNoScore ? 0.0f : now;
@@ -625,7 +706,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
             float sum = 0.0f, e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                e[i] = exp2_fast(__builtin_fmaf(s[g / 2][8 * (g & 1) + i], c[g], -off));
+                e[i] = exp2_fast(__builtin_fmaf(s[g / 2][8 * (g & 1) + i], factor, -off));
                 sum += e[i];
             }
             l += BF ? sum : __builtin_amdgcn_ldexpf(sum, -dv);

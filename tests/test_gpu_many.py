@@ -321,6 +321,29 @@ def test_rows_of_very_different_scales(fmt):
     case.check(out, lse)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new,had", [([1, 2, 5], [0, 3, 0]), ([33, 1, 64], [0, 700, 200]), ([130], [1500])])
+def test_sums_over_four_bits_are_those_of_the_caches_own_keys(d, new, had):
+    """Where bf16 queries meet codes, lse is still fp32's: no key is rounded.  A score is the sum over groups of scale * (codes . q) + shift * (sum of q).  Sums of 32 products, two terms to each of d / 32 <= 8 groups and
+    three parts of the sum of q, all in fp32, are off by (32 + 16 + 3) 2^-24 < 2^-18 of M = sum of |q| (|shift| + 15 scale) <= 3 sum of |q| max |k| over a group, whose least and largest values have the codes 0 and 15; lse
+    is off by no more than its largest score, and by its own rounding and that of the sum: 2^-18 (1 + |lse|)."""
+    case = Case(np.random.default_rng(d + len(new)), "int4", d, 2, 3, 16, "heads", new, had, kv.KVTC_BF16)
+    out, lse, status = case.run()
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    lse = lse.double().cpu().numpy()
+    for b, n in enumerate(new):
+        for h in range(2):
+            k = kp.values(*case.pool.rows(0, case.slots[b], h), "int4", d)
+            group = np.repeat(np.abs(k).reshape(len(k), d // 32, 32).max(-1), 32, axis=1)
+            for i in range(n):
+                r, t, at = case.starts[b] + i, case.lengths[b] - n + i + 1, slice(3 * h, 3 * h + 3)
+                s = case.scale * (case.q[r, at].astype(np.float64) @ k[:t].T)
+                want = np.log(np.exp(s - s.max(-1, keepdims=True)).sum(-1)) + s.max(-1)
+                most = 1.02 * 3 * case.scale * (np.abs(case.q[r, at]) @ group[:t].T).max(-1)
+                assert (np.abs(lse[r, at] - want) <= 2.0 ** -18 * (most + 1 + np.abs(want))).all(), (b, h, i, np.abs(lse[r, at] - want).max(), most)
+
+
 def test_queries_inside_a_fused_projection_and_heads_first():
     rng = np.random.default_rng(6)
     case = Case(rng, "int4", 128, 2, 4, 64, "heads", [33, 1, 5], [333, 64, 0], kv.KVTC_BF16, behind=0)
