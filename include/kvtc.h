@@ -587,9 +587,9 @@ kvtc_status kvtc_rope_scaled(const void* x_dev, void* out_dev, kvtc_dtype dtype,
  *   status_dev    (device, may be null; the caller zeroes it) 1 + the lowest sequence whose starts are not ascending or not in 0..n_tokens (its rows are left as they are), whose length is negative
  *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen)
  * n_tokens * n_q_heads at most 2^29 (KVTC_E_UNSUPPORTED beyond).
- * fp32 queries: all in fp32.  bf16 queries: products of 16-bit numbers, summed in fp32.  Over bf16 pages those are what the cache and the queries hold and probabilities rounded to bf16; over 8 and 4 bits fp16:
- * 8-bit codes and queries as they are, probabilities rounded, 4-bit keys and values rounded (2^-11 of each; lse is off by as much as that moves scores).  What is more than 2^28 below the largest of a
- * row's queries, or its probabilities times values below the largest, may be lost; a result's own rounding to bf16 is the larger.
+ * fp32 queries: all in fp32.  bf16 queries: products of 16-bit numbers, summed in fp32; no key is rounded, so that lse is fp32's.  Over bf16 pages probabilities are rounded to bf16; over 8 and 4 bits to fp16, and
+ * 4-bit values too (2^-11 of each).  What is more than 2^28 (4 bits: 2^23) below the largest of a row's queries, or its probabilities times values 2^28 below the largest, may be lost; a result's own rounding to
+ * bf16 is the larger.
  * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 or n_tokens == 0 is a no-op.
  */
 size_t kvtc_attend_many_work_bytes(const kvtc_cache* cache, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens);     /* 0 for what kvtc_attend_many refuses */

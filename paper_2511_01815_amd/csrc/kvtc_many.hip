@@ -436,7 +436,7 @@ static ManyCost many_cost(int kind, int format, int d) {
     static constexpr ManyCost of_128[3][4] = {
         {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 1.36f, 2.15f}, {64, 64, 2, 1.0f, 1.33f}, {32, 128, 1, 1.2f, 1.55f}},
         {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 2.02f, 2.73f}, {64, 64, 2, 1.74f, 2.3f}, {32, 128, 2, 2.07f, 2.65f}},
-        {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 2.15f, 3.3f}, {64, 64, 2, 1.87f, 2.75f}, {32, 128, 2, 2.4f, 3.7f}}};
+        {{64, 32, 3, 4.0f, 8.2f}, {128, 64, 2, 2.45f, 3.8f}, {64, 64, 2, 2.1f, 3.1f}, {32, 128, 2, 2.7f, 4.2f}}};
     ManyCost c = of_128[format][kind];
     if (d == 64) {
         c.alone *= 0.6f;
