@@ -118,7 +118,7 @@ struct Shape {
     // Where a wave's tokens are those that it brings in, it waits for no other, and numbers that it makes itself need one buffer.
     static constexpr bool ALONE = RW == 1;
     static constexpr int BUFFERS = ALONE && !is_bf16<F>() ? 1 : 2;
-    // behind the buffers of keys and values: exponents of 16 tokens' keys and values; 8 bits: every token's scales, 4 bits: its keys' scales and shifts; tokens with values that are not finite, by waves
+    // behind the buffers of keys and values: exponents of 16 tokens' values; 8 bits: every token's scales, 4 bits: its keys' scales and shifts; tokens with values that are not finite, by waves
     static constexpr int G = F == KVTC_CACHE_INT4 ? D / 32 : 0;              // groups of a row with a header each
     static constexpr int kExponents = 2 * BUFFERS * BUFFER, kScales = kExponents + BUFFERS * (TILE / 16) * 4, kWild = kScales + (F == KVTC_CACHE_FP8 ? BUFFERS * 2 * TILE * 4 : BUFFERS * TILE * G * 6),
                          kLds = kWild + BUFFERS * NW * 4;
