@@ -98,14 +98,6 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int from) {
 }
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// 64 x 16 bytes from memory to the LDS, lane after lane from `to` on.  (The loads' counter is waited for before the barrier that ends the tile; m0 is only set where it is used.)
-__device__ __forceinline__ void to_lds(const void* base, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
-}
-__device__ __forceinline__ void to_lds(const void* at, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(at) : "memory");
-}
-
 template <int F, int D, int RW, int TW, int TOKENS>
 struct Shape {
     static constexpr int NW = RW * TW;
@@ -442,7 +434,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                     constexpr int each = NJ / NG;
 #pragma unroll
                     for (int j = 0; j < each; ++j) {
-                        to_lds((const void*)(uintptr_t)(from + off), off_of[g * each + j], to + (g * each + j) * 1024);
+                        dma16_async((const void*)(uintptr_t)(from + off), off_of[g * each + j], to + (g * each + j) * 1024);
                     }
                 }
             } else {
@@ -450,7 +442,7 @@ __global__ void __launch_bounds__(64 * RW * TW, D == 256 ? 1 : 2) many_mfma_kern
                 for (int j = 0; j < NJ; ++j) {
                     const uint32_t t = wave * RPW + (j * 1024 + lane * 16) / S::ROW;
                     const int64_t off = shfl64(rows_of[TILE > 64 ? (wave * RPW) / 64 : 0], t & 63);
-                    to_lds((const void*)(uintptr_t)(from + off + off_of[j]), to + j * 1024);
+                    dma16_async((const void*)(uintptr_t)(from + off + off_of[j]), to + j * 1024);
                 }
             }
         }
