@@ -460,8 +460,11 @@ __device__ __forceinline__ void dma16_async(const void* gsrc, uint32_t lds_byte_
 // per-transfer address arithmetic stays on the scalar unit and costs no vector registers.
 // (Values the compiler cannot prove uniform would reach the "s" operands in vector registers, so
 // both go through readfirstlane, which folds away when they already are scalar.)
+// The base may come out of a vector register just before -- by readfirstlane, or where scalars are parked in
+// lanes -- and a load must not read such a scalar within five wait states: the write of m0 and four more.  (The
+// compiler counts them for its own instructions, not into assembly.)
 __device__ __forceinline__ void dma16_async(const void* base_uniform, uint32_t lane_byte_off, uint32_t lds_byte_addr) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1"
                  :: "v"(lane_byte_off), "s"(uniform_ptr(reinterpret_cast<const char*>(base_uniform))),
                     "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr)) : "memory");
 }
@@ -472,14 +475,14 @@ __device__ __forceinline__ void dma16_async_once(const void* gsrc, uint32_t lds_
                  :: "v"(gsrc), "s"(lds_byte_addr) : "memory");
 }
 __device__ __forceinline__ void dma16_async_once(const void* base_uniform, uint32_t lane_byte_off, uint32_t lds_byte_addr) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1 nt"
                  :: "v"(lane_byte_off), "s"(uniform_ptr(reinterpret_cast<const char*>(base_uniform))),
                     "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr)) : "memory");
 }
 
 // One dword per lane: lane i's dword lands at lds_byte_addr + 4 * i.
 __device__ __forceinline__ void dma4_async(const void* base_uniform, uint32_t lane_byte_off, uint32_t lds_byte_addr) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dword %0, %1"
                  :: "v"(lane_byte_off), "s"(uniform_ptr(reinterpret_cast<const char*>(base_uniform))),
                     "s"(__builtin_amdgcn_readfirstlane(lds_byte_addr)) : "memory");
 }

@@ -1,4 +1,5 @@
-"""Waits that the hardware does not make by itself and the compiler does not put into inline assembly, read out of the sources: between a write of m0 and a load into the LDS that goes by it, one."""
+"""Waits that the hardware does not make by itself and the compiler does not put into inline assembly, read out of the sources: between a write of m0 and a load into the LDS that goes by it, one;
+between a scalar that comes out of a vector register and a load by that base, five (the compiler may put the former right before the assembly)."""
 import glob
 import os
 import re
@@ -35,3 +36,9 @@ def test_the_reader_finds_loads():
 def test_loads_into_the_lds_wait_for_their_address(source):
     for between, _ in loads_into_the_lds(open(os.path.join(CSRC, source)).read()):
         assert between is not None and waits(between) >= 1, source
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_loads_into_the_lds_wait_for_their_base(source):
+    for between, last in loads_into_the_lds(open(os.path.join(CSRC, source)).read()):
+        assert last == "off" or waits(between) + 1 >= 5, source              # (the write of m0 is one)
