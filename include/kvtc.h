@@ -585,7 +585,8 @@ kvtc_status kvtc_rope_scaled(const void* x_dev, void* out_dev, kvtc_dtype dtype,
  *                 for, with those of kvtc_attend as well (which has to have been zero before the first of these); calls that may overlap need one each.  Fewer tokens may need
  *                 more: where the sizes of calls differ, the most of what they need
  *   status_dev    (device, may be null; the caller zeroes it) 1 + the lowest sequence whose starts are not ascending or not in 0..n_tokens (its rows are left as they are), whose length is negative
- *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen)
+ *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen).  Of starts that do not ascend,
+ *                 a sequence that begins below a start before it (one in 0..n_tokens), whose rows may be another's, is left as well; the others are worked out
  * n_tokens * n_q_heads at most 2^29 (KVTC_E_UNSUPPORTED beyond).
  * fp32 queries: all in fp32.  bf16 queries: products of 16-bit numbers, summed in fp32; no key is rounded, so that lse is fp32's.  Over bf16 pages probabilities are rounded to bf16; over 8 and 4 bits to fp16, and
  * 4-bit values too (2^-11 of each).  What is more than 2^28 (4 bits: 2^23) below the largest of a row's queries, or its probabilities times values 2^28 below the largest, may be lost; a result's own rounding to

@@ -104,6 +104,21 @@ def seen(at: int, length: int, causal: bool, sinks: int, window: int) -> np.ndar
     return t if window == 0 else t[(t < sinks) | (t > at - window)]
 
 
+def served(starts, n_tokens: int):
+    """Starts of any kind, [B + 1] -> the sequences that attention of many new tokens works out, and what status is: 1 + the lowest whose starts do not ascend or leave 0..n_tokens, or 0.  Left out are those, and
+    what begins below a start before it (of those in 0..n_tokens), whose rows may be another's."""
+    out, bad, top = [], 0, 0
+    for b in range(len(starts) - 1):
+        s0, s1 = int(starts[b]), int(starts[b + 1])
+        if 0 <= s0 <= n_tokens:
+            top = max(top, s0)
+        if not 0 <= s0 <= s1 <= n_tokens:
+            bad = bad or b + 1
+        elif s0 == top:
+            out.append(b)
+    return out, bad
+
+
 def bound(q, k, v, scale, key_bits, kept_bits, value_bits, out_bits):
     """kvtc_paged.attend_bound where keys, probabilities and values enter their products rounded to key_bits, kept_bits and value_bits (each off by 2^-bits of itself, at most):
     (out [n, d], lse [n])."""

@@ -40,6 +40,7 @@ struct ManyPlan {                                          // what the host work
     uint32_t page_mul, page_shift;                         // token / page_tokens = token * page_mul >> page_shift
     float* part_out;                                       // [parts][n_tokens * n_q_heads][d_head]
     float2* part_sums;                                     // [parts][n_tokens * n_q_heads]: the largest score, in powers of two, and the sum
+    int32_t* order;                                        // [n_seqs] where they are more than kManyScanned: the largest start so far
 };
 
 // An item: up to r.rows rows of one sequence and KV head, row = new token * group + query head of the group, and the tokens that any of them sees.
@@ -59,24 +60,66 @@ __device__ __forceinline__ bool many_sees(const ManyPlan& p, int at, int t) {
     return !p.a.causal || (t <= at && (p.window == 0u || (uint32_t)t < p.sinks || (uint32_t)(at - t) < p.window));
 }
 
-// Items are numbered so that the first of sequence b is starts[b] * group / rows + b: a sequence of n tokens has no more than there are to the next one's.  (No prefix sum is needed; some numbers have no item.)
+// Items are numbered so that the first of sequence b is m[b] * group / rows + b, where m[b] is the largest of starts[0] .. starts[b] that are in 0..n_tokens: numbers rise with b, whatever starts holds, and a sequence that
+// begins at m[b] and has n tokens has no more items than there are numbers to the next one's.  (No prefix sum is needed; some numbers have no item.)  A sequence that begins below m[b] has none: its rows may be another's.
+//
+// Few sequences: every wave looks at all starts, 256 at a time, and works m out.  More: many_order_kernel has, in a launch before.  (By halving over starts as they are, one that does not ascend hides items of sequences before
+// and behind it.  Both ways, sequences of 1 to 4 new tokens behind 50 to 400, 32 query heads of 128 to 8, bf16, us: 256 of them 61.6 and 64.1, 500 113.3 and 113.0, 1000 222.6 and 207.5, 4000 1150 and 804.)
+constexpr int kManyScanned = 512;
+
+// The running maximum of numbers that are not negative over the lanes.
+__device__ __forceinline__ int many_running_max(int v) {
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));              // from 1, 2, 4 and 8 lanes before, of 16
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));              // lanes 15 and 47 to the 16 behind them
+    return max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));           // lane 31 to the 32 behind it
+}
+__device__ __forceinline__ int many_start_or_zero(const ManyPlan& p, int start) { return (uint32_t)start <= (uint32_t)p.a.n_tokens ? start : 0; }
+
 // The same in all lanes of a wave; all of them take part.
 __device__ inline bool many_item(const ManyPlan& p, uint32_t number, ManyItem& it) {
-    const int lane = threadIdx.x & 63;
-    const int64_t want = number;
-    auto number_of = [&](int b) { return (int64_t)p.a.starts[b] * p.group / p.r.rows + b; };
-    int lo = 0, hi = p.a.n_seqs;                           // the last sequence whose first item's number is not above the wanted one
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, b = lo + lane * step;
-        const uint64_t below = __ballot(b < hi && number_of(b < hi ? b : lo) <= want);
-        if (below == 0) break;
-        lo += (63 - __builtin_clzll(below)) * step;
-        hi = lo + step < hi ? lo + step : hi;
+    const int lane = threadIdx.x & 63, shift = __builtin_ctz((uint32_t)p.r.rows);
+    auto number_of = [&](int m, int b) { return ((uint32_t)m * (uint32_t)p.group >> shift) + (uint32_t)b; };        // (below 2^29 / 32 + 2^16)
+    int lo = -1, m = 0;                                    // the last sequence whose first item's number is not above the wanted one, and its m
+    if (p.a.n_seqs <= kManyScanned) {
+        for (int first = 0, before = 0; first < p.a.n_seqs; first += 256) {
+            int v[4];
+            bool all = true;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = first + 64 * c + lane < p.a.n_seqs ? p.a.starts[first + 64 * c + lane] : 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (first + 64 * c >= p.a.n_seqs || !all) break;
+                const int b = first + 64 * c + lane, mine = max(many_running_max(many_start_or_zero(p, v[c])), before);
+                const uint64_t below = __ballot(b < p.a.n_seqs && number_of(mine, b) <= number);
+                if (below != 0) {
+                    const int last = 63 - __builtin_clzll(below);
+                    lo = first + 64 * c + last;
+                    m = __builtin_amdgcn_readlane(mine, last);
+                }
+                all = below == ~0ull;
+                before = __builtin_amdgcn_readlane(mine, 63);
+            }
+            if (!all) break;
+        }
+    } else {
+        lo = 0;
+        for (int hi = p.a.n_seqs; hi - lo > 1;) {
+            const int step = (hi - lo + 63) / 64, b = lo + lane * step;
+            const uint64_t below = __ballot(b < hi && number_of(p.order[b < hi ? b : lo], b) <= number);
+            if (below == 0) break;
+            lo += (63 - __builtin_clzll(below)) * step;
+            hi = lo + step < hi ? lo + step : hi;
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        m = __builtin_amdgcn_readfirstlane(p.order[lo]);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
+    if (lo < 0 || number < number_of(m, lo)) return false;
     const int s0 = __builtin_amdgcn_readfirstlane(p.a.starts[lo]), s1 = __builtin_amdgcn_readfirstlane(p.a.starts[lo + 1]);
-    const int64_t block = want - ((int64_t)s0 * p.group / p.r.rows + lo);
-    if (s0 < 0 || s1 < s0 || s1 > p.a.n_tokens || block < 0) return false;
+    if (s0 != m || s1 < s0 || s1 > p.a.n_tokens) return false;
+    const int64_t block = number - number_of(m, lo);
     const int64_t all = (int64_t)(s1 - s0) * p.group, row0 = block * p.r.rows;
     if (row0 >= all) return false;
     it.b = lo;

@@ -427,6 +427,25 @@ static hipError_t launch_join(const ManyPlan& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// ---- many sequences: the largest start so far ----------------------------------------------------------------------------------
+
+// A workgroup writes 1024 of them, and looks at all starts before for itself.
+__global__ void __launch_bounds__(1024) many_order_kernel(const ManyPlan p) {
+    __shared__ int of_waves[2][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = (int)blockIdx.x * 1024, b = first + tid;
+    int before = 0;
+    for (int i = tid; i < first; i += 1024) before = max(before, many_start_or_zero(p, p.a.starts[i]));
+    before = __builtin_amdgcn_readlane(many_running_max(before), 63);
+    int v = many_running_max(many_start_or_zero(p, b < p.a.n_seqs ? p.a.starts[b] : 0));
+    if (lane == 63) {
+        of_waves[0][wave] = before;
+        of_waves[1][wave] = v;
+    }
+    __syncthreads();
+    for (int w = 0; w < 16; ++w) v = max(v, max(of_waves[0][w], w < wave ? of_waves[1][w] : 0));
+    if (b < p.a.n_seqs) p.order[b] = v;
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------------------
 
 // A kernel's rows, tokens of a tile and workgroups to a compute unit, and the time of a tile (us) where a compute unit has one workgroup and where it has all of them.
@@ -513,7 +532,7 @@ size_t many_work_bytes(const kvtc_cache& c, int n_seqs, int64_t n_tokens, int n_
         const size_t need = parts > 1 ? (size_t)parts * (size_t)n_tokens * n_q_heads * (c.d_head + 2) * sizeof(float) : 0;
         most = need > most ? need : most;
     }
-    return most + kAttendMaxShares * 4;
+    return most + kAttendMaxShares * 4 + (n_seqs > kManyScanned ? (size_t)n_seqs * 4 : 0);
 }
 
 hipError_t launch_many_mfma_0(const ManyPlan& p, hipStream_t stream);
@@ -558,6 +577,8 @@ hipError_t launch_many(const ManyArgs& a, kvtc_dtype dtype, hipStream_t stream) 
     const int64_t rows = (int64_t)a.n_tokens * a.n_q_heads;
     p.part_out = static_cast<float*>(a.work) + kAttendMaxShares;           // (behind kvtc_attend's counters)
     p.part_sums = reinterpret_cast<float2*>(p.part_out + (p.r.parts > 1 ? p.r.parts * rows * a.c.d_head : 0));
+    p.order = reinterpret_cast<int32_t*>(p.part_sums + (p.r.parts > 1 ? p.r.parts * rows : 0));
+    if (a.n_seqs > kManyScanned) hipLaunchKernelGGL(many_order_kernel, dim3((a.n_seqs + 1023) / 1024), dim3(1024), 0, stream, p);
     hipError_t e;
     if (p.r.kind == kManyPlain) {
         launch_plain_format(p, stream);
