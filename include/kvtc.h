@@ -583,14 +583,14 @@ kvtc_status kvtc_rope_scaled(const void* x_dev, void* out_dev, kvtc_dtype dtype,
  *   out_dev       [n_tokens][n_q_heads][d_head] of `dtype`, contiguous, 16-byte aligned; lse_dev [n_tokens][n_q_heads] fp32, or null
  *   work_dev      kvtc_attend_many_work_bytes(...) bytes, 256-byte aligned (work_bytes less: KVTC_E_SMALL), of any contents: calls on one stream may share it, of any sizes that it is large enough
  *                 for, with those of kvtc_attend as well (which has to have been zero before the first of these); calls that may overlap need one each.  Fewer tokens may need
- *                 more: where the sizes of calls differ, the most of what they need
+ *                 more: where the sizes of calls differ, the most of what they need.  The size serves both dtypes, with and without a window
  *   status_dev    (device, may be null; the caller zeroes it) 1 + the lowest sequence whose starts are not ascending or not in 0..n_tokens (its rows are left as they are), whose length is negative
  *                 or above max_tokens (its rows become 0 and minus infinity) or one of whose pages with seen tokens is not in the pool (those tokens are not seen).  Of starts that do not ascend,
  *                 a sequence that begins below a start before it (one in 0..n_tokens), whose rows may be another's, is left as well; the others are worked out
  * n_tokens * n_q_heads at most 2^29 (KVTC_E_UNSUPPORTED beyond).
- * fp32 queries: all in fp32.  bf16 queries: products of 16-bit numbers, summed in fp32; no key is rounded, so that lse is fp32's.  Over bf16 pages probabilities are rounded to bf16; over 8 and 4 bits to fp16, and
- * 4-bit values too (2^-11 of each).  What is more than 2^28 (4 bits: 2^23) below the largest of a row's queries, or its probabilities times values 2^28 below the largest, may be lost; a result's own rounding to
- * bf16 is the larger.
+ * fp32 queries: all in fp32.  bf16 queries: products of 16-bit numbers, summed in fp32; no key is rounded, so that lse is fp32's.  Over bf16 pages probabilities are rounded to bf16 (2^-8 of each at most; kvtc_attend
+ * keeps more of them, so that the last place of the same token's result may differ); over 8 and 4 bits to fp16, and 4-bit values too (2^-11 of each).  Over 8 and 4 bits queries more than 2^28 (4 bits: 2^23) below the
+ * largest of their row lose bits, and probabilities (8 bits: times their values' scales) below 2^-20 of the largest are off by up to 2^-31 of it: the result by that times the sum of their tokens' values.
  * Ordered on `stream`, allocates nothing, does not synchronise; n_seqs == 0 or n_tokens == 0 is a no-op.
  */
 size_t kvtc_attend_many_work_bytes(const kvtc_cache* cache, int n_seqs, int64_t n_tokens, int n_q_heads, int64_t max_tokens);     /* 0 for what kvtc_attend_many refuses */

@@ -450,7 +450,9 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 // compiler's back: the compiler neither orders later LDS reads after it nor counts it, so a
 // step's transfers can stay in flight while the previous slab is read (the builtin form makes the
 // compiler wait for vmcnt(0) before any later LDS read).  The caller owns the wait: wait_vmem<N>()
-// before the barrier that publishes the data.
+// before the barrier that publishes the data.  (M0 is reserved and cannot be named as overwritten; the compiler
+// sets it before each use of its own, of which these kernels have none.  A load must not go by M0 in the
+// instruction behind its write: one wait state.)
 __device__ __forceinline__ void dma16_async(const void* gsrc, uint32_t lds_byte_addr) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                  :: "v"(gsrc), "s"(lds_byte_addr) : "memory");

@@ -1,8 +1,8 @@
 // Attention over several sets of tokens, worked out apart, joined to attention over all of them, for gfx950.
 //
 // Of a row's parts (out_p, lse_p), with m = max lse_p:   out = sum_p e^(lse_p - m) out_p / sum_p e^(lse_p - m),   lse = m + log sum_p e^(lse_p - m).
-// Streaming, bound by memory: a lane has eight neighbouring features of a row in all parts, whose loads are on their way together, four parts at a time.  (3 fp32 parts of 6001 rows of 32 heads of 128 into bf16, 347 MB:
-// 64 us, 5.4 TB/s; 2 parts of 64 rows: 3.5 us in the kernel.)
+// A lane has eight neighbouring features of a row in all parts, one part after another: its log-sum, then, unless that is minus infinity (the row may hold anything), the features.  Large calls are bound by memory, with waves
+// enough to cover that (3 fp32 parts of 6001 rows of 32 heads of 128 into bf16, 347 MB: 64 us, 5.4 TB/s), small ones by the launch and by two latencies to a part (64 rows of 2 parts 3.5 us in the kernel, of 16 parts 10.6).
 #include <hip/hip_runtime.h>
 #include <cmath>
 #include "kvtc_cache.h"

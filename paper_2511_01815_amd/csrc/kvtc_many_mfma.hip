@@ -4,11 +4,14 @@
 // (64, or 32 to a wave), whose results are joined through the LDS in the end.
 //
 // Operands.  bf16 pages: keys, values and queries as they are, probabilities rounded to bf16 (off by 2^-8 of themselves at most, as much as the rounding of the output; sums of probabilities are of those before it).
+// Outputs are 0.00168 to 0.00173 of themselves off, of which 0.00166 are their own rounding; in two parts, 16 bits, probabilities make that 0.00166, for half as many products again: a prompt of 8192 tokens 770 us for 578, of
+// 1000 33 for 29, 8 tokens of each of 32 caches 168 for 154.  (kvtc_attend, which memory bounds, keeps 24 bits: the same token's result differs in its last place.)
 // 8 and 4 bits: fp16.  Queries times a power of two, a row's largest below 2^15 (4 bits: 2^10); codes of keys as they are.  8 bits: a token's scales go into its scores and probabilities.  4 bits: a score is the sum over groups of
 // 32 features of scale * (codes . queries), scaled in fp32, and of shift * (sum of queries), one product more with that sum in three parts: no key is rounded (rounded once to fp16 they were 20 % faster, and lse, which is fp32,
 // 1e-5 off and more); values are shift + code * scale, rounded once to fp16 (2^-11, as the probabilities; a number of the format below 2^-14 is one of fp16; 16 tokens of which one passes 2^15 are all divided by a power of two),
 // which the output's rounding to bf16 covers.  Probabilities, of 8 bits times the values' scale, are rounded to fp16.  The scales of 16 tokens' values have an exponent in common, which goes into the probabilities' exponential.
-// What is more than 2^28 (queries of 4 bits: 2^23) below the largest value so far loses bits.
+// Queries more than 2^28 (over 4 bits: 2^23) below a row's largest lose bits.  Probabilities stand 2^kBias = 2^6 times as high as they are of the largest so far (of 8 bits, times the largest scale so far): they keep 11 bits
+// down to 2^-20 of it, and are off by 2^-31 of it at most below.
 //
 // Products.  32 x 32 x 16 instructions, S^T = K Q^T and O^T = V^T P^T.  A lane has the scores of one row, of tokens 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..15, of every 32.  The second product sums over
 // tokens in that order: its operand of probabilities is what the lane has, and that of values comes out of the LDS by transposing loads of four tokens of a feature.  Maxima and sums need one exchange of halves.
@@ -20,9 +23,10 @@
 // Tiles of which some row does not see all (or that have no page) are masked, row by row, as 32 bits to 32 tokens.  Their values that are not finite are zeros in the LDS, lest a probability of zero make NaN of them, and are added
 // afterwards to the rows that see them.
 //
-// What bounds it.  Large calls: matrix products and, by the same waves in between, the softmax; two workgroups to a compute unit work at both at once.  A prompt of 8192 tokens, 32 query heads of 128 to 8: 550 us, 1000 TFLOP/s of
-// products that count, 81 % of what a large product alone reaches here (both at the clock that power leaves).  2048 tokens behind 30720: 1397 us in 8 bits, 2112 in 4: the vector unit, with scales, codes to numbers and the softmax.
-// Few items: a tile's chain of instructions, 1.0 to 2.3 us with one workgroup to a compute unit, hence parts; 6 tokens behind 131066 in 8 bits 65 us, 4.2 TB/s.
+// What bounds it.  Large calls: matrix products and, by the same waves in between, the softmax; two workgroups to a compute unit work at both at once.  A prompt of 8192 tokens, 32 query heads of 128 to 8: 570 to 580 us,
+// 960 TFLOP/s of products that count, 77 % of what a large product alone reaches here (both at the clock that power leaves).  2048 tokens behind 30720: 1405 us in 8 bits, 2100 in 4: the vector unit, with scales, codes to
+// numbers and the softmax.
+// Few items: a tile's chain of instructions, 1.0 to 2.3 us with one workgroup to a compute unit, hence parts; 6 tokens behind 131066 in 8 bits 66 us, 4.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <type_traits>
 #include "kvtc_dev.h"
