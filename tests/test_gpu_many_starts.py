@@ -81,3 +81,54 @@ def test_many_sequences(dtype, n_seqs):
         for k in rng.integers(0, n_seqs + 1, 1 + n_seqs // 200):
             starts[k] += rng.choice([-2 ** 30, -50, -1, 50, 2 ** 30])
         run(case, starts, most)
+
+
+@pytest.mark.parametrize("dtype", [kv.KVTC_BF16, kv.KVTC_F32])
+@pytest.mark.parametrize("n_seqs,had", [(3, 9000), (513, 40), (1030, 40), (600, 3000)])
+def test_nothing_is_written_behind_the_workspace(dtype, n_seqs, had):
+    """One sequence with a long context: parts, and where sequences are many, their starts in order as well."""
+    case = Case(np.random.default_rng(n_seqs), "int4", 64, 1, 2, 16, "heads", [3] + [1] * (n_seqs - 1), [had] + [5] * (n_seqs - 1), dtype)
+    need = kv.kvtc_attend_many_work_bytes(case.cache, n_seqs, case.rows, 2, max(case.lengths))
+    whole = torch.full((need + 65536,), 0xA5, dtype=torch.uint8, device=DEV)
+    out, lse, status = case.run(work=whole[:need])
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and bool((whole[need:] == 0xA5).all()) and bool((whole[:4096] == 0xA5).all())
+    case.check(out, lse, only={0, 1, n_seqs // 2, n_seqs - 1})
+    with pytest.raises(kv.KvtcError, match="KVTC_E_SMALL"):
+        case.run(work=whole[:need - 1])
+
+
+def test_many_sequences_under_capture():
+    """Starts that change between replays."""
+    rng = np.random.default_rng(31)
+    n_seqs = 700
+    case = Case(rng, "bf16", 64, 1, 2, 16, "heads", [int(n) for n in rng.integers(1, 4, n_seqs)], [int(n) for n in rng.integers(0, 40, n_seqs)], kv.KVTC_BF16)
+    spoilt = case.starts.copy()
+    spoilt[[20, 300, 650]] = -5, 3, 1 << 30
+    kinds = [torch.from_numpy(s).to(DEV) for s in (case.starts, spoilt)]
+    most = max(case.lengths)
+    work = torch.zeros(kv.kvtc_attend_many_work_bytes(case.cache, n_seqs, case.rows, 2, most), dtype=torch.uint8, device=DEV)
+    out, status = (torch.empty_like(case.q_dev), torch.empty((case.rows, 2), device=DEV)), torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def clear():
+        out[0].fill_(5.0), out[1].fill_(5.0), status.zero_()
+
+    eager = []
+    for starts in kinds:
+        case.starts_dev.copy_(starts)
+        clear()
+        case.run(out=out, status=status, work=work)
+        torch.cuda.synchronize()
+        eager.append([t.clone() for t in (*out, status)])
+    assert [int(e[2].item()) for e in eager] == [sv.served(s, case.rows)[1] for s in (case.starts, spoilt)] == [0, 20]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        case.run(out=out, status=status, work=work, stream=torch.cuda.current_stream().cuda_stream)
+    for i in (0, 1, 1, 0):
+        case.starts_dev.copy_(kinds[i])
+        clear()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*out, status), eager[i])), i
+        case.run()                                                   # the program's own eager work between replays
+        torch.cuda.synchronize()
